@@ -377,6 +377,134 @@ int craftax_stats(const void *state, craftax_metrics *out, void *workspace, size
 #define CRAFTAX_STATS_STATIC_MAX_ENVS 524288
 int craftax_stats_static(const void *state, craftax_metrics *out, int n, void *stream);
 
+/* ---- Operators of a policy with memory ------------------------------------------------------------
+ *
+ * A window of 7x9 or 9x11 cells shows little of a world, so a policy needs a memory (section
+ * "Baselines" of the paper: its strongest baseline is recurrent).  These calls are the parts of a
+ * recurrent policy block that are no plain matrix product, for acting (one token per environment
+ * and step), for reading prompts and for training on rollouts as this library writes them.  They
+ * take no state object and know nothing of the game.
+ *
+ * Activations are sequences of `steps` tokens of `n` environments with `channels` contiguous values
+ * each, of type `dtype`; a craftax_view says where value 0 of step 0 of environment 0 lies and how
+ * many values apart steps and environments are (rollouts: step = n * channels, env = channels;
+ * batch first: step = channels, env = steps * channels; for one token only env counts).  A view
+ * whose data is NULL is absent.  Parameters and their gradients are float, states of the scan too.
+ * All sums and states are kept in 32 bits and every output is rounded once.
+ *
+ * first (uint8, a view) marks the steps at which an episode begins: 1 where the craftax_step or
+ * craftax_rollout call that produced the step's observation set done.  What came before such a step
+ * is forgotten, whatever it was (infinities and NaN among it).  lengths (int32[n] or NULL) gives
+ * the number of steps that count of each environment, from 0 to `steps` (values outside are brought
+ * into that range); later steps leave the state as it is, and their outputs and gradients are 0.
+ *
+ * Conventions of this header hold: DEVICE pointers, no allocation, work is only enqueued on
+ * `stream`, nothing is launched on an error.  No result depends on the order in which blocks run.
+ * Pointers and strides only have to be aligned to their elements unless something else is said.
+ * Outputs must not overlap inputs, except that a state may be updated in place.  A workspace is
+ * DEVICE scratch, 256-byte aligned, contents irrelevant before and after; its size, for the same
+ * arguments, comes from the *_workspace_bytes call (0: none is needed).  Errors: CRAFTAX_E_NULL,
+ * CRAFTAX_E_ALIGN, CRAFTAX_E_COUNT (a size outside its range or a workspace too small),
+ * CRAFTAX_E_CONFIG (an unknown dtype, activation or number of states), CRAFTAX_E_HIP. */
+enum { CRAFTAX_F32 = 0, CRAFTAX_BF16 = 1, CRAFTAX_F16 = 2 };
+typedef struct craftax_view { void *data; int64_t step, env; } craftax_view;
+
+/* Short causal convolution of every channel: y = act(bias + sum over k of weight[k] * input k - (taps - 1)
+ * steps before), inputs before an episode's begin being 0 and inputs before step 0 coming from the
+ * state; act = x * sigmoid(x) if silu, else nothing.  The state, [n][taps - 1][channels] of `dtype`,
+ * holds the last inputs, oldest first, 0 where they no longer count. */
+typedef struct craftax_conv_args {
+    uint32_t dtype;             /* of x, y, the states and their gradients */
+    uint32_t silu;
+    int32_t steps, n, channels; /* all positive (one token: steps 1), n * channels below 2^31 - 4095 */
+    int32_t taps;               /* 2..4 */
+    const float *weight;        /* [channels][taps], the newest input last */
+    const float *bias;          /* [channels] or NULL */
+    craftax_view first;         /* uint8, or absent */
+    const int32_t *lengths;     /* or NULL */
+    craftax_view x, y;
+    const void *state_in;       /* or NULL: 0 */
+    void *state_out;            /* or NULL; may be state_in */
+    /* craftax_causal_conv_backward only */
+    craftax_view dy, dx;
+    const void *dstate_out;     /* gradient of state_out, or NULL: 0 */
+    void *dstate_in;            /* gradient of state_in, or NULL */
+    float *dweight, *dbias;     /* [channels][taps], [channels]; either NULL if not wanted */
+    void *workspace;
+    size_t workspace_bytes;
+} craftax_conv_args;
+int craftax_causal_conv(const craftax_conv_args *args, void *stream);
+/* Gradients of x, state, weight and bias; y and state_out are neither read nor written. */
+size_t craftax_causal_conv_workspace_bytes(const craftax_conv_args *args);
+int craftax_causal_conv_backward(const craftax_conv_args *args, void *stream);
+
+/* Selective state space scan.  With D = delta + delta_bias, through softplus if asked, per
+ * environment, channel and state: h = exp(D * a) * h + D * x * b, y = (sum over states of c * h + d * x) * z *
+ * sigmoid(z) (the last factors only with a gate z).  b and c are shared by channels / groups channels
+ * in a row.  The state h is float[n][channels][states].
+ * For a backward pass the forward call leaves what it needs in `saved` (DEVICE, 256-byte aligned,
+ * craftax_selective_scan_saved_bytes() long, states at regular steps); the backward call gets it
+ * with the same inputs. */
+typedef struct craftax_scan_args {
+    uint32_t dtype;             /* of x, delta, b, c, z, y and their gradients */
+    uint32_t softplus;
+    int32_t steps, n, channels; /* as above */
+    int32_t states;             /* 8, 16 or 32 */
+    int32_t groups;             /* divides channels */
+    const float *a;             /* [channels][states], 16-byte aligned */
+    const float *d;             /* [channels] or NULL */
+    const float *delta_bias;    /* [channels] or NULL */
+    craftax_view first;         /* uint8, or absent */
+    const int32_t *lengths;     /* or NULL */
+    craftax_view x, delta, z, y;   /* z may be absent */
+    craftax_view b, c;          /* [groups][states] values per step and environment, 4-byte aligned rows */
+    const float *state_in;      /* or NULL: 0; 16-byte aligned */
+    float *state_out;           /* or NULL; may be state_in; 16-byte aligned */
+    void *saved;                /* or NULL: no backward pass follows */
+    /* craftax_selective_scan_backward only */
+    craftax_view dy, dx, ddelta, dz, db, dc;
+    const float *dstate_out;    /* gradient of state_out, or NULL: 0; 16-byte aligned */
+    float *dstate_in;           /* gradient of state_in, or NULL; 16-byte aligned */
+    float *da, *dd, *ddelta_bias;  /* as a, d, delta_bias; dd and ddelta_bias NULL if not wanted; da 16-byte aligned */
+    void *workspace;
+    size_t workspace_bytes;
+} craftax_scan_args;
+size_t craftax_selective_scan_saved_bytes(const craftax_scan_args *args);
+/* backward: 0 for craftax_selective_scan, 1 for craftax_selective_scan_backward */
+size_t craftax_selective_scan_workspace_bytes(const craftax_scan_args *args, int backward);
+int craftax_selective_scan(const craftax_scan_args *args, void *stream);
+int craftax_selective_scan_backward(const craftax_scan_args *args, void *stream);
+
+/* Between two blocks, in one pass over a row (the values of a step of an environment), r(v) =
+ * 1 / sqrt(mean of v * v + eps):
+ *   branch = y * r(y) * post_weight            (norm after the block; y itself if post_weight is NULL)
+ *   out    = residual + branch * scale * act(gate)
+ *   u      = out * r(out) * pre_weight          (norm before the next block)
+ * u is computed from out before out is rounded.  out and residual are of `residual_dtype`, the other
+ * activations of `dtype`. */
+enum { CRAFTAX_GATE_SIGMOID = 0, CRAFTAX_GATE_SILU = 1, CRAFTAX_GATE_LINEAR = 2 };
+typedef struct craftax_norm_args {
+    uint32_t dtype;
+    uint32_t residual_dtype;    /* dtype or CRAFTAX_F32 */
+    uint32_t gate_act;          /* CRAFTAX_GATE_* */
+    int32_t steps, n, channels; /* steps * n (below 2^31) rows of 1..8192 values */
+    float eps;                  /* > 0 */
+    const float *post_weight;   /* [channels] or NULL: no norm after the block */
+    const float *scale;         /* [channels] or NULL: 1 */
+    const float *pre_weight;    /* [channels] or NULL: 1 */
+    craftax_view y, residual, gate;   /* gate may be absent: 1 */
+    craftax_view out, u;
+    /* craftax_residual_norm_backward only: out and u are neither read nor written */
+    craftax_view dout, du;      /* dout may be absent: 0 */
+    craftax_view dy, dresidual, dgate;   /* dgate absent if there is no gate */
+    float *dpost_weight, *dscale, *dpre_weight;   /* NULL if not wanted */
+    void *workspace;
+    size_t workspace_bytes;
+} craftax_norm_args;
+size_t craftax_residual_norm_workspace_bytes(const craftax_norm_args *args);
+int craftax_residual_norm(const craftax_norm_args *args, void *stream);
+int craftax_residual_norm_backward(const craftax_norm_args *args, void *stream);
+
 /* Debug build with bounds checks (a build of the same sources with -DCRAFTAX_DEBUG_BOUNDS, shipped
  * as libcraftax_hip_debug.so): every index the kernels form into a map, an LDS window or a staging
  * area is checked on the device; an index outside its range is counted (and replaced by 0, so that

@@ -26,6 +26,9 @@ EXPORTS = [
     "craftax_rollout", "craftax_export_envs", "craftax_import_envs", "craftax_mutate_swap", "craftax_mutate_noise", "craftax_synth_actions", "craftax_last_error",
     "craftax_stats_workspace_bytes", "craftax_stats", "craftax_stats_static",
     "craftax_debug_bounds", "craftax_debug_bounds_selftest",
+    "craftax_causal_conv", "craftax_causal_conv_backward", "craftax_causal_conv_workspace_bytes",
+    "craftax_selective_scan", "craftax_selective_scan_backward", "craftax_selective_scan_saved_bytes", "craftax_selective_scan_workspace_bytes",
+    "craftax_residual_norm", "craftax_residual_norm_backward", "craftax_residual_norm_workspace_bytes",
 ]
 
 
@@ -70,6 +73,46 @@ STATS_ACHIEVEMENTS = 96
 STATS_DTYPE = np.dtype([("episodes", "<u8"), ("steps", "<u8"), ("achievements", "<u4", (STATS_ACHIEVEMENTS,)), ("n", "<u4"), ("pad", "<u4"),
                         ("unlocks", "<u8", (STATS_ACHIEVEMENTS,))])
 assert STATS_DTYPE.itemsize == 408 + 8 * STATS_ACHIEVEMENTS
+
+
+F32, BF16, F16 = 0, 1, 2
+GATE_SIGMOID, GATE_SILU, GATE_LINEAR = 0, 1, 2
+
+
+def _view(name):
+    """The three fields of a craftax_view called `name`."""
+    return [(name, ctypes.c_void_p), (name + "_step", ctypes.c_int64), (name + "_env", ctypes.c_int64)]
+
+
+def _pointers(*names):
+    return [(name, ctypes.c_void_p) for name in names]
+
+
+def _ints(*names):
+    return [(name, ctypes.c_int32) for name in names]
+
+
+_WORKSPACE = [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class ConvArgs(ctypes.Structure):
+    _fields_ = (_ints("dtype", "silu", "steps", "n", "channels", "taps") + _pointers("weight", "bias") + _view("first") + _pointers("lengths") +
+                _view("x") + _view("y") + _pointers("state_in", "state_out") + _view("dy") + _view("dx") +
+                _pointers("dstate_out", "dstate_in", "dweight", "dbias") + _WORKSPACE)
+
+
+class ScanArgs(ctypes.Structure):
+    _fields_ = (_ints("dtype", "softplus", "steps", "n", "channels", "states", "groups") + _pointers("a", "d", "delta_bias") + _view("first") +
+                _pointers("lengths") + _view("x") + _view("delta") + _view("z") + _view("y") + _view("b") + _view("c") +
+                _pointers("state_in", "state_out", "saved") + _view("dy") + _view("dx") + _view("ddelta") + _view("dz") + _view("db") + _view("dc") +
+                _pointers("dstate_out", "dstate_in", "da", "dd", "ddelta_bias") + _WORKSPACE)
+
+
+class NormArgs(ctypes.Structure):
+    _fields_ = (_ints("dtype", "residual_dtype", "gate_act", "steps", "n", "channels") + [("eps", ctypes.c_float)] +
+                _pointers("post_weight", "scale", "pre_weight") + _view("y") + _view("residual") + _view("gate") + _view("out") + _view("u") +
+                _view("dout") + _view("du") + _view("dy") + _view("dresidual") + _view("dgate") +
+                _pointers("dpost_weight", "dscale", "dpre_weight") + _WORKSPACE)
 
 
 class CraftaxError(RuntimeError):
@@ -139,6 +182,14 @@ def load() -> ctypes.CDLL:
     L.craftax_stats_static.argtypes = [vp, vp, i32, vp]
     L.craftax_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32 * 4)]
     L.craftax_debug_bounds_selftest.argtypes = []
+    for name, args in (("causal_conv", ConvArgs), ("selective_scan", ScanArgs), ("residual_norm", NormArgs)):
+        for call in (name, name + "_backward"):
+            getattr(L, "craftax_" + call).argtypes = [ctypes.POINTER(args), vp]
+        size = getattr(L, f"craftax_{name}_workspace_bytes")
+        size.argtypes = [ctypes.POINTER(args)] + ([i32] if name == "selective_scan" else [])
+        size.restype = ctypes.c_size_t
+    L.craftax_selective_scan_saved_bytes.argtypes = [ctypes.POINTER(ScanArgs)]
+    L.craftax_selective_scan_saved_bytes.restype = ctypes.c_size_t
     L.craftax_last_error.argtypes = []
     L.craftax_last_error.restype = ctypes.c_char_p
     _lib = L

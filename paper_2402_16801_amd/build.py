@@ -5,7 +5,7 @@ import os
 import subprocess
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(_PKG, "csrc", f) for f in ("craftax.hip", "full.hip")]
+SRCS = [os.path.join(_PKG, "csrc", f) for f in ("craftax.hip", "full.hip", "memory_conv.hip", "memory_scan.hip", "memory_norm.hip")]
 OUT = os.path.join(_PKG, "libcraftax_hip.so")
 
 HIPCC_FLAGS = [

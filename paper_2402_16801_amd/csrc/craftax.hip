@@ -14,6 +14,7 @@
 
 #include "common.hpp"
 #include "full_api.hpp"
+#include "memory_api.hpp"
 #include "launch_limits.hpp"
 #include "lookahead.hpp"
 #include "regen_units.hpp"
@@ -1691,6 +1692,57 @@ int craftax_stats(const void* state, craftax_metrics* out, void* workspace, size
     if (workspace_bytes < craftax_stats_workspace_bytes(n)) return fail(CRAFTAX_E_COUNT, "workspace smaller than craftax_stats_workspace_bytes(n)");
     if (int rc = need_worlds(s)) return rc;
     return launch_stats(state, s, out, static_cast<uint32_t*>(workspace), n, (hipStream_t)stream);
+}
+
+// ---- operators of a policy with memory (csrc/memory_*.hip): the message of a refusal goes to craftax_last_error ----
+static int memory_call(int rc, const char* why)
+{
+    try {
+        return rc == CRAFTAX_OK ? rc : fail(rc, why);
+    } catch (...) {       // no memory for the message
+        return rc;
+    }
+}
+
+int craftax_causal_conv(const craftax_conv_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::conv(args, stream, &why);
+    return memory_call(rc, why);
+}
+size_t craftax_causal_conv_workspace_bytes(const craftax_conv_args* args) { return mem::host::conv_workspace_bytes(args); }
+int craftax_causal_conv_backward(const craftax_conv_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::conv_backward(args, stream, &why);
+    return memory_call(rc, why);
+}
+size_t craftax_selective_scan_saved_bytes(const craftax_scan_args* args) { return mem::host::scan_saved_bytes(args); }
+size_t craftax_selective_scan_workspace_bytes(const craftax_scan_args* args, int backward) { return mem::host::scan_workspace_bytes(args, backward != 0); }
+int craftax_selective_scan(const craftax_scan_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::scan(args, stream, &why);
+    return memory_call(rc, why);
+}
+int craftax_selective_scan_backward(const craftax_scan_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::scan_backward(args, stream, &why);
+    return memory_call(rc, why);
+}
+size_t craftax_residual_norm_workspace_bytes(const craftax_norm_args* args) { return mem::host::norm_workspace_bytes(args); }
+int craftax_residual_norm(const craftax_norm_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::norm(args, stream, &why);
+    return memory_call(rc, why);
+}
+int craftax_residual_norm_backward(const craftax_norm_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::norm_backward(args, stream, &why);
+    return memory_call(rc, why);
 }
 
 int craftax_debug_bounds(uint32_t report[4])

@@ -1,0 +1,420 @@
+// Between two blocks: norm after the block, gate, scale, residual, norm before the next block, in one
+// pass over a row, and the backward pass.
+//
+// Bound by memory: a row is read once, kept in registers, and written once (forward 3 in, 2 out with a gate;
+// backward 5 in, 3 out).  The backward pass computes the two roots again from the row, which is there
+// anyway, so nothing is saved between the passes.  A row belongs to W wavefronts, as few as hold it with 16
+// values per lane; with one wavefront every sum stays inside it, with more the sums meet in LDS.
+// Blocks go on to further rows with the weights, and in the backward pass their gradients, in registers.
+#include "memory_api.hpp"
+#include "memory_common.hpp"
+
+#include <type_traits>
+
+namespace mem {
+
+template <typename E, typename R> struct NormParams {
+    const float *post_weight, *scale, *pre_weight;
+    Seq<const E> y, gate, du;
+    Seq<const R> residual, dout;
+    Seq<E> u, dy, dgate;
+    Seq<R> out, dresidual;
+    float* part;               // backward: [blocks][3][channels]
+    uint32_t rows, n;
+    int channels, gate_act;
+    float eps;
+};
+
+// sum over the W wavefronts of a row, in every lane; slots: W floats of LDS for this row and this sum
+template <int W>
+__device__ __forceinline__ float row_sum(float v, float* slots)
+{
+    v = wave_sum(v);
+    if constexpr (W > 1) {
+        const int lane = threadIdx.x & (WAVE - 1), wave = (threadIdx.x / WAVE) % W;
+        if (lane == 0) slots[wave] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) v += slots[k];
+    }
+    return v;
+}
+
+__device__ __forceinline__ float gate_value(float g, int act)
+{
+    if (act == CRAFTAX_GATE_LINEAR) return g;
+    const float s = sigmoid(g);
+    return act == CRAFTAX_GATE_SIGMOID ? s : g * s;
+}
+__device__ __forceinline__ float gate_slope(float g, int act)
+{
+    if (act == CRAFTAX_GATE_LINEAR) return 1.0f;
+    const float s = sigmoid(g);
+    return act == CRAFTAX_GATE_SIGMOID ? s * (1.0f - s) : s * __builtin_fmaf(g, 1.0f - s, 1.0f);
+}
+
+// What is left of g without its part along the unit row, g - unit * mean(g * unit).  The mean of unit * unit is
+// 1 - eps * root * root, so in a row of one value only eps * root * root * g is left, which the difference of the two
+// terms would not show in 32 bits.
+template <int W, typename P>
+__device__ __forceinline__ float off_axis(const P& p, float g, float unit, float along, float root)
+{
+    if (W == 1 && p.channels == 1) return p.eps * root * root * g;
+    return __builtin_fmaf(-unit, along, g);
+}
+
+template <int W> struct RowBlock {
+    static constexpr int THREADS = W * WAVE > 256 ? W * WAVE : 256;
+    static constexpr int ROWS = THREADS / (W * WAVE);      // rows a block works on at once
+};
+
+template <int CHUNKS, int V> struct RowPlace {
+    int at[CHUNKS], count[CHUNKS];       // first value and number of values of this lane's chunks
+    __device__ __forceinline__ RowPlace(int channels, int side, int width)
+    {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            at[c] = (c * width + side) * V;
+            const int left = channels - at[c];
+            count[c] = left < 0 ? 0 : (left < V ? left : V);
+        }
+    }
+};
+
+template <int CHUNKS, int V, typename P, typename T>
+__device__ __forceinline__ void load_chunks(const RowPlace<CHUNKS, V>& place, const P* p, T (&v)[CHUNKS][V])
+{
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) load_row<P, V>(p + place.at[c], place.count[c], v[c]);
+}
+template <int CHUNKS, int V, typename P>
+__device__ __forceinline__ void store_chunks(const RowPlace<CHUNKS, V>& place, P* p, const float (&v)[CHUNKS][V])
+{
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) store_row<P, V>(p + place.at[c], place.count[c], v[c]);
+}
+template <int CHUNKS, int V>
+__device__ __forceinline__ void load_weight(const RowPlace<CHUNKS, V>& place, const float* p, float (&v)[CHUNKS][V])
+{
+    if (p) { load_chunks<CHUNKS, V>(place, p, v); return; }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[c][j] = 1.0f;
+}
+
+template <typename E, typename R, int W, int CHUNKS>
+__global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<E, R> p)
+{
+    constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS;
+    __shared__ float slots[2][ROWS][W];
+    const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (W * WAVE));
+    const RowPlace<CHUNKS, V> place(p.channels, threadIdx.x % (W * WAVE), W * WAVE);
+    float w1[CHUNKS][V], scale[CHUNKS][V], w2[CHUNKS][V];
+    load_weight<CHUNKS, V>(place, p.post_weight, w1);
+    load_weight<CHUNKS, V>(place, p.scale, scale);
+    load_weight<CHUNKS, V>(place, p.pre_weight, w2);
+    const float mean = 1.0f / (float)p.channels;
+    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += gridDim.x * ROWS) {
+        const bool on = base + which < p.rows;
+        const uint32_t row = on ? base + which : p.rows - 1;
+        const int t = (int)(row / p.n), i = (int)(row % p.n);
+        float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V];
+        load_chunks<CHUNKS, V>(place, p.y.at(t, i), y);
+        load_chunks<CHUNKS, V>(place, p.residual.at(t, i), r);
+        if (p.gate.data) load_chunks<CHUNKS, V>(place, p.gate.at(t, i), g);
+        float root = 1.0f;
+        if (p.post_weight) {
+            float s = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) s = __builtin_fmaf(y[c][j], y[c][j], s);
+            root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
+        }
+        float s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float branch = y[c][j] * root * w1[c][j] * scale[c][j];
+                if (p.gate.data) branch *= gate_value(g[c][j], p.gate_act);
+                r[c][j] += branch;
+                if (j < place.count[c]) s = __builtin_fmaf(r[c][j], r[c][j], s);
+            }
+        root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
+        if (on) {
+            store_chunks<CHUNKS, V>(place, p.out.at(t, i), r);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) r[c][j] = r[c][j] * root * w2[c][j];
+            store_chunks<CHUNKS, V>(place, p.u.at(t, i), r);
+        }
+        if (W > 1) __syncthreads();
+    }
+}
+
+template <typename E, typename R, int W, int CHUNKS>
+__global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const NormParams<E, R> p)
+{
+    constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS, THREADS = RowBlock<W>::THREADS;
+    __shared__ float slots[4][ROWS][W];
+    __shared__ float sums[ROWS > 1 ? THREADS * CHUNKS * V : 1];
+    const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (W * WAVE)), side = threadIdx.x % (W * WAVE);
+    const RowPlace<CHUNKS, V> place(p.channels, side, W * WAVE);
+    float w1[CHUNKS][V], scale[CHUNKS][V], w2[CHUNKS][V];
+    load_weight<CHUNKS, V>(place, p.post_weight, w1);
+    load_weight<CHUNKS, V>(place, p.scale, scale);
+    load_weight<CHUNKS, V>(place, p.pre_weight, w2);
+    float d1[CHUNKS][V] = {}, ds[CHUNKS][V] = {}, d2[CHUNKS][V] = {};
+    const float mean = 1.0f / (float)p.channels;
+    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += gridDim.x * ROWS) {
+        const bool on = base + which < p.rows;
+        const uint32_t row = on ? base + which : p.rows - 1;
+        const int t = (int)(row / p.n), i = (int)(row % p.n);
+        float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V], du[CHUNKS][V], dr[CHUNKS][V];
+        load_chunks<CHUNKS, V>(place, p.y.at(t, i), y);
+        load_chunks<CHUNKS, V>(place, p.residual.at(t, i), r);
+        if (p.gate.data) load_chunks<CHUNKS, V>(place, p.gate.at(t, i), g);
+        load_chunks<CHUNKS, V>(place, p.du.at(t, i), du);
+        if (p.dout.data) load_chunks<CHUNKS, V>(place, p.dout.at(t, i), dr);
+        float root_y = 1.0f;
+        if (p.post_weight) {
+            float s = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) s = __builtin_fmaf(y[c][j], y[c][j], s);
+            root_y = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
+        }
+        // out again, its root, and the sum over the row of (du w2) (out root)
+        float s = 0.0f, m = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                y[c][j] *= root_y;                                   // from here on without its scale
+                float branch = y[c][j] * w1[c][j] * scale[c][j];
+                if (p.gate.data) branch *= gate_value(g[c][j], p.gate_act);
+                r[c][j] += branch;
+                if (j < place.count[c]) s = __builtin_fmaf(r[c][j], r[c][j], s);
+            }
+        const float root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                r[c][j] *= root;
+                if (on && j < place.count[c]) d2[c][j] = __builtin_fmaf(du[c][j], r[c][j], d2[c][j]);
+                du[c][j] *= w2[c][j];
+                if (j < place.count[c]) m = __builtin_fmaf(du[c][j], r[c][j], m);
+            }
+        m = row_sum<W>(m, slots[2][which]) * mean;
+        float q = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = __builtin_fmaf(root, off_axis<W>(p, du[c][j], r[c][j], m, root), p.dout.data ? dr[c][j] : 0.0f);
+                dr[c][j] = d;
+                const float act = p.gate.data ? gate_value(g[c][j], p.gate_act) : 1.0f;
+                const float v = y[c][j] * w1[c][j];
+                if (on && j < place.count[c]) ds[c][j] = __builtin_fmaf(d * v, act, ds[c][j]);
+                const float dv = d * scale[c][j] * act;
+                if (p.gate.data) g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
+                if (on && j < place.count[c]) d1[c][j] = __builtin_fmaf(dv, y[c][j], d1[c][j]);
+                du[c][j] = dv * w1[c][j];
+                if (j < place.count[c]) q = __builtin_fmaf(du[c][j], y[c][j], q);
+            }
+        if (on) {
+            store_chunks<CHUNKS, V>(place, p.dresidual.at(t, i), dr);
+            if (p.gate.data) store_chunks<CHUNKS, V>(place, p.dgate.at(t, i), g);
+        }
+        if (p.post_weight) {
+            q = row_sum<W>(q, slots[3][which]) * mean;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) du[c][j] = root_y * off_axis<W>(p, du[c][j], y[c][j], q, root_y);
+        }
+        if (on) store_chunks<CHUNKS, V>(place, p.dy.at(t, i), du);
+        if (W > 1) __syncthreads();
+    }
+    if (p.part == nullptr) return;
+    // one partial row per block and weight; the rows that a block works on at once are added up in LDS
+    auto put = [&](int weight, const float (&v)[CHUNKS][V]) {
+        float* out = p.part + ((int64_t)blockIdx.x * 3 + weight) * p.channels;
+        if constexpr (ROWS == 1) {
+            store_chunks<CHUNKS, V>(place, out, v);
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sums[(c * V + j) * THREADS + threadIdx.x] = v[c][j];
+            __syncthreads();
+            if (which == 0) {
+                float total[CHUNKS][V];
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        total[c][j] = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < ROWS; ++k) total[c][j] += sums[(c * V + j) * THREADS + k * (W * WAVE) + side];
+                    }
+                store_chunks<CHUNKS, V>(place, out, total);
+            }
+        }
+    };
+    put(0, d1);
+    put(1, ds);
+    put(2, d2);
+}
+
+struct PutNorm {
+    float* out[3];
+    int channels;
+    __device__ void operator()(int64_t column, float v) const
+    {
+        const int which = (int)(column / channels);
+        float* p = which == 0 ? out[0] : which == 1 ? out[1] : out[2];
+        if (p) p[column - (int64_t)which * channels] = v;
+    }
+};
+
+namespace host {
+
+constexpr int NORM_CHANNELS = 8192;
+
+static int norm_check(const craftax_norm_args* a, bool backward, const char** why)
+{
+    if (!a) return refuse(CRAFTAX_E_NULL, "args is NULL", why);
+    if (a->dtype > CRAFTAX_F16) return refuse(CRAFTAX_E_CONFIG, "unknown dtype", why);
+    if (a->residual_dtype != a->dtype && a->residual_dtype != CRAFTAX_F32) return refuse(CRAFTAX_E_CONFIG, "residual_dtype must be dtype or CRAFTAX_F32", why);
+    if (a->gate_act > CRAFTAX_GATE_LINEAR) return refuse(CRAFTAX_E_CONFIG, "unknown gate_act", why);
+    if (!(a->eps > 0.0f)) return refuse(CRAFTAX_E_CONFIG, "eps must be positive", why);
+    if (a->steps < 1 || a->n < 1) return refuse(CRAFTAX_E_COUNT, "steps and n must be positive", why);
+    if ((int64_t)a->steps * a->n >= (int64_t)1 << 31) return refuse(CRAFTAX_E_COUNT, "steps * n must be below 2^31", why);
+    if (a->channels < 1 || a->channels > NORM_CHANNELS) return refuse(CRAFTAX_E_COUNT, "channels must be 1..8192", why);
+    if (!a->y.data || !a->residual.data) return refuse(CRAFTAX_E_NULL, "y or residual is NULL", why);
+    const size_t e = elem_bytes(a->dtype), r = elem_bytes(a->residual_dtype);
+    if (!aligned(a->y.data, e) || !aligned(a->gate.data, e) || !aligned(a->residual.data, r) || !aligned(a->post_weight, 4) ||
+        !aligned(a->scale, 4) || !aligned(a->pre_weight, 4))
+        return refuse(CRAFTAX_E_ALIGN, "a pointer is not aligned to its elements", why);
+    if (!backward) {
+        if (!a->out.data || !a->u.data) return refuse(CRAFTAX_E_NULL, "out or u is NULL", why);
+        if (!aligned(a->out.data, r) || !aligned(a->u.data, e)) return refuse(CRAFTAX_E_ALIGN, "a pointer is not aligned to its elements", why);
+        return CRAFTAX_OK;
+    }
+    if (!a->du.data || !a->dy.data || !a->dresidual.data) return refuse(CRAFTAX_E_NULL, "du, dy or dresidual is NULL", why);
+    if (a->gate.data && !a->dgate.data) return refuse(CRAFTAX_E_NULL, "dgate is NULL", why);
+    if (!aligned(a->du.data, e) || !aligned(a->dy.data, e) || !aligned(a->dgate.data, e) || !aligned(a->dout.data, r) || !aligned(a->dresidual.data, r) ||
+        !aligned(a->dpost_weight, 4) || !aligned(a->dscale, 4) || !aligned(a->dpre_weight, 4))
+        return refuse(CRAFTAX_E_ALIGN, "a pointer is not aligned to its elements", why);
+    return CRAFTAX_OK;
+}
+
+template <typename E, typename R> static NormParams<E, R> norm_params(const craftax_norm_args* a)
+{
+    NormParams<E, R> p{};
+    p.post_weight = a->post_weight; p.scale = a->scale; p.pre_weight = a->pre_weight;
+    p.y = seq_in<E>(a->y); p.gate = seq_in<E>(a->gate); p.du = seq_in<E>(a->du);
+    p.residual = seq_in<R>(a->residual); p.dout = seq_in<R>(a->dout);
+    p.u = seq<E>(a->u); p.dy = seq<E>(a->dy); p.dgate = seq<E>(a->dgate);
+    p.out = seq<R>(a->out); p.dresidual = seq<R>(a->dresidual);
+    p.rows = (uint32_t)((int64_t)a->steps * a->n); p.n = (uint32_t)a->n; p.channels = a->channels; p.gate_act = (int)a->gate_act; p.eps = a->eps;
+    return p;
+}
+
+// Wavefronts per row: as few (1, 2, 4, 8) as hold it with 16 values per lane.
+static int row_waves(int channels)
+{
+    int w = 1;
+    while (w < 8 && w * WAVE * 16 < channels) w *= 2;
+    return w;
+}
+static int row_threads(int w) { return w * WAVE > 256 ? w * WAVE : 256; }
+
+// Blocks: all that the chip holds at once, then on to further rows.
+static unsigned row_blocks(const craftax_norm_args* a, int waves_per_simd)
+{
+    const int w = row_waves(a->channels), threads = row_threads(w);
+    const int64_t need = ceil_div((int64_t)a->steps * a->n, threads / (w * WAVE));
+    const int64_t most = (int64_t)CHIP_SIMDS * waves_per_simd * WAVE / threads;
+    return (unsigned)(need < most ? need : most);
+}
+constexpr int NORM_WAVES = 8, NORM_BACK_WAVES = 4;
+
+// calls f with the element types, the wavefronts per row and the chunks per lane as constants
+template <typename F> static void with_row(const craftax_norm_args* a, F&& f)
+{
+    const int w = row_waves(a->channels);
+    with_type(a->dtype, [&](auto e) {
+        using E = decltype(e);
+        constexpr int V = 16 / sizeof(E);
+        auto chunks = [&](auto r, auto wc) {
+            constexpr int W = decltype(wc)::value;
+            if (a->channels <= W * WAVE * V) f(e, r, wc, std::integral_constant<int, 1>{});
+            else if (V == 8 || a->channels <= W * WAVE * V * 2) f(e, r, wc, std::integral_constant<int, 2>{});
+            else f(e, r, wc, std::integral_constant<int, V == 8 ? 2 : 4>{});
+        };
+        auto waves = [&](auto r) {
+            if (w == 1) chunks(r, std::integral_constant<int, 1>{});
+            else if (w == 2) chunks(r, std::integral_constant<int, 2>{});
+            else if (w == 4) chunks(r, std::integral_constant<int, 4>{});
+            else chunks(r, std::integral_constant<int, 8>{});
+        };
+        if (a->residual_dtype == CRAFTAX_F32) waves(float{});
+        else waves(E{});
+    });
+}
+
+int norm(const craftax_norm_args* a, void* stream, const char** why)
+{
+    if (int rc = norm_check(a, false, why)) return rc;
+    with_row(a, [&](auto e, auto r, auto w, auto chunks) {
+        using E = decltype(e);
+        using R = decltype(r);
+        constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
+        hipLaunchKernelGGL((k_norm<E, R, W, C>), dim3(row_blocks(a, NORM_WAVES)), dim3(RowBlock<W>::THREADS), 0, (hipStream_t)stream,
+                           (norm_params<E, R>(a)));
+    });
+    return launched(why);
+}
+
+size_t norm_workspace_bytes(const craftax_norm_args* a)
+{
+    if (!a || a->steps < 1 || a->n < 1 || a->channels < 1 || a->channels > NORM_CHANNELS) return 0;
+    if (!a->dpost_weight && !a->dscale && !a->dpre_weight) return 0;
+    return round256((size_t)row_blocks(a, NORM_BACK_WAVES) * 3 * a->channels * sizeof(float));
+}
+
+int norm_backward(const craftax_norm_args* a, void* stream, const char** why)
+{
+    if (int rc = norm_check(a, true, why)) return rc;
+    const size_t need = norm_workspace_bytes(a);
+    if (need && !a->workspace) return refuse(CRAFTAX_E_NULL, "workspace is NULL", why);
+    if (need && !aligned(a->workspace, 256)) return refuse(CRAFTAX_E_ALIGN, "workspace must be 256-byte aligned", why);
+    if (a->workspace_bytes < need) return refuse(CRAFTAX_E_COUNT, "workspace smaller than craftax_residual_norm_workspace_bytes", why);
+    const unsigned blocks = row_blocks(a, NORM_BACK_WAVES);
+    const hipStream_t st = (hipStream_t)stream;
+    with_row(a, [&](auto e, auto r, auto w, auto chunks) {
+        using E = decltype(e);
+        using R = decltype(r);
+        constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
+        NormParams<E, R> p = norm_params<E, R>(a);
+        p.part = need ? static_cast<float*>(a->workspace) : nullptr;
+        hipLaunchKernelGGL((k_norm_backward<E, R, W, C>), dim3(blocks), dim3(RowBlock<W>::THREADS), 0, st, p);
+    });
+    if (int rc = launched(why)) return rc;
+    if (need)
+        sum_rows(static_cast<const float*>(a->workspace), (int)blocks, (int64_t)3 * a->channels,
+                 PutNorm{{a->post_weight ? a->dpost_weight : nullptr, a->dscale, a->dpre_weight}, a->channels}, st);
+    return launched(why);
+}
+
+}  // namespace host
+}  // namespace mem
