@@ -92,6 +92,9 @@ __device__ __forceinline__ float softplus(float v)
     return (v < 0.0f ? 0.0f : v) + q * r;
 }
 
+// v is computed here, not where it is used
+__device__ __forceinline__ void pin(float& v) { asm volatile("" : "+v"(v)); }
+
 // ---- moves across lanes ----------------------------------------------------------------------------
 template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {

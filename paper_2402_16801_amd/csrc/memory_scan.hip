@@ -7,12 +7,15 @@
 // to 12 bytes: vector issue bounds sequences, memory bounds single tokens (the state is read and written
 // for one step of work).
 //
-// Sequences: a lane is a channel and holds all of its states, so y is a sum inside the lane; a wavefront is
-// 64 channels of one group of one environment, so b and c are the same in all lanes and come through
-// scalar loads into scalar registers, which the multiplications take directly.  Where environments and
-// channels do not fill the chip, the steps are split too ("parts"): a first kernel gives every part's
-// effect on the state (its end from zero, and the sum of D, which is the exponent of the decay), a
-// second carries the states through the parts, and the third runs the parts from their own starts.
+// Sequences: a lane holds four states of a channel, so N / 4 neighbouring lanes are a channel and a wavefront
+// is 64 / (N / 4) channels of one group of one environment.  It goes on by blocks of eight steps.  What a step
+// needs of a channel (D and D x) is computed once, by the lane that owns the step, and handed to the
+// channel's lanes through LDS, as are b and c, which all channels read; y of eight steps is summed over the
+// channel's lanes by folding, which leaves each lane the steps it owns.  Everything in LDS belongs to one
+// wavefront, so there are no barriers.  Where environments and channels do not fill the chip, the steps are
+// split too ("parts"): a first kernel gives every part's effect on the state (its end from zero, and the
+// sum of D, which is the exponent of the decay), a second carries the states through the parts, and the
+// third runs the parts from their own starts.
 #include "memory_api.hpp"
 #include "memory_common.hpp"
 
@@ -22,7 +25,14 @@ namespace mem {
 
 constexpr int SCAN_THREADS = 256;                      // four wavefronts, each with a tile of its own
 constexpr int SCAN_WAVES = SCAN_THREADS / WAVE;
-constexpr int AHEAD = 8;                               // steps whose activations are loaded together
+constexpr int BLOCK = 8;                               // steps that are worked on together
+
+// How N states lie on a wavefront.
+template <int N> struct Lay {
+    static constexpr int LANES = N / 4;                // lanes of a channel, four states each: 2, 4 or 8
+    static constexpr int CHANNELS = WAVE / LANES;      // channels of a wavefront
+    static constexpr int OWN = BLOCK / LANES;          // steps of a block that a lane owns: lane q the steps q * OWN ..
+};
 
 template <typename E> struct ScanParams {
     const float *a, *d, *delta_bias;
@@ -32,31 +42,34 @@ template <typename E> struct ScanParams {
     Seq<E> y, dx, ddelta, dz;
     const float *state_in, *dstate_out;
     float *state_out, *dstate_in;
-    float4* starts;        // states at the start of each part, tiled (see tiled_state)
-    float2* decays;        // per part, environment, tile and lane: sum of D since the last begin of an episode, 1 if one began
-    float4* saved;         // states before every SAVE_STEPS-th step, tiled
-    float* shared_part;    // backward: [step][n][tiles][2 * N] sums over a tile for db and dc
+    float4* starts;        // states at the start of each part, [part][n][tile][lane]
+    float2* decays;        // per part, environment, tile and channel: sum of D since the last begin of an episode, 1 if one began
+    float4* saved;         // states before every block of steps, [block][n][tile][lane]
+    float* shared_part;    // backward: [step][n][groups][group_blocks][2 * N] sums for db and dc
     float* weight_part;    // backward: [rows][channels][N + 2] sums for da, dd and ddelta_bias
     int steps, n, channels, groups, group_channels, group_tiles, tiles, softplus;
-    int part, parts;       // steps per part, number of parts
-    int rows;              // backward: rows of weight_part
+    int part, parts;       // steps per part (whole blocks), number of parts
+    int rows, waves, group_blocks;   // backward: rows of weight_part, wavefronts per block, blocks per group
 };
 
-// What a wavefront works on: 64 channels of one group (`tile`) of one environment.
+// What a wavefront works on: some channels of one group (`tile`) of one environment.
 struct Tile {
-    int tile, group, channel;      // channel of this lane; the group's last one where the lane has none
+    int tile, group, quad;         // quad: the lane's four states are 4 * quad ..
+    uint32_t channel;              // channel of this lane; the group's last one where the lane has none
     bool owns;                     // the lane has a channel
 };
 
-template <typename E>
+template <int N, typename E>
 __device__ __forceinline__ Tile tile_of(const ScanParams<E>& p, int tile)
 {
+    const int lane = (int)(threadIdx.x & (WAVE - 1));
     Tile w;
     w.tile = tile;
     w.group = tile / p.group_tiles;
-    const int in_group = (tile % p.group_tiles) * WAVE + (int)(threadIdx.x & (WAVE - 1));
+    w.quad = lane % Lay<N>::LANES;
+    const int in_group = (tile % p.group_tiles) * Lay<N>::CHANNELS + lane / Lay<N>::LANES;
     w.owns = in_group < p.group_channels;
-    w.channel = w.group * p.group_channels + (w.owns ? in_group : p.group_channels - 1);
+    w.channel = (uint32_t)(w.group * p.group_channels + (w.owns ? in_group : p.group_channels - 1));
     return w;
 }
 
@@ -78,247 +91,269 @@ __device__ __forceinline__ uint64_t begins(const ScanParams<E>& p, int t, int en
     return __ballot(on);
 }
 
-// N shared values of a step (b or c of the group), in scalar registers.
-template <typename E, int N> struct Shared;
-template <int N> struct Shared<float, N> {
-    float v[N];
-    __device__ __forceinline__ void load(const float* p)
-    {
-        const __attribute__((address_space(4))) float* q = (const __attribute__((address_space(4))) float*)(uintptr_t)p;
-#pragma unroll
-        for (int n = 0; n < N; ++n) v[n] = q[n];
-    }
-    __device__ __forceinline__ float operator[](int n) const { return v[n]; }
-};
-template <int N> struct Shared<__bf16, N> {
-    uint32_t v[N / 2];
-    __device__ __forceinline__ void load(const __bf16* p)
-    {
-        const __attribute__((address_space(4))) uint32_t* q = (const __attribute__((address_space(4))) uint32_t*)(uintptr_t)p;
-#pragma unroll
-        for (int n = 0; n < N / 2; ++n) v[n] = q[n];
-    }
-    __device__ __forceinline__ float operator[](int n) const { return __uint_as_float(n & 1 ? v[n / 2] & 0xffff0000u : v[n / 2] << 16); }
-};
-template <int N> struct Shared<_Float16, N> {
-    uint32_t v[N / 2];
-    __device__ __forceinline__ void load(const _Float16* p)
-    {
-        const __attribute__((address_space(4))) uint32_t* q = (const __attribute__((address_space(4))) uint32_t*)(uintptr_t)p;
-#pragma unroll
-        for (int n = 0; n < N / 2; ++n) v[n] = q[n];
-    }
-    __device__ __forceinline__ float operator[](int n) const
-    {
-        return (float)__builtin_bit_cast(_Float16, (uint16_t)(n & 1 ? v[n / 2] >> 16 : v[n / 2] & 0xffffu));
-    }
-};
-
-// State in a workspace: [...][tile][N / 4][lane] float4, so that a wavefront moves whole kilobytes.
-template <int N>
-__device__ __forceinline__ float4* tiled_state(float4* base, int64_t index, const Tile& w, int tiles)
+// Four states of this lane in a workspace ([index][tile][lane]) and as the caller has them ([n][channels][N]).
+__device__ __forceinline__ float4* tiled(float4* base, int64_t index, const Tile& w, int tiles)
 {
-    return base + ((index * tiles + w.tile) * (N / 4)) * WAVE + (threadIdx.x & (WAVE - 1));
+    return base + (index * tiles + w.tile) * WAVE + (threadIdx.x & (WAVE - 1));
 }
-template <int N> __device__ __forceinline__ void load_tiled(const float4* q, float (&h)[N])
+template <int N, typename P> __device__ __forceinline__ P* state_of(P* state, int channels, int i, const Tile& w)
 {
-#pragma unroll
-    for (int k = 0; k < N / 4; ++k) {
-        const float4 v = q[k * WAVE];
-        h[4 * k] = v.x; h[4 * k + 1] = v.y; h[4 * k + 2] = v.z; h[4 * k + 3] = v.w;
-    }
+    return state + ((int64_t)i * channels + w.channel) * N + w.quad * 4;
 }
-template <int N> __device__ __forceinline__ void store_tiled(float4* q, const float (&h)[N])
+__device__ __forceinline__ void load4(const void* p, float (&h)[4])
 {
-#pragma unroll
-    for (int k = 0; k < N / 4; ++k) q[k * WAVE] = make_float4(h[4 * k], h[4 * k + 1], h[4 * k + 2], h[4 * k + 3]);
+    const float4 v = *static_cast<const float4*>(p);
+    h[0] = v.x; h[1] = v.y; h[2] = v.z; h[3] = v.w;
 }
-// State as the caller has it: [n][channels][N].
-template <int N> __device__ __forceinline__ void load_state(const float* state, int64_t index, float (&h)[N])
-{
-    const float4* q = reinterpret_cast<const float4*>(state + index * N);
-#pragma unroll
-    for (int k = 0; k < N / 4; ++k) {
-        const float4 v = q[k];
-        h[4 * k] = v.x; h[4 * k + 1] = v.y; h[4 * k + 2] = v.z; h[4 * k + 3] = v.w;
-    }
-}
-template <int N> __device__ __forceinline__ void store_state(float* state, int64_t index, const float (&h)[N])
-{
-    float4* q = reinterpret_cast<float4*>(state + index * N);
-#pragma unroll
-    for (int k = 0; k < N / 4; ++k) q[k] = make_float4(h[4 * k], h[4 * k + 1], h[4 * k + 2], h[4 * k + 3]);
-}
-template <int N> __device__ __forceinline__ void zero(float (&h)[N])
-{
-#pragma unroll
-    for (int n = 0; n < N; ++n) h[n] = 0.0f;
-}
+__device__ __forceinline__ void store4(void* p, const float (&h)[4]) { *static_cast<float4*>(p) = make_float4(h[0], h[1], h[2], h[3]); }
+__device__ __forceinline__ void zero(float (&h)[4]) { h[0] = h[1] = h[2] = h[3] = 0.0f; }
 
 // The decay's exponent is taken to base 2: a is scaled once.
-template <int N> __device__ __forceinline__ void load_rates(const float* a, int channel, float (&a2)[N])
+template <int N> __device__ __forceinline__ void load_rates(const float* a, const Tile& w, float (&a2)[4])
 {
-    load_state<N>(a, channel, a2);
+    load4(a + (int64_t)w.channel * N + w.quad * 4, a2);
 #pragma unroll
-    for (int n = 0; n < N; ++n) a2[n] *= LOG2E;
+    for (int m = 0; m < 4; ++m) a2[m] *= LOG2E;
 }
 
-// States are saved before every SAVE-th step for the backward pass, which holds SAVE * N of them per lane.
-template <int N> struct Save { static constexpr int STEPS = 128 / N; };
+// Where a lane reads or writes one sequence: its channel at its own first step of the current block of steps.
+template <typename P> struct Walk {
+    P* at;
+    int64_t step;
+    template <int N> __device__ __forceinline__ void start(const Seq<P>& q, int t, int i, const Tile& w)
+    {
+        step = q.step;
+        at = q.data ? q.at(t + w.quad * Lay<N>::OWN, i) + w.channel : nullptr;
+    }
+    __device__ __forceinline__ void move(int steps) { at += steps * step; }
+    template <int OWN> __device__ __forceinline__ void load(int own, int count, float (&v)[OWN]) const
+    {
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) v[k] = own + k < count ? Elem<typename std::remove_const<P>::type>::up(at[k * step]) : 0.0f;
+    }
+};
+
+// b and c of a block of steps, [step][2 N] (b first): every lane brings LANES values of one step, 0 behind the end.
+template <typename E, int N> struct WalkShared {
+    const E* at;
+    int64_t step;
+    int row;
+    __device__ __forceinline__ void start(const ScanParams<E>& p, int t, int i, const Tile& w)
+    {
+        const int lane = (int)(threadIdx.x & (WAVE - 1)), piece = lane % 8;
+        row = lane / 8;
+        step = piece < 4 ? p.b.step : p.c.step;
+        at = (piece < 4 ? p.b.at(t + row, i) : p.c.at(t + row, i)) + w.group * N + (piece & 3) * Lay<N>::LANES;
+    }
+    __device__ __forceinline__ void move(int steps) { at += steps * step; }
+    __device__ __forceinline__ void load(int count, float (&v)[Lay<N>::LANES]) const
+    {
+        if (row < count) {
+            load_row<E, Lay<N>::LANES>(at, Lay<N>::LANES, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < Lay<N>::LANES; ++k) v[k] = 0.0f;
+        }
+    }
+};
+template <int N> __device__ __forceinline__ void stage_shared(float* lds, const float (&v)[Lay<N>::LANES])
+{
+    float* q = lds + (threadIdx.x & (WAVE - 1)) * Lay<N>::LANES;       // (step, piece) in a row
+#pragma unroll
+    for (int k = 0; k < Lay<N>::LANES; ++k) q[k] = v[k];
+}
+
+// LDS of one wavefront is written and then read by its lanes: in order for the hardware, and kept so for the compiler.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Sums of the values of eight steps over a channel's lanes; lane q is left with those of its steps q * OWN ..
+template <int LANES>
+__device__ __forceinline__ void fold_steps(float (&v)[BLOCK])
+{
+    const int lane = (int)(threadIdx.x & (WAVE - 1));
+    int half = BLOCK / 2;
+    if constexpr (LANES == 8) {
+        const bool up = lane & 4;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float a = v[k] + dpp<DPP_HALF_MIRROR>(v[k]), b = v[k + 4] + dpp<DPP_HALF_MIRROR>(v[k + 4]);
+            v[k] = up ? b : a;
+        }
+        half = 2;
+    }
+    if constexpr (LANES >= 4) {
+        const bool up = lane & 2;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k >= half) break;
+            const float a = v[k] + dpp<DPP_XOR2>(v[k]), b = v[k + half] + dpp<DPP_XOR2>(v[k + half]);
+            v[k] = up ? b : a;
+        }
+        half /= 2;
+    }
+    const bool up = lane & 1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (k >= half) break;
+        const float a = v[k] + dpp<DPP_XOR1>(v[k]), b = v[k + half] + dpp<DPP_XOR1>(v[k + half]);
+        v[k] = up ? b : a;
+    }
+}
 
 // ---- forward ------------------------------------------------------------------------------------------
-// One wavefront: the steps of one part of one tile of one environment.
-template <typename E, int N>
+// One wavefront: the steps of one part of one tile of one environment.  PART: only the part's effect on the
+// state.  The activations of the next block are under way while a block is computed.
+template <typename E, int N, bool PART>
 __global__ __launch_bounds__(SCAN_THREADS) void k_scan(const ScanParams<E> p)
 {
+    constexpr int LANES = Lay<N>::LANES, CHANNELS = Lay<N>::CHANNELS, OWN = Lay<N>::OWN;
+    __shared__ float4 shared_lds[SCAN_WAVES][BLOCK * N / 2];
+    __shared__ float2 step_lds[SCAN_WAVES][BLOCK * CHANNELS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + wave;
     if (item >= (int64_t)p.n * p.tiles) return;
     const int i = (int)(item / p.tiles);
-    const Tile w = tile_of(p, (int)(item % p.tiles));
+    const Tile w = tile_of<N>(p, (int)(item % p.tiles));
+    const int mine = (int)(threadIdx.x & (WAVE - 1)) / LANES;
     const int part = (int)blockIdx.y, t0 = part * p.part;
     const int t1 = p.steps - t0 < p.part ? p.steps : t0 + p.part;
     const int length = scan_length(p, i);
     const int end = t1 < length ? t1 : length;
-    float a2[N], h[N];
-    load_rates<N>(p.a, w.channel, a2);
+    float a2[4], h[4];
+    load_rates<N>(p.a, w, a2);
     const float skip = p.d ? p.d[w.channel] : 0.0f;
     const float bias = p.delta_bias ? p.delta_bias[w.channel] : 0.0f;
-    if (part > 0) load_tiled<N>(tiled_state<N>(p.starts, (int64_t)part * p.n + i, w, p.tiles), h);
-    else if (p.state_in) load_state<N>(p.state_in, (int64_t)i * p.channels + w.channel, h);
+    if (PART) zero(h);
+    else if (part > 0) load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), h);
+    else if (p.state_in) load4(state_of<N>(p.state_in, p.channels, i, w), h);
     else zero(h);
-    uint64_t starts = 0;
-    for (int t = t0; t < end; t += AHEAD) {
-        if (((t - t0) & (WAVE - 1)) == 0) starts = begins(p, t, end, i);
-        float x[AHEAD], delta[AHEAD], z[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int s = t + k < end ? t + k : end - 1;
-            x[k] = Elem<E>::up(p.x.at(s, i)[w.channel]);
-            delta[k] = Elem<E>::up(p.delta.at(s, i)[w.channel]);
-            if (p.z.data) z[k] = Elem<E>::up(p.z.at(s, i)[w.channel]);
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (t + k >= end) break;
-            if (p.saved && (t + k) % Save<N>::STEPS == 0)
-                store_tiled<N>(tiled_state<N>(p.saved, (int64_t)((t + k) / Save<N>::STEPS) * p.n + i, w, p.tiles), h);
-            Shared<E, N> b, c;
-            b.load(p.b.at(t + k, i) + w.group * N);
-            c.load(p.c.at(t + k, i) + w.group * N);
-            if (starts >> ((t + k - t0) & (WAVE - 1)) & 1u) zero(h);
-            float size = delta[k] + bias;
-            if (p.softplus) size = softplus(size);
-            const float u = size * x[k];
-            float y[4] = {skip * x[k], 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                h[n] = __builtin_fmaf(exp2_fast(size * a2[n]), h[n], u * b[n]);
-                y[n & 3] = __builtin_fmaf(h[n], c[n], y[n & 3]);
-            }
-            float out = (y[0] + y[1]) + (y[2] + y[3]);
-            if (p.z.data) out *= z[k] * sigmoid(z[k]);
-            if (w.owns) p.y.at(t + k, i)[w.channel] = Elem<E>::down(out);
-        }
-    }
-    if (w.owns) {
-        for (int t = t0 > end ? t0 : end; t < t1; ++t) p.y.at(t, i)[w.channel] = Elem<E>::down(0.0f);
-        if (p.state_out && p.parts == 1) store_state<N>(p.state_out, (int64_t)i * p.channels + w.channel, h);
-    }
-}
-
-// What a part does to the state: its end from zero, and how the state before it decays.
-template <typename E, int N>
-__global__ __launch_bounds__(SCAN_THREADS) void k_scan_part(const ScanParams<E> p)
-{
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + wave;
-    if (item >= (int64_t)p.n * p.tiles) return;
-    const int i = (int)(item / p.tiles);
-    const Tile w = tile_of(p, (int)(item % p.tiles));
-    const int part = (int)blockIdx.y, t0 = part * p.part;
-    const int t1 = p.steps - t0 < p.part ? p.steps : t0 + p.part;
-    const int length = scan_length(p, i);
-    const int end = t1 < length ? t1 : length;
-    float a2[N], h[N];
-    load_rates<N>(p.a, w.channel, a2);
-    const float bias = p.delta_bias ? p.delta_bias[w.channel] : 0.0f;
-    zero(h);
     float total = 0.0f, cut = 0.0f;
     uint64_t starts = 0;
-    for (int t = t0; t < end; t += AHEAD) {
+    const bool gate = !PART && p.z.data;
+    const int own = w.quad * OWN;
+    Walk<const E> at_x, at_delta, at_z;
+    Walk<E> at_y;
+    WalkShared<E, N> at_shared;
+    at_x.template start<N>(p.x, t0, i, w);
+    at_delta.template start<N>(p.delta, t0, i, w);
+    at_z.template start<N>(p.z, t0, i, w);
+    at_y.template start<N>(p.y, t0, i, w);
+    at_shared.start(p, t0, i, w);
+    float x[OWN], delta[OWN], z[OWN], shared[LANES];
+    auto fetch = [&](int count) {
+        at_shared.load(count, shared);
+        at_x.load(own, count, x);
+        at_delta.load(own, count, delta);
+        if (gate) at_z.load(own, count, z);
+        at_shared.move(BLOCK);
+        at_x.move(BLOCK);
+        at_delta.move(BLOCK);
+        at_z.move(BLOCK);
+    };
+    if (t0 < end) fetch(end - t0);
+    for (int t = t0; t < end; t += BLOCK) {
+        const int count = end - t < BLOCK ? end - t : BLOCK;
         if (((t - t0) & (WAVE - 1)) == 0) starts = begins(p, t, end, i);
-        float x[AHEAD], delta[AHEAD];
+        float x_now[OWN], z_now[OWN];
+        wave_fence();
+        stage_shared<N>(reinterpret_cast<float*>(shared_lds[wave]), shared);
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int s = t + k < end ? t + k : end - 1;
-            x[k] = Elem<E>::up(p.x.at(s, i)[w.channel]);
-            delta[k] = Elem<E>::up(p.delta.at(s, i)[w.channel]);
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (t + k >= end) break;
-            Shared<E, N> b;
-            b.load(p.b.at(t + k, i) + w.group * N);
-            if (starts >> ((t + k - t0) & (WAVE - 1)) & 1u) { zero(h); total = 0.0f; cut = 1.0f; }
+        for (int k = 0; k < OWN; ++k) {
+            x_now[k] = x[k];
+            z_now[k] = gate ? z[k] : 0.0f;
             float size = delta[k] + bias;
             if (p.softplus) size = softplus(size);
-            const float u = size * x[k];
-            total += size;
-#pragma unroll
-            for (int n = 0; n < N; ++n) h[n] = __builtin_fmaf(exp2_fast(size * a2[n]), h[n], u * b[n]);
+            // steps behind the end leave the state as it is
+            step_lds[wave][(own + k) * CHANNELS + mine] = own + k < count ? make_float2(size, size * x[k]) : make_float2(0.0f, 0.0f);
         }
+        wave_fence();
+        if (t + BLOCK < end) fetch(end - t - BLOCK);
+        if (!PART && p.saved) store4(tiled(p.saved, (int64_t)(t / BLOCK) * p.n + i, w, p.tiles), h);
+        float y[BLOCK];
+#pragma unroll
+        for (int k = 0; k < BLOCK; ++k) {
+            const float2 step = step_lds[wave][k * CHANNELS + mine];
+            float b[4], c[4];
+            load4(&shared_lds[wave][k * (N / 2) + w.quad], b);
+            if (!PART) load4(&shared_lds[wave][k * (N / 2) + N / 4 + w.quad], c);
+            if (starts >> ((t + k - t0) & (WAVE - 1)) & 1u) {
+                zero(h);
+                if (PART) { total = 0.0f; cut = 1.0f; }
+            }
+            if (PART) total += step.x;
+            float sum = 0.0f;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                h[m] = __builtin_fmaf(exp2_fast(step.x * a2[m]), h[m], step.y * b[m]);
+                if (!PART) sum = __builtin_fmaf(h[m], c[m], sum);
+            }
+            y[k] = sum;
+        }
+        if (PART) continue;
+        fold_steps<LANES>(y);
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) {
+            float out = __builtin_fmaf(skip, x_now[k], y[k]);
+            if (gate) out *= z_now[k] * sigmoid(z_now[k]);
+            if (w.owns && own + k < count) at_y.at[k * at_y.step] = Elem<E>::down(out);
+        }
+        at_y.move(BLOCK);
     }
-    const int64_t index = (int64_t)part * p.n + i;
-    store_tiled<N>(tiled_state<N>(p.starts, index, w, p.tiles), h);
-    p.decays[(index * p.tiles + w.tile) * WAVE + (threadIdx.x & (WAVE - 1))] = make_float2(total, cut);
+    if (PART) {
+        const int64_t index = (int64_t)part * p.n + i;
+        store4(tiled(p.starts, index, w, p.tiles), h);
+        if (w.quad == 0) p.decays[(index * p.tiles + w.tile) * CHANNELS + mine] = make_float2(total, cut);
+        return;
+    }
+    if (!w.owns) return;
+    for (int t = (t0 > end ? t0 : end) + w.quad; t < t1; t += LANES) p.y.at(t, i)[w.channel] = Elem<E>::down(0.0f);
+    if (p.state_out && p.parts == 1) store4(state_of<N>(p.state_out, p.channels, i, w), h);
 }
 
 // Carries the state through the parts: starts[part] turns from the part's own end into the state at its
-// start.  A thread takes four states of one channel.  Backward in time for the gradient of the state.
+// start.  Backward in time for the gradient of the state.
 template <typename E, int N, bool BACK>
 __global__ __launch_bounds__(SCAN_THREADS) void k_scan_carry(const ScanParams<E> p)
 {
-    constexpr int QUADS = N / 4;
-    const int64_t item = ((int64_t)blockIdx.x * SCAN_THREADS + threadIdx.x) / WAVE;     // (environment, tile, four states)
-    if (item >= (int64_t)p.n * p.tiles * QUADS) return;
-    const int quad = (int)(item % QUADS);
-    const int i = (int)(item / QUADS / p.tiles);
-    const Tile w = tile_of(p, (int)(item / QUADS % p.tiles));
-    const int lane = threadIdx.x & (WAVE - 1);
-    const float4 a = *reinterpret_cast<const float4*>(p.a + (int64_t)w.channel * N + quad * 4);
-    const float a2[4] = {a.x * LOG2E, a.y * LOG2E, a.z * LOG2E, a.w * LOG2E};
-    const int64_t own = ((int64_t)i * p.channels + w.channel) * N + quad * 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + wave;
+    if (item >= (int64_t)p.n * p.tiles) return;
+    const int i = (int)(item / p.tiles);
+    const Tile w = tile_of<N>(p, (int)(item % p.tiles));
+    const int mine = (int)(threadIdx.x & (WAVE - 1)) / Lay<N>::LANES;
+    float a2[4], h[4];
+    load_rates<N>(p.a, w, a2);
     const float* in = BACK ? p.dstate_out : p.state_in;
     float* out = BACK ? p.dstate_in : p.state_out;
-    float h[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (in) {
-        const float4 v = *reinterpret_cast<const float4*>(in + own);
-        h[0] = v.x; h[1] = v.y; h[2] = v.z; h[3] = v.w;
-    }
+    if (in) load4(state_of<N>(in, p.channels, i, w), h);
+    else zero(h);
     constexpr int GO = 8;
     for (int q0 = 0; q0 < p.parts; q0 += GO) {
-        float4 end[GO];
+        float end[GO][4];
         float2 decay[GO];
 #pragma unroll
         for (int k = 0; k < GO; ++k) {
             const int q = q0 + k < p.parts ? q0 + k : p.parts - 1;
-            const int64_t index = ((int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i) * p.tiles + w.tile;
-            end[k] = p.starts[(index * QUADS + quad) * WAVE + lane];
-            decay[k] = p.decays[index * WAVE + lane];
+            const int64_t index = (int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i;
+            load4(tiled(p.starts, index, w, p.tiles), end[k]);
+            decay[k] = p.decays[(index * p.tiles + w.tile) * Lay<N>::CHANNELS + mine];
         }
 #pragma unroll
         for (int k = 0; k < GO; ++k) {
             const int q = q0 + k;
             if (q >= p.parts) break;
-            const int64_t index = ((int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i) * p.tiles + w.tile;
-            p.starts[(index * QUADS + quad) * WAVE + lane] = make_float4(h[0], h[1], h[2], h[3]);
-            const float e[4] = {end[k].x, end[k].y, end[k].z, end[k].w};
+            const int64_t index = (int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i;
+            store4(tiled(p.starts, index, w, p.tiles), h);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) h[m] = decay[k].y != 0.0f ? e[m] : __builtin_fmaf(exp2_fast(decay[k].x * a2[m]), h[m], e[m]);
+            for (int m = 0; m < 4; ++m) h[m] = decay[k].y != 0.0f ? end[k][m] : __builtin_fmaf(exp2_fast(decay[k].x * a2[m]), h[m], end[k][m]);
         }
     }
-    if (out && w.owns) *reinterpret_cast<float4*>(out + own) = make_float4(h[0], h[1], h[2], h[3]);
+    if (out && w.owns) store4(state_of<N>(out, p.channels, i, w), h);
 }
 
 // ---- one token -------------------------------------------------------------------------------------------
@@ -396,10 +431,6 @@ static int scan_check(const craftax_scan_args* a, bool backward, const char** wh
     const craftax_view* all[] = {&a->x, &a->delta, &a->z, &a->b, &a->c};
     for (const craftax_view* v : all)
         if (!aligned(v->data, e)) return refuse(CRAFTAX_E_ALIGN, "an activation is not aligned to its elements", why);
-    const craftax_view* rows[] = {&a->b, &a->c};
-    for (const craftax_view* v : rows)
-        if (!aligned(v->data, 4) || (a->steps > 1 && v->step * (int64_t)e % 4 != 0) || (a->n > 1 && v->env * (int64_t)e % 4 != 0))
-            return refuse(CRAFTAX_E_ALIGN, "rows of b and c must be 4-byte aligned", why);
     if (!aligned(a->a, 16) || !aligned(a->state_in, 16) || !aligned(a->state_out, 16))
         return refuse(CRAFTAX_E_ALIGN, "a and the states must be 16-byte aligned", why);
     if (!aligned(a->d, 4) || !aligned(a->delta_bias, 4) || !aligned(a->lengths, 4))
@@ -430,7 +461,7 @@ static ScanTiles scan_tiles(const craftax_scan_args* a)
 {
     ScanTiles t;
     t.group_channels = a->channels / a->groups;
-    t.group_tiles = (int)ceil_div(t.group_channels, WAVE);
+    t.group_tiles = (int)ceil_div(t.group_channels, WAVE / (a->states / 4));
     t.tiles = t.group_tiles * a->groups;
     return t;
 }
@@ -452,8 +483,8 @@ static ScanParts scan_parts(const craftax_scan_args* a, int tiles, int64_t wavef
     return s;
 }
 
-constexpr int64_t SCAN_FILL = (int64_t)CHIP_SIMDS * 2;           // wavefronts: two per SIMD
-constexpr int64_t SCAN_BACK_FILL = (int64_t)CHIP_SIMDS * 2;
+constexpr int64_t SCAN_FILL = (int64_t)CHIP_SIMDS * 8;           // wavefronts that fill the chip
+constexpr int64_t SCAN_BACK_FILL = (int64_t)CHIP_SIMDS * 4;
 
 static bool scan_shape_ok(const craftax_scan_args* a)
 {
@@ -461,38 +492,41 @@ static bool scan_shape_ok(const craftax_scan_args* a)
            a->channels % a->groups == 0 && a->dtype <= CRAFTAX_F16;
 }
 
-static size_t state_bytes(const craftax_scan_args* a, int tiles) { return (size_t)a->n * tiles * WAVE * a->states * sizeof(float); }
+// the states of all environments, tiled
+static size_t tile_bytes(const craftax_scan_args* a, int tiles) { return (size_t)a->n * tiles * WAVE * sizeof(float4); }
 
 size_t scan_saved_bytes(const craftax_scan_args* a)
 {
     if (!scan_shape_ok(a)) return 0;
-    return (size_t)ceil_div(a->steps, 128 / a->states) * state_bytes(a, scan_tiles(a).tiles);
+    return (size_t)ceil_div(a->steps, BLOCK) * tile_bytes(a, scan_tiles(a).tiles);
 }
 
 // What lies where in a workspace.
-struct ScanSpace { ScanParts parts; size_t starts, decays, shared, weights, bytes; int rows, turns; };
+struct ScanSpace { ScanParts parts; size_t starts, decays, shared, weights, bytes; int rows, waves, group_blocks; };
 static ScanSpace scan_space(const craftax_scan_args* a, bool backward)
 {
-    const int tiles = scan_tiles(a).tiles;
+    const ScanTiles t = scan_tiles(a);
     ScanSpace s{};
-    s.parts = scan_parts(a, tiles, backward ? SCAN_BACK_FILL : SCAN_FILL);
+    s.parts = scan_parts(a, t.tiles, backward ? SCAN_BACK_FILL : SCAN_FILL);
     size_t at = 0;
     if (s.parts.parts > 1) {
         s.starts = at;
-        at += round256((size_t)s.parts.parts * state_bytes(a, tiles));
+        at += round256((size_t)s.parts.parts * tile_bytes(a, t.tiles));
         s.decays = at;
-        at += round256((size_t)s.parts.parts * a->n * tiles * WAVE * sizeof(float2));
+        at += round256((size_t)s.parts.parts * a->n * t.tiles * (WAVE / (a->states / 4)) * sizeof(float2));
     }
     if (backward) {
-        // a wavefront takes `turns` environments one after the other, so that no more rows of partial sums are written
-        // than fill the chip
-        const int64_t waves = (int64_t)a->n * tiles;
+        s.waves = 1;
+        while (s.waves < SCAN_BACK_WAVES && s.waves < t.group_tiles) s.waves *= 2;
+        s.group_blocks = (int)ceil_div(t.group_tiles, s.waves);
+        // a block takes several environments one after the other, so that no more rows of partial sums are written than
+        // fill the chip
+        const int64_t waves = (int64_t)a->n * a->groups * s.group_blocks * s.waves;
         int64_t turns = s.parts.parts > 1 ? 1 : waves / SCAN_BACK_FILL;
         if (turns < 1) turns = 1;
-        s.turns = (int)turns;
         s.rows = (int)ceil_div(a->n, turns) * s.parts.parts;
         s.shared = at;
-        at += round256((size_t)a->steps * a->n * tiles * 2 * a->states * sizeof(float));
+        at += round256((size_t)a->steps * a->n * a->groups * s.group_blocks * 2 * a->states * sizeof(float));
         s.weights = at;
         at += round256((size_t)s.rows * a->channels * (a->states + 2) * sizeof(float));
     }
@@ -558,15 +592,15 @@ int scan(const craftax_scan_args* a, void* stream, const char** why)
             const ScanSpace s = scan_space(a, false);
             char* base = static_cast<char*>(a->workspace);
             p.part = s.parts.part; p.parts = s.parts.parts;
-            const dim3 grid((unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES), (unsigned)p.parts);
+            const unsigned blocks = (unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES);
+            const dim3 grid(blocks, (unsigned)p.parts);
             if (p.parts > 1) {
                 p.starts = reinterpret_cast<float4*>(base + s.starts);
                 p.decays = reinterpret_cast<float2*>(base + s.decays);
-                const unsigned carry = (unsigned)ceil_div((int64_t)a->n * p.tiles * (N / 4), SCAN_WAVES);
-                hipLaunchKernelGGL((k_scan_part<E, N>), grid, dim3(SCAN_THREADS), 0, st, p);
-                hipLaunchKernelGGL((k_scan_carry<E, N, false>), dim3(carry), dim3(SCAN_THREADS), 0, st, p);
+                hipLaunchKernelGGL((k_scan<E, N, true>), grid, dim3(SCAN_THREADS), 0, st, p);
+                hipLaunchKernelGGL((k_scan_carry<E, N, false>), dim3(blocks), dim3(SCAN_THREADS), 0, st, p);
             }
-            hipLaunchKernelGGL((k_scan<E, N>), grid, dim3(SCAN_THREADS), 0, st, p);
+            hipLaunchKernelGGL((k_scan<E, N, false>), grid, dim3(SCAN_THREADS), 0, st, p);
         });
     });
     return launched(why);
@@ -582,22 +616,20 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
         using E = decltype(e);
         ScanParams<E> p = scan_params<E>(a);
         char* base = static_cast<char*>(a->workspace);
-        p.part = s.parts.part; p.parts = s.parts.parts; p.rows = s.rows;
+        p.part = s.parts.part; p.parts = s.parts.parts; p.rows = s.rows; p.waves = s.waves; p.group_blocks = s.group_blocks;
         p.starts = reinterpret_cast<float4*>(base + s.starts);
         p.decays = reinterpret_cast<float2*>(base + s.decays);
         p.shared_part = reinterpret_cast<float*>(base + s.shared);
         p.weight_part = reinterpret_cast<float*>(base + s.weights);
         with_states(a->states, [&](auto states) {
             constexpr int N = decltype(states)::value;
-            const dim3 parts_grid((unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES), (unsigned)p.parts);
             if (p.parts > 1) {
-                const unsigned carry = (unsigned)ceil_div((int64_t)a->n * p.tiles * (N / 4), SCAN_WAVES);
-                hipLaunchKernelGGL((k_scan_back_part<E, N>), parts_grid, dim3(SCAN_THREADS), 0, st, p);
-                hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3(carry), dim3(SCAN_THREADS), 0, st, p);
+                const unsigned blocks = (unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES);
+                hipLaunchKernelGGL((k_scan_back_part<E, N>), dim3(blocks, (unsigned)p.parts), dim3(SCAN_THREADS), 0, st, p);
+                hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3(blocks), dim3(SCAN_THREADS), 0, st, p);
             }
-            const int env_rows = s.rows / p.parts;
-            const dim3 grid((unsigned)ceil_div((int64_t)env_rows * p.tiles, SCAN_WAVES), (unsigned)p.parts);
-            hipLaunchKernelGGL((k_scan_back<E, N>), grid, dim3(SCAN_THREADS), 0, st, p);
+            const dim3 grid((unsigned)((int64_t)(s.rows / p.parts) * a->groups * s.group_blocks), (unsigned)p.parts);
+            hipLaunchKernelGGL((k_scan_back<E, N>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
             const int64_t values = (int64_t)a->steps * a->n * a->groups * 2 * N;
             hipLaunchKernelGGL((k_scan_shared<E, N>), dim3((unsigned)ceil_div(values, SCAN_THREADS)), dim3(SCAN_THREADS), 0, st, p,
                                seq<E>(a->db), seq<E>(a->dc));
