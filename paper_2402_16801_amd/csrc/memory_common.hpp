@@ -92,8 +92,22 @@ __device__ __forceinline__ float softplus(float v)
     return (v < 0.0f ? 0.0f : v) + q * r;
 }
 
-// v is computed here, not where it is used
+// v is computed, or has arrived from memory, here and not where it is used
 __device__ __forceinline__ void pin(float& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void pin(uint32_t& v) { asm volatile("" : "+v"(v)); }
+template <typename E> __device__ __forceinline__ void pin16(E& v)
+{
+    uint16_t bits = __builtin_bit_cast(uint16_t, v);
+    asm volatile("" : "+v"(bits));
+    v = __builtin_bit_cast(E, bits);
+}
+__device__ __forceinline__ void pin(__bf16& v) { pin16(v); }
+__device__ __forceinline__ void pin(_Float16& v) { pin16(v); }
+template <typename T, int N> __device__ __forceinline__ void pin(T (&v)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) pin(v[k]);
+}
 
 // ---- moves across lanes ----------------------------------------------------------------------------
 template <int CTRL> __device__ __forceinline__ float dpp(float v)

@@ -49,7 +49,7 @@ template <typename E> struct ScanParams {
     float* weight_part;    // backward: [rows][channels][N + 2] sums for da, dd and ddelta_bias
     int steps, n, channels, groups, group_channels, group_tiles, tiles, softplus;
     int part, parts;       // steps per part (whole blocks), number of parts
-    int rows, waves, group_blocks;   // backward: rows of weight_part, wavefronts per block, blocks per group
+    int rows, group_blocks;          // backward: rows of weight_part, blocks per group
 };
 
 // What a wavefront works on: some channels of one group (`tile`) of one environment.
@@ -81,15 +81,28 @@ __device__ __forceinline__ int scan_length(const ScanParams<E>& p, int i)
     return l < 0 ? 0 : (l > p.steps ? p.steps : l);
 }
 
-// begins of episodes among the steps t .. t + 63 below `end`, one bit each
-template <typename E>
-__device__ __forceinline__ uint64_t begins(const ScanParams<E>& p, int t, int end, int i)
-{
-    if (p.first.data == nullptr) return 0;
-    const int s = t + (int)(threadIdx.x & (WAVE - 1));
-    const bool on = s < end && *p.first.at(s < end ? s : end - 1, i) != 0;
-    return __ballot(on);
-}
+// Begins of episodes in a block of steps: lane l < 8 brings the flag of its step l.
+struct WalkFirst {
+    const uint8_t *at, *safe;
+    int64_t step;
+    uint32_t flag;
+    template <typename E> __device__ __forceinline__ void start(const ScanParams<E>& p, int t, int i)
+    {
+        step = p.first.step;
+        safe = p.first.data ? p.first.at(t, i) : nullptr;
+        at = safe + (int)(threadIdx.x & (BLOCK - 1)) * step;
+        step *= BLOCK;
+        flag = 0;
+    }
+    __device__ __forceinline__ void load(int count)
+    {
+        if (safe) flag = *((int)(threadIdx.x & (BLOCK - 1)) < count ? at : safe);
+    }
+    __device__ __forceinline__ uint32_t cuts(int count) const
+    {
+        return (uint32_t)__ballot((int)(threadIdx.x & (WAVE - 1)) < count && flag != 0);
+    }
+};
 
 // Four states of this lane in a workspace ([index][tile][lane]) and as the caller has them ([n][channels][N]).
 __device__ __forceinline__ float4* tiled(float4* base, int64_t index, const Tile& w, int tiles)
@@ -117,51 +130,49 @@ template <int N> __device__ __forceinline__ void load_rates(const float* a, cons
 }
 
 // Where a lane reads or writes one sequence: its channel at its own first step of the current block of steps.
-template <typename P> struct Walk {
-    P* at;
-    int64_t step;
-    template <int N> __device__ __forceinline__ void start(const Seq<P>& q, int t, int i, const Tile& w)
-    {
-        step = q.step;
-        at = q.data ? q.at(t + w.quad * Lay<N>::OWN, i) + w.channel : nullptr;
-    }
-    __device__ __forceinline__ void move(int steps) { at += steps * step; }
-    template <int OWN> __device__ __forceinline__ void load(int own, int count, float (&v)[OWN]) const
-    {
+template <typename P, int N> __device__ __forceinline__ P* walk_from(const Seq<P>& q, int t, int i, const Tile& w)
+{
+    return q.data ? q.at(t + w.quad * Lay<N>::OWN, i) + w.channel : nullptr;
+}
+// The lane's own steps as they lie in memory, any other valid step (`safe`) behind the end.  Nothing is converted or
+// tested here: the first use of a value waits for it, and that is to be a block of steps later.
+template <typename E, int OWN>
+__device__ __forceinline__ void load_own(const E* at, int64_t step, const E* safe, int own, int count, E (&v)[OWN])
+{
 #pragma unroll
-        for (int k = 0; k < OWN; ++k) v[k] = own + k < count ? Elem<typename std::remove_const<P>::type>::up(at[k * step]) : 0.0f;
-    }
-};
+    for (int k = 0; k < OWN; ++k) v[k] = *(own + k < count ? at + k * step : safe);
+}
 
-// b and c of a block of steps, [step][2 N] (b first): every lane brings LANES values of one step, 0 behind the end.
+// b and c of a block of steps, [step][2 N] (b first): every lane brings LANES values of one step.
 template <typename E, int N> struct WalkShared {
-    const E* at;
+    const E *at, *safe;
     int64_t step;
     int row;
+    uint32_t words[Lay<N>::LANES * sizeof(E) / 4];
     __device__ __forceinline__ void start(const ScanParams<E>& p, int t, int i, const Tile& w)
     {
         const int lane = (int)(threadIdx.x & (WAVE - 1)), piece = lane % 8;
         row = lane / 8;
         step = piece < 4 ? p.b.step : p.c.step;
-        at = (piece < 4 ? p.b.at(t + row, i) : p.c.at(t + row, i)) + w.group * N + (piece & 3) * Lay<N>::LANES;
+        safe = (piece < 4 ? p.b.at(t, i) : p.c.at(t, i)) + w.group * N + (piece & 3) * Lay<N>::LANES;
+        at = safe + row * step;
+        step *= BLOCK;
     }
-    __device__ __forceinline__ void move(int steps) { at += steps * step; }
-    __device__ __forceinline__ void load(int count, float (&v)[Lay<N>::LANES]) const
+    __device__ __forceinline__ void load(int count)
     {
-        if (row < count) {
-            load_row<E, Lay<N>::LANES>(at, Lay<N>::LANES, v);
-        } else {
+        const Pack<E, Lay<N>::LANES> v = *reinterpret_cast<const Pack<E, Lay<N>::LANES>*>(row < count ? at : safe);
+        __builtin_memcpy(words, &v, sizeof(v));
+    }
+    // 0 behind the end
+    __device__ __forceinline__ void stage(float4* lds, int count) const
+    {
+        Pack<E, Lay<N>::LANES> v;
+        __builtin_memcpy(&v, words, sizeof(v));
+        float* q = reinterpret_cast<float*>(lds) + (threadIdx.x & (WAVE - 1)) * Lay<N>::LANES;       // (step, piece) in a row
 #pragma unroll
-            for (int k = 0; k < Lay<N>::LANES; ++k) v[k] = 0.0f;
-        }
+        for (int k = 0; k < Lay<N>::LANES; ++k) q[k] = row < count ? Elem<E>::up(v.v[k]) : 0.0f;
     }
 };
-template <int N> __device__ __forceinline__ void stage_shared(float* lds, const float (&v)[Lay<N>::LANES])
-{
-    float* q = lds + (threadIdx.x & (WAVE - 1)) * Lay<N>::LANES;       // (step, piece) in a row
-#pragma unroll
-    for (int k = 0; k < Lay<N>::LANES; ++k) q[k] = v[k];
-}
 
 // LDS of one wavefront is written and then read by its lanes: in order for the hardware, and kept so for the compiler.
 __device__ __forceinline__ void wave_fence()
@@ -209,7 +220,7 @@ __device__ __forceinline__ void fold_steps(float (&v)[BLOCK])
 // One wavefront: the steps of one part of one tile of one environment.  PART: only the part's effect on the
 // state.  The activations of the next block are under way while a block is computed.
 template <typename E, int N, bool PART>
-__global__ __launch_bounds__(SCAN_THREADS) void k_scan(const ScanParams<E> p)
+__global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5))) void k_scan(const ScanParams<E> p)
 {
     constexpr int LANES = Lay<N>::LANES, CHANNELS = Lay<N>::CHANNELS, OWN = Lay<N>::OWN;
     __shared__ float4 shared_lds[SCAN_WAVES][BLOCK * N / 2];
@@ -233,76 +244,102 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan(const ScanParams<E> p)
     else if (p.state_in) load4(state_of<N>(p.state_in, p.channels, i, w), h);
     else zero(h);
     float total = 0.0f, cut = 0.0f;
-    uint64_t starts = 0;
     const bool gate = !PART && p.z.data;
     const int own = w.quad * OWN;
-    Walk<const E> at_x, at_delta, at_z;
-    Walk<E> at_y;
+    const E *at_x = walk_from<const E, N>(p.x, t0, i, w), *at_delta = walk_from<const E, N>(p.delta, t0, i, w);
+    const E* at_z = walk_from<const E, N>(p.z, t0, i, w);
+    E* at_y = walk_from<E, N>(p.y, t0, i, w);
     WalkShared<E, N> at_shared;
-    at_x.template start<N>(p.x, t0, i, w);
-    at_delta.template start<N>(p.delta, t0, i, w);
-    at_z.template start<N>(p.z, t0, i, w);
-    at_y.template start<N>(p.y, t0, i, w);
+    WalkFirst at_first;
     at_shared.start(p, t0, i, w);
-    float x[OWN], delta[OWN], z[OWN], shared[LANES];
+    at_first.start(p, t0, i);
+    const E *safe_x = at_x - own * p.x.step, *safe_delta = at_delta - own * p.delta.step, *safe_z = at_z - own * p.z.step;
+    E x[OWN], delta[OWN], z[OWN];
     auto fetch = [&](int count) {
-        at_shared.load(count, shared);
-        at_x.load(own, count, x);
-        at_delta.load(own, count, delta);
-        if (gate) at_z.load(own, count, z);
-        at_shared.move(BLOCK);
-        at_x.move(BLOCK);
-        at_delta.move(BLOCK);
-        at_z.move(BLOCK);
+        at_first.load(count);
+        at_shared.load(count);
+        load_own<E, OWN>(at_x, p.x.step, safe_x, own, count, x);
+        load_own<E, OWN>(at_delta, p.delta.step, safe_delta, own, count, delta);
+        if (gate) load_own<E, OWN>(at_z, p.z.step, safe_z, own, count, z);
+        at_first.at += at_first.step;
+        at_shared.at += at_shared.step;
+        at_x += BLOCK * p.x.step;
+        at_delta += BLOCK * p.delta.step;
+        at_z += BLOCK * p.z.step;
     };
     if (t0 < end) fetch(end - t0);
+    float4* at_saved = tiled(p.saved, (int64_t)(t0 / BLOCK) * p.n + i, w, p.tiles);
     for (int t = t0; t < end; t += BLOCK) {
         const int count = end - t < BLOCK ? end - t : BLOCK;
-        if (((t - t0) & (WAVE - 1)) == 0) starts = begins(p, t, end, i);
+        const bool whole = count == BLOCK;
+        const uint32_t cuts = at_first.cuts(count);
         float x_now[OWN], z_now[OWN];
         wave_fence();
-        stage_shared<N>(reinterpret_cast<float*>(shared_lds[wave]), shared);
+        at_shared.stage(shared_lds[wave], count);
 #pragma unroll
         for (int k = 0; k < OWN; ++k) {
-            x_now[k] = x[k];
-            z_now[k] = gate ? z[k] : 0.0f;
-            float size = delta[k] + bias;
+            x_now[k] = whole || own + k < count ? Elem<E>::up(x[k]) : 0.0f;
+            z_now[k] = gate ? Elem<E>::up(z[k]) : 0.0f;
+            float size = Elem<E>::up(delta[k]) + bias;
             if (p.softplus) size = softplus(size);
             // steps behind the end leave the state as it is
-            step_lds[wave][(own + k) * CHANNELS + mine] = own + k < count ? make_float2(size, size * x[k]) : make_float2(0.0f, 0.0f);
+            if (!whole && own + k >= count) size = 0.0f;
+            step_lds[wave][(own + k) * CHANNELS + mine] = make_float2(size, size * x_now[k]);
         }
         wave_fence();
-        if (t + BLOCK < end) fetch(end - t - BLOCK);
-        if (!PART && p.saved) store4(tiled(p.saved, (int64_t)(t / BLOCK) * p.n + i, w, p.tiles), h);
-        float y[BLOCK];
-#pragma unroll
-        for (int k = 0; k < BLOCK; ++k) {
-            const float2 step = step_lds[wave][k * CHANNELS + mine];
-            float b[4], c[4];
-            load4(&shared_lds[wave][k * (N / 2) + w.quad], b);
-            if (!PART) load4(&shared_lds[wave][k * (N / 2) + N / 4 + w.quad], c);
-            if (starts >> ((t + k - t0) & (WAVE - 1)) & 1u) {
-                zero(h);
-                if (PART) { total = 0.0f; cut = 1.0f; }
-            }
-            if (PART) total += step.x;
-            float sum = 0.0f;
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                h[m] = __builtin_fmaf(exp2_fast(step.x * a2[m]), h[m], step.y * b[m]);
-                if (!PART) sum = __builtin_fmaf(h[m], c[m], sum);
-            }
-            y[k] = sum;
+        if (!PART && p.saved) {
+            store4(at_saved, h);
+            at_saved += (int64_t)p.n * p.tiles * WAVE;
         }
+        if (t + BLOCK < end) fetch(end - t - BLOCK);
+        float y[BLOCK];
+        auto walk = [&](auto check) {
+#pragma unroll
+            for (int k = 0; k < BLOCK; ++k) {
+                const float2 step = step_lds[wave][k * CHANNELS + mine];
+                float b[4], c[4];
+                load4(&shared_lds[wave][k * (N / 2) + w.quad], b);
+                if (!PART) load4(&shared_lds[wave][k * (N / 2) + N / 4 + w.quad], c);
+                if (decltype(check)::value && (cuts >> k & 1u)) {
+                    zero(h);
+                    if (PART) { total = 0.0f; cut = 1.0f; }
+                }
+                if (PART) total += step.x;
+                float sum = 0.0f;
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    h[m] = __builtin_fmaf(exp2_fast(step.x * a2[m]), h[m], step.y * b[m]);
+                    if (!PART) sum = m == 0 ? h[m] * c[m] : __builtin_fmaf(h[m], c[m], sum);
+                }
+                y[k] = sum;
+                if (!PART) pin(y[k]);
+                if (k % 2 == 1) __builtin_amdgcn_sched_barrier(0);     // the operands of two steps at a time, not of eight, are in registers
+            }
+        };
+        // most blocks have no begin in them and run without a test per step
+        if (cuts == 0) walk(std::false_type{});
+        else walk(std::true_type{});
         if (PART) continue;
         fold_steps<LANES>(y);
 #pragma unroll
         for (int k = 0; k < OWN; ++k) {
             float out = __builtin_fmaf(skip, x_now[k], y[k]);
             if (gate) out *= z_now[k] * sigmoid(z_now[k]);
-            if (w.owns && own + k < count) at_y.at[k * at_y.step] = Elem<E>::down(out);
+            y[k] = out;
         }
-        at_y.move(BLOCK);
+        // the next block's values, under way since before this one's steps, are waited for here: behind the stores, the wait
+        // would be for those too
+        pin(at_first.flag);
+        pin(at_shared.words);
+        pin(x);
+        pin(delta);
+        if (gate) pin(z);
+        if (w.owns) {
+#pragma unroll
+            for (int k = 0; k < OWN; ++k)
+                if (whole || own + k < count) at_y[k * p.y.step] = Elem<E>::down(y[k]);
+        }
+        at_y += BLOCK * p.y.step;
     }
     if (PART) {
         const int64_t index = (int64_t)part * p.n + i;
@@ -616,7 +653,7 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
         using E = decltype(e);
         ScanParams<E> p = scan_params<E>(a);
         char* base = static_cast<char*>(a->workspace);
-        p.part = s.parts.part; p.parts = s.parts.parts; p.rows = s.rows; p.waves = s.waves; p.group_blocks = s.group_blocks;
+        p.part = s.parts.part; p.parts = s.parts.parts; p.rows = s.rows; p.group_blocks = s.group_blocks;
         p.starts = reinterpret_cast<float4*>(base + s.starts);
         p.decays = reinterpret_cast<float2*>(base + s.decays);
         p.shared_part = reinterpret_cast<float*>(base + s.shared);

@@ -44,190 +44,245 @@ template <int N> constexpr size_t scan_back_lds()
     return BLOCK * 2 * N * sizeof(float) + BLOCK * Lay<N>::CHANNELS * sizeof(float4) + 2 * BLOCK * 2 * N * sizeof(float);
 }
 
-template <typename E, int N>
-__global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_per_eu(2))) void k_scan_back(const ScanParams<E> p)
+// The arguments, read anew: strides and addresses that only the turn to another environment needs are not kept in scalar
+// registers, of which they would take more than there are.
+template <typename E> __device__ __forceinline__ const ScanParams<E>& arguments_again()
 {
-    constexpr int LANES = Lay<N>::LANES, CHANNELS = Lay<N>::CHANNELS, OWN = Lay<N>::OWN;
+    uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const ScanParams<E>*)(const __attribute__((address_space(4))) void*)at;
+}
+
+template <typename E, int N>
+__global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_per_eu(2))) void k_scan_back(const ScanParams<E> given)
+{
+    constexpr int LANES = Lay<N>::LANES, CHANNELS = Lay<N>::CHANNELS, OWN = Lay<N>::OWN, SUMS = BLOCK * 2 * N;
     extern __shared__ float4 lds[];
     const int lane = (int)(threadIdx.x & (WAVE - 1)), mine = lane / LANES;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), waves = (int)blockDim.x / WAVE;
     float4* shared_lds = lds + wave * (BLOCK * N / 2);                                   // [step][2 N] floats
-    float4* step_lds = lds + p.waves * (BLOCK * N / 2) + wave * (BLOCK * CHANNELS);      // [step][channel]: D, D x, dy, x
-    float* sum_lds = reinterpret_cast<float*>(lds + p.waves * (BLOCK * N / 2 + BLOCK * CHANNELS));   // [turn][wave][step][2 N]
-    const int group_block = (int)(blockIdx.x % (unsigned)(p.groups * p.group_blocks));
-    const int env_row = (int)(blockIdx.x / (unsigned)(p.groups * p.group_blocks)), env_rows = p.rows / p.parts;
-    const int group = group_block / p.group_blocks, in_group = (group_block % p.group_blocks) * p.waves + wave;
-    const bool works = in_group < p.group_tiles;          // the other wavefronts only keep the barriers
-    const Tile w = tile_of<N>(p, group * p.group_tiles + (works ? in_group : p.group_tiles - 1));
+    float4* step_lds = lds + waves * (BLOCK * N / 2) + wave * (BLOCK * CHANNELS);        // [step][channel]: D, D x, dy, x
+    float* sum_lds = reinterpret_cast<float*>(lds + waves * (BLOCK * N / 2 + BLOCK * CHANNELS));   // [turn][wave][step][2 N]
+    const int blocks = given.groups * given.group_blocks;
+    const int group_block = (int)(blockIdx.x % (unsigned)blocks);
+    const int env_row = (int)(blockIdx.x / (unsigned)blocks), env_rows = given.rows / given.parts;
+    const int group = group_block / given.group_blocks, in_group = (group_block % given.group_blocks) * waves + wave;
+    const bool works = in_group < given.group_tiles;          // the other wavefronts only keep the barriers
+    const Tile w = tile_of<N>(given, group * given.group_tiles + (works ? in_group : given.group_tiles - 1));
     const bool owns = works && w.owns;
-    const int part = (int)blockIdx.y, t0 = part * p.part;
-    const int t1 = p.steps - t0 < p.part ? p.steps : t0 + p.part;
+    const int part = (int)blockIdx.y;
     float a2[4], g[4], da[4], dd = 0.0f, dbias = 0.0f;
-    load_rates<N>(p.a, w, a2);
+    load_rates<N>(given.a, w, a2);
     zero(da);
-    const float skip = p.d ? p.d[w.channel] : 0.0f;
-    const float bias = p.delta_bias ? p.delta_bias[w.channel] : 0.0f;
+    const float skip = given.d ? given.d[w.channel] : 0.0f;
+    const float bias = given.delta_bias ? given.delta_bias[w.channel] : 0.0f;
     const int slot = fold_value(lane) / 4 * N + w.quad * 4 + fold_value(lane) % 4;       // among the 2 N sums of a step
     const int own = w.quad * OWN;
     int turn = 0;
-    for (int i = env_row; i < p.n; i += env_rows) {
+    for (int i = env_row; i < given.n; i += env_rows) {
+        const ScanParams<E>& p = arguments_again<E>();
+        const int t0 = part * p.part, t1 = p.steps - t0 < p.part ? p.steps : t0 + p.part;
         const int length = scan_length(p, i);
         const int end = t1 < length ? t1 : length;
         const int dead = t0 > end ? t0 : end;
+        const bool gate = p.z.data;
         if (owns)
             for (int t = dead + w.quad; t < t1; t += LANES) {
                 p.dx.at(t, i)[w.channel] = Elem<E>::down(0.0f);
                 p.ddelta.at(t, i)[w.channel] = Elem<E>::down(0.0f);
-                if (p.z.data) p.dz.at(t, i)[w.channel] = Elem<E>::down(0.0f);
+                if (gate) p.dz.at(t, i)[w.channel] = Elem<E>::down(0.0f);
             }
-        for (int q = (int)threadIdx.x; q < (t1 - dead) * 2 * N; q += p.waves * WAVE)
-            p.shared_part[(((int64_t)(dead + q / (2 * N)) * p.n + i) * (p.groups * p.group_blocks) + group_block) * (2 * N) + q % (2 * N)] = 0.0f;
+        const int64_t sum_step = (int64_t)p.n * blocks * (2 * N);          // from one step's sums to the next one's
+        float* at_sums = p.shared_part + ((int64_t)i * blocks + group_block) * (2 * N);
+        for (int q = (int)threadIdx.x; q < (t1 - dead) * 2 * N; q += (int)blockDim.x)
+            at_sums[(dead + q / (2 * N)) * sum_step + q % (2 * N)] = 0.0f;
         if (p.parts > 1) load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), g);
         else if (p.dstate_out) load4(state_of<N>(p.dstate_out, p.channels, i, w), g);
         else zero(g);
-        int t = t0 + (end - t0 - 1) / BLOCK * BLOCK;       // the last block of steps
-        Walk<const E> at_x, at_delta, at_dy, at_z;
-        Walk<E> at_dx, at_ddelta, at_dz;
-        WalkShared<E, N> at_shared;
-        at_x.template start<N>(p.x, t, i, w);
-        at_delta.template start<N>(p.delta, t, i, w);
-        at_dy.template start<N>(p.dy, t, i, w);
-        at_z.template start<N>(p.z, t, i, w);
-        at_dx.template start<N>(p.dx, t, i, w);
-        at_ddelta.template start<N>(p.ddelta, t, i, w);
-        at_dz.template start<N>(p.dz, t, i, w);
-        at_shared.start(p, t, i, w);
-        const float4* at_saved = tiled(p.saved, (int64_t)(t / BLOCK) * p.n + i, w, p.tiles);
-        float next_x[OWN], next_delta[OWN], next_dy[OWN], next_z[OWN], shared[LANES], next_h[4];
-        auto fetch = [&](int count) {
-            at_shared.load(count, shared);
-            at_x.load(own, count, next_x);
-            at_delta.load(own, count, next_delta);
-            at_dy.load(own, count, next_dy);
-            if (p.z.data) at_z.load(own, count, next_z);
-            load4(at_saved, next_h);
-            at_shared.move(-BLOCK);
-            at_x.move(-BLOCK);
-            at_delta.move(-BLOCK);
-            at_dy.move(-BLOCK);
-            at_z.move(-BLOCK);
-            at_saved -= (int64_t)p.n * p.tiles * WAVE;
-        };
-        if (t0 < end) fetch(end - t);
-        for (; t0 < end && t >= t0; t -= BLOCK) {
-            const int count = end - t < BLOCK ? end - t : BLOCK;
-            const uint32_t starts = (uint32_t)begins(p, t, t + count, i);
-            float slope[OWN], dz[OWN], h[4];
-            wave_fence();
-            stage_shared<N>(reinterpret_cast<float*>(shared_lds), shared);
-#pragma unroll
-            for (int k = 0; k < OWN; ++k) {
-                const float pre = next_delta[k] + bias;
-                const float size = p.softplus ? softplus(pre) : pre;
-                slope[k] = p.softplus ? sigmoid(pre) : 1.0f;
-                float dout = next_dy[k];
-                if (p.z.data) {
-                    const float s = sigmoid(next_z[k]);
-                    dz[k] = dout * (s * __builtin_fmaf(next_z[k], 1.0f - s, 1.0f));
-                    dout *= next_z[k] * s;
-                }
-                // steps behind the end and channels that are none add nothing
-                step_lds[(own + k) * CHANNELS + mine] = owns && own + k < count ? make_float4(size, size * next_x[k], dout, next_x[k])
-                                                                               : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            }
-#pragma unroll
-            for (int m = 0; m < 4; ++m) h[m] = next_h[m];
-            wave_fence();
-            if (t > t0) fetch(BLOCK);
-            // the states of these steps again: the decays, and what decayed of the state before
-            float decay[BLOCK][4], kept[BLOCK][4], y[BLOCK];
-#pragma unroll
-            for (int k = 0; k < BLOCK; ++k) {
-                const float4 step = step_lds[k * CHANNELS + mine];
-                float b[4];
-                load4(&shared_lds[k * (N / 2) + w.quad], b);
-                if (starts >> k & 1u) zero(h);
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    decay[k][m] = exp2_fast(step.x * a2[m]);
-                    kept[k][m] = decay[k][m] * h[m];
-                    h[m] = __builtin_fmaf(step.y, b[m], kept[k][m]);
-                }
-                if (p.z.data) {
-                    float c[4];
-                    load4(&shared_lds[k * (N / 2) + N / 4 + w.quad], c);
-                    y[k] = h[0] * c[0];
-#pragma unroll
-                    for (int m = 1; m < 4; ++m) y[k] = __builtin_fmaf(h[m], c[m], y[k]);
-                }
-                if (p.z.data) pin(y[k]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (p.z.data) {
-                fold_steps<LANES>(y);
+        if (t0 < end) {
+            int t = t0 + (end - t0 - 1) / BLOCK * BLOCK;       // the last block of steps
+            const E *at_x = walk_from<const E, N>(p.x, t, i, w), *at_delta = walk_from<const E, N>(p.delta, t, i, w);
+            const E *at_dy = walk_from<const E, N>(p.dy, t, i, w), *at_z = walk_from<const E, N>(p.z, t, i, w);
+            E *at_dx = walk_from<E, N>(p.dx, t, i, w), *at_ddelta = walk_from<E, N>(p.ddelta, t, i, w), *at_dz = walk_from<E, N>(p.dz, t, i, w);
+            WalkShared<E, N> at_shared;
+            at_shared.start(p, t, i, w);
+            const float4* at_saved = tiled(p.saved, (int64_t)(t / BLOCK) * p.n + i, w, p.tiles);
+            const int64_t saved_step = (int64_t)p.n * p.tiles * WAVE;
+            const int64_t step_x = p.x.step, step_delta = p.delta.step, step_dy = p.dy.step, step_z = p.z.step;
+            const int64_t step_dx = p.dx.step, step_ddelta = p.ddelta.step, step_dz = p.dz.step;
+            const bool soft = p.softplus != 0;
+            WalkFirst at_first;
+            at_first.start(p, t, i);
+            at_sums += t * sum_step;
+            const E *safe_x = p.x.at(t0, i) + w.channel, *safe_delta = p.delta.at(t0, i) + w.channel, *safe_dy = p.dy.at(t0, i) + w.channel;
+            const E* safe_z = gate ? p.z.at(t0, i) + w.channel : nullptr;
+            E next_x[OWN], next_delta[OWN], next_dy[OWN], next_z[OWN];
+            float next_h[4];
+            auto fetch = [&](int count) {
+                at_first.load(count);
+                at_shared.load(count);
+                load_own<E, OWN>(at_x, step_x, safe_x, own, count, next_x);
+                load_own<E, OWN>(at_delta, step_delta, safe_delta, own, count, next_delta);
+                load_own<E, OWN>(at_dy, step_dy, safe_dy, own, count, next_dy);
+                if (gate) load_own<E, OWN>(at_z, step_z, safe_z, own, count, next_z);
+                load4(at_saved, next_h);
+                at_first.at -= at_first.step;
+                at_shared.at -= at_shared.step;
+                at_x -= BLOCK * step_x;
+                at_delta -= BLOCK * step_delta;
+                at_dy -= BLOCK * step_dy;
+                at_z -= BLOCK * step_z;
+                at_saved -= saved_step;
+            };
+            fetch(end - t);
+            for (; t >= t0; t -= BLOCK) {
+                const int count = end - t < BLOCK ? end - t : BLOCK;
+                const bool whole = count == BLOCK;
+                const uint32_t cuts = at_first.cuts(count);
+                float slope[OWN], dz[OWN], h[4];
+                wave_fence();
+                at_shared.stage(shared_lds, count);
 #pragma unroll
                 for (int k = 0; k < OWN; ++k) {
-                    const float x = step_lds[(own + k) * CHANNELS + mine].w;
-                    if (owns && own + k < count) at_dz.at[k * at_dz.step] = Elem<E>::down(dz[k] * __builtin_fmaf(skip, x, y[k]));
+                    const float pre = Elem<E>::up(next_delta[k]) + bias;
+                    float size = soft ? softplus(pre) : pre;
+                    slope[k] = soft ? sigmoid(pre) : 1.0f;
+                    float dout = Elem<E>::up(next_dy[k]), x = Elem<E>::up(next_x[k]);
+                    if (gate) {
+                        const float z = Elem<E>::up(next_z[k]), s = sigmoid(z);
+                        dz[k] = dout * (s * __builtin_fmaf(z, 1.0f - s, 1.0f));
+                        dout *= z * s;
+                    }
+                    // steps behind the end and channels that are none add nothing
+                    if (!owns || (!whole && own + k >= count)) size = dout = x = 0.0f;
+                    step_lds[(own + k) * CHANNELS + mine] = make_float4(size, size * x, dout, x);
                 }
-            }
-            wave_fence();       // what is in LDS is read again rather than kept in registers: 64 more of them
-            float gb[BLOCK], rate[BLOCK];
-            float* sums = sum_lds + (turn * p.waves + wave) * (BLOCK * 2 * N);
 #pragma unroll
-            for (int k = BLOCK - 1; k >= 0; --k) {
-                const float4 step = step_lds[k * CHANNELS + mine];
-                float b[4], c[4], v[8];
-                load4(&shared_lds[k * (N / 2) + w.quad], b);
-                load4(&shared_lds[k * (N / 2) + N / 4 + w.quad], c);
-                gb[k] = rate[k] = 0.0f;
+                for (int m = 0; m < 4; ++m) h[m] = next_h[m];
+                wave_fence();
+                if (t > t0) fetch(BLOCK);
+                // the states of these steps again: the decays, and what decayed of the state before
+                float decay[BLOCK][4], kept[BLOCK][4], y[BLOCK];
+                auto states = [&](auto check) {
+                    float4 step = step_lds[mine];
+                    float b[4], c[4];
+                    load4(&shared_lds[w.quad], b);
+                    if (gate) load4(&shared_lds[N / 4 + w.quad], c);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    v[4 + m] = step.z * __builtin_fmaf(step.y, b[m], kept[k][m]);
-                    const float gm = __builtin_fmaf(c[m], step.z, g[m]);
-                    v[m] = gm * step.y;
-                    gb[k] = __builtin_fmaf(gm, b[m], gb[k]);
-                    const float through = gm * kept[k][m];
-                    rate[k] = __builtin_fmaf(through, a2[m], rate[k]);
-                    da[m] = __builtin_fmaf(through, step.x, da[m]);
-                    g[m] = decay[k][m] * gm;
+                    for (int k = 0; k < BLOCK; ++k) {
+                        float4 next_step = step;
+                        float next_b[4] = {}, next_c[4] = {};
+                        if (k + 1 < BLOCK) {
+                            next_step = step_lds[(k + 1) * CHANNELS + mine];
+                            load4(&shared_lds[(k + 1) * (N / 2) + w.quad], next_b);
+                            if (gate) load4(&shared_lds[(k + 1) * (N / 2) + N / 4 + w.quad], next_c);
+                        }
+                        if (decltype(check)::value && (cuts >> k & 1u)) zero(h);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+                            decay[k][m] = exp2_fast(step.x * a2[m]);
+                            kept[k][m] = decay[k][m] * h[m];
+                            h[m] = __builtin_fmaf(step.y, b[m], kept[k][m]);
+                        }
+                        if (gate) {
+                            y[k] = h[0] * c[0];
+#pragma unroll
+                            for (int m = 1; m < 4; ++m) y[k] = __builtin_fmaf(h[m], c[m], y[k]);
+                            pin(y[k]);
+                        }
+                        step = next_step;
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) { b[m] = next_b[m]; c[m] = next_c[m]; }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                if (cuts == 0) states(std::false_type{});
+                else states(std::true_type{});
+                wave_fence();       // what is in LDS is read again rather than kept in registers: 64 more of them
+                if (gate) {
+                    fold_steps<LANES>(y);
+#pragma unroll
+                    for (int k = 0; k < OWN; ++k) {
+                        const float x = step_lds[(own + k) * CHANNELS + mine].w;
+                        if (owns && (whole || own + k < count)) at_dz[k * step_dz] = Elem<E>::down(dz[k] * __builtin_fmaf(skip, x, y[k]));
+                    }
                 }
-                if (starts >> k & 1u) zero(g);
-                const float folded = fold_channels<LANES>(v);
-                if (fold_writes<LANES>(lane)) sums[k * 2 * N + slot] = works ? folded : 0.0f;
-                // all of a step is done in its turn: put off to the end, the sums would keep every step's factors in registers
-                pin(gb[k]);
-                pin(rate[k]);
+                float gb[BLOCK], rate[BLOCK];
+                float* sums = sum_lds + (turn * waves + wave) * SUMS;
+                auto back = [&](auto check) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m) pin(da[m]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            wave_fence();
-            fold_steps<LANES>(gb);
-            fold_steps<LANES>(rate);
+                    for (int k = BLOCK - 1; k >= 0; --k) {
+                        const float4 step = step_lds[k * CHANNELS + mine];
+                        float b[4], c[4], v[8];
+                        load4(&shared_lds[k * (N / 2) + w.quad], b);
+                        load4(&shared_lds[k * (N / 2) + N / 4 + w.quad], c);
 #pragma unroll
-            for (int k = 0; k < OWN; ++k) {
-                const float4 step = step_lds[(own + k) * CHANNELS + mine];
-                const float dsize = slope[k] * __builtin_fmaf(gb[k], step.w, rate[k] * (1.0f / LOG2E));
-                if (owns && own + k < count) {
+                        for (int m = 0; m < 4; ++m) {
+                            v[4 + m] = step.z * __builtin_fmaf(step.y, b[m], kept[k][m]);
+                            const float gm = __builtin_fmaf(c[m], step.z, g[m]);
+                            v[m] = gm * step.y;
+                            gb[k] = m == 0 ? gm * b[m] : __builtin_fmaf(gm, b[m], gb[k]);
+                            const float through = gm * kept[k][m];
+                            rate[k] = m == 0 ? through * a2[m] : __builtin_fmaf(through, a2[m], rate[k]);
+                            da[m] = __builtin_fmaf(through, step.x, da[m]);
+                            g[m] = decay[k][m] * gm;
+                        }
+                        if (decltype(check)::value && (cuts >> k & 1u)) zero(g);
+                        const float folded = fold_channels<LANES>(v);
+                        if (fold_writes<LANES>(lane)) sums[k * 2 * N + slot] = folded;
+                        // all of a step is done in its turn: put off to the end, the sums would keep every step's factors in registers
+                        pin(gb[k]);
+                        pin(rate[k]);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) pin(da[m]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                if (cuts == 0) back(std::false_type{});
+                else back(std::true_type{});
+                wave_fence();
+                fold_steps<LANES>(gb);
+                fold_steps<LANES>(rate);
+                float dx[OWN], dsize[OWN];
+#pragma unroll
+                for (int k = 0; k < OWN; ++k) {
+                    const float4 step = step_lds[(own + k) * CHANNELS + mine];
+                    dsize[k] = slope[k] * __builtin_fmaf(gb[k], step.w, rate[k] * (1.0f / LOG2E));
+                    dx[k] = __builtin_fmaf(gb[k], step.x, skip * step.z);
                     dd = __builtin_fmaf(step.z, step.w, dd);
-                    dbias += dsize;
-                    at_dx.at[k * at_dx.step] = Elem<E>::down(__builtin_fmaf(gb[k], step.x, skip * step.z));
-                    at_ddelta.at[k * at_ddelta.step] = Elem<E>::down(dsize);
+                    if (whole || own + k < count) dbias += dsize[k];
                 }
+                // the next block's values have been under way since before this one's steps; behind the stores, the wait would be for
+                // those too
+                pin(at_first.flag);
+                pin(at_shared.words);
+                pin(next_x);
+                pin(next_delta);
+                pin(next_dy);
+                if (gate) pin(next_z);
+                pin(next_h);
+                if (owns) {
+#pragma unroll
+                    for (int k = 0; k < OWN; ++k)
+                        if (whole || own + k < count) {
+                            at_dx[k * step_dx] = Elem<E>::down(dx[k]);
+                            at_ddelta[k * step_ddelta] = Elem<E>::down(dsize[k]);
+                        }
+                }
+                at_dx -= BLOCK * step_dx;
+                at_ddelta -= BLOCK * step_ddelta;
+                at_dz -= BLOCK * step_dz;
+                __syncthreads();
+                // sums over the block's wavefronts; the next turn writes the other half, so one barrier is enough
+                const float* from = sum_lds + turn * waves * SUMS;
+                for (int q = (int)threadIdx.x; q < count * 2 * N; q += (int)blockDim.x) {
+                    float s = from[q];
+                    for (int v = 1; v < waves; ++v) s += from[v * SUMS + q];
+                    at_sums[(q / (2 * N)) * sum_step + q % (2 * N)] = s;
+                }
+                at_sums -= BLOCK * sum_step;
+                turn ^= 1;
             }
-            at_dx.move(-BLOCK);
-            at_ddelta.move(-BLOCK);
-            at_dz.move(-BLOCK);
-            __syncthreads();
-            // sums over the block's wavefronts; the next turn writes the other half, so one barrier is enough
-            const float* from = sum_lds + turn * p.waves * (BLOCK * 2 * N);
-            for (int q = (int)threadIdx.x; q < count * 2 * N; q += p.waves * WAVE) {
-                float s = from[q];
-                for (int v = 1; v < p.waves; ++v) s += from[v * (BLOCK * 2 * N) + q];
-                p.shared_part[(((int64_t)(t + q / (2 * N)) * p.n + i) * (p.groups * p.group_blocks) + group_block) * (2 * N) + q % (2 * N)] = s;
-            }
-            turn ^= 1;
         }
         if (p.parts == 1 && p.dstate_in && owns) store4(state_of<N>(p.dstate_in, p.channels, i, w), g);
     }
@@ -237,7 +292,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
     if constexpr (LANES >= 4) { dd += dpp<DPP_XOR2>(dd); dbias += dpp<DPP_XOR2>(dbias); }
     if constexpr (LANES >= 8) { dd += dpp<DPP_HALF_MIRROR>(dd); dbias += dpp<DPP_HALF_MIRROR>(dbias); }
     if (owns) {
-        float* row = p.weight_part + ((int64_t)(part * env_rows + env_row) * p.channels + w.channel) * (N + 2);
+        float* row = given.weight_part + ((int64_t)(part * env_rows + env_row) * given.channels + w.channel) * (N + 2);
 #pragma unroll
         for (int m = 0; m < 4; ++m) row[w.quad * 4 + m] = da[m];
         if (w.quad == 0) { row[N] = dd; row[N + 1] = dbias; }
@@ -268,34 +323,39 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
     float total = 0.0f, cut = 0.0f;
     const int own = w.quad * OWN;
     int t = t0 + (end - t0 - 1) / BLOCK * BLOCK;
-    Walk<const E> at_delta, at_dy, at_z;
+    const E *at_delta = walk_from<const E, N>(p.delta, t, i, w), *at_dy = walk_from<const E, N>(p.dy, t, i, w), *at_z = walk_from<const E, N>(p.z, t, i, w);
+    const E *safe_delta = p.delta.at(t0, i) + w.channel, *safe_dy = p.dy.at(t0, i) + w.channel, *safe_z = p.z.data ? p.z.at(t0, i) + w.channel : nullptr;
     WalkShared<E, N> at_shared;
-    at_delta.template start<N>(p.delta, t, i, w);
-    at_dy.template start<N>(p.dy, t, i, w);
-    at_z.template start<N>(p.z, t, i, w);
+    WalkFirst at_first;
     at_shared.start(p, t, i, w);
+    at_first.start(p, t, i);
     for (; t0 < end && t >= t0; t -= BLOCK) {
         const int count = end - t < BLOCK ? end - t : BLOCK;
-        const uint32_t starts = (uint32_t)begins(p, t, t + count, i);
-        float shared[LANES], delta[OWN], dy[OWN], z[OWN];
-        at_shared.load(count, shared);
-        at_delta.load(own, count, delta);
-        at_dy.load(own, count, dy);
-        if (p.z.data) at_z.load(own, count, z);
-        at_shared.move(-BLOCK);
-        at_delta.move(-BLOCK);
-        at_dy.move(-BLOCK);
-        at_z.move(-BLOCK);
+        E delta[OWN], dy[OWN], z[OWN];
+        at_first.load(count);
+        at_shared.load(count);
+        load_own<E, OWN>(at_delta, p.delta.step, safe_delta, own, count, delta);
+        load_own<E, OWN>(at_dy, p.dy.step, safe_dy, own, count, dy);
+        if (p.z.data) load_own<E, OWN>(at_z, p.z.step, safe_z, own, count, z);
+        const uint32_t cuts = at_first.cuts(count);
+        at_first.at -= at_first.step;
+        at_shared.at -= at_shared.step;
+        at_delta -= BLOCK * p.delta.step;
+        at_dy -= BLOCK * p.dy.step;
+        at_z -= BLOCK * p.z.step;
         float2 step[OWN];
 #pragma unroll
         for (int k = 0; k < OWN; ++k) {
-            float size = delta[k] + bias;
+            float size = Elem<E>::up(delta[k]) + bias, dout = Elem<E>::up(dy[k]);
             if (p.softplus) size = softplus(size);
-            if (p.z.data) dy[k] *= z[k] * sigmoid(z[k]);
-            step[k] = own + k < count ? make_float2(size, dy[k]) : make_float2(0.0f, 0.0f);
+            if (p.z.data) {
+                const float v = Elem<E>::up(z[k]);
+                dout *= v * sigmoid(v);
+            }
+            step[k] = own + k < count ? make_float2(size, dout) : make_float2(0.0f, 0.0f);
         }
         wave_fence();
-        stage_shared<N>(reinterpret_cast<float*>(shared_lds[wave]), shared);
+        at_shared.stage(shared_lds[wave], count);
 #pragma unroll
         for (int k = 0; k < OWN; ++k) step_lds[wave][(own + k) * CHANNELS + mine] = step[k];
         wave_fence();
@@ -307,7 +367,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
             total += s.x;
 #pragma unroll
             for (int m = 0; m < 4; ++m) g[m] = exp2_fast(s.x * a2[m]) * __builtin_fmaf(c[m], s.y, g[m]);
-            if (starts >> k & 1u) { zero(g); total = 0.0f; cut = 1.0f; }
+            if (cuts >> k & 1u) { zero(g); total = 0.0f; cut = 1.0f; }
         }
     }
     const int64_t index = (int64_t)part * p.n + i;
