@@ -81,22 +81,25 @@ __device__ __forceinline__ int scan_length(const ScanParams<E>& p, int i)
     return l < 0 ? 0 : (l > p.steps ? p.steps : l);
 }
 
-// Begins of episodes in a block of steps: lane l < 8 brings the flag of its step l.
+// Begins of episodes in a block of steps: lane l brings the flag of step l % 8.
 struct WalkFirst {
-    const uint8_t *at, *safe;
+    const uint8_t* at;
     int64_t step;
     uint32_t flag;
     template <typename E> __device__ __forceinline__ void start(const ScanParams<E>& p, int t, int i)
     {
         step = p.first.step;
-        safe = p.first.data ? p.first.at(t, i) : nullptr;
-        at = safe + (int)(threadIdx.x & (BLOCK - 1)) * step;
-        step *= BLOCK;
+        at = p.first.data ? p.first.at(t, i) + (int)(threadIdx.x & (BLOCK - 1)) * step : nullptr;
         flag = 0;
     }
-    __device__ __forceinline__ void load(int count)
+    __device__ __forceinline__ void move(int blocks) { at += blocks * BLOCK * step; }
+    __device__ __forceinline__ void load(bool any, int count)
     {
-        if (safe) flag = *((int)(threadIdx.x & (BLOCK - 1)) < count ? at : safe);
+        if (!any) return;
+        const int row = (int)(threadIdx.x & (BLOCK - 1));
+        const uint8_t* q = at;
+        if (count < BLOCK && row >= count) q -= row * step;
+        flag = *q;
     }
     __device__ __forceinline__ uint32_t cuts(int count) const
     {
@@ -134,43 +137,54 @@ template <typename P, int N> __device__ __forceinline__ P* walk_from(const Seq<P
 {
     return q.data ? q.at(t + w.quad * Lay<N>::OWN, i) + w.channel : nullptr;
 }
-// The lane's own steps as they lie in memory, any other valid step (`safe`) behind the end.  Nothing is converted or
-// tested here: the first use of a value waits for it, and that is to be a block of steps later.
+// The lane's own steps as they lie in memory, the block's first step behind the end.  Nothing is converted or tested
+// here: the first use of a value waits for it, and that is to be a block of steps later.
 template <typename E, int OWN>
-__device__ __forceinline__ void load_own(const E* at, int64_t step, const E* safe, int own, int count, E (&v)[OWN])
+__device__ __forceinline__ void load_own(const E* at, int64_t step, int own, int count, E (&v)[OWN])
 {
+    if (count >= BLOCK) {
 #pragma unroll
-    for (int k = 0; k < OWN; ++k) v[k] = *(own + k < count ? at + k * step : safe);
+        for (int k = 0; k < OWN; ++k) v[k] = at[k * step];
+    } else {
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) v[k] = at[(own + k < count ? k : -own) * step];
+    }
 }
 
 // b and c of a block of steps, [step][2 N] (b first): every lane brings LANES values of one step.
 template <typename E, int N> struct WalkShared {
-    const E *at, *safe;
+    const E* at;
     int64_t step;
-    int row;
     uint32_t words[Lay<N>::LANES * sizeof(E) / 4];
     __device__ __forceinline__ void start(const ScanParams<E>& p, int t, int i, const Tile& w)
     {
         const int lane = (int)(threadIdx.x & (WAVE - 1)), piece = lane % 8;
-        row = lane / 8;
         step = piece < 4 ? p.b.step : p.c.step;
-        safe = (piece < 4 ? p.b.at(t, i) : p.c.at(t, i)) + w.group * N + (piece & 3) * Lay<N>::LANES;
-        at = safe + row * step;
-        step *= BLOCK;
+        at = (piece < 4 ? p.b.at(t, i) : p.c.at(t, i)) + w.group * N + (piece & 3) * Lay<N>::LANES + lane / 8 * step;
     }
+    __device__ __forceinline__ void move(int blocks) { at += blocks * BLOCK * step; }
     __device__ __forceinline__ void load(int count)
     {
-        const Pack<E, Lay<N>::LANES> v = *reinterpret_cast<const Pack<E, Lay<N>::LANES>*>(row < count ? at : safe);
+        const int row = (int)(threadIdx.x & (WAVE - 1)) / 8;
+        const E* q = at;
+        if (count < BLOCK && row >= count) q -= row * step;
+        const Pack<E, Lay<N>::LANES> v = *reinterpret_cast<const Pack<E, Lay<N>::LANES>*>(q);
         __builtin_memcpy(words, &v, sizeof(v));
     }
     // 0 behind the end
     __device__ __forceinline__ void stage(float4* lds, int count) const
     {
+        const int row = (int)(threadIdx.x & (WAVE - 1)) / 8;
         Pack<E, Lay<N>::LANES> v;
         __builtin_memcpy(&v, words, sizeof(v));
         float* q = reinterpret_cast<float*>(lds) + (threadIdx.x & (WAVE - 1)) * Lay<N>::LANES;       // (step, piece) in a row
+        if (count >= BLOCK) {
 #pragma unroll
-        for (int k = 0; k < Lay<N>::LANES; ++k) q[k] = row < count ? Elem<E>::up(v.v[k]) : 0.0f;
+            for (int k = 0; k < Lay<N>::LANES; ++k) q[k] = Elem<E>::up(v.v[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < Lay<N>::LANES; ++k) q[k] = row < count ? Elem<E>::up(v.v[k]) : 0.0f;
+        }
     }
 };
 
@@ -253,16 +267,15 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
     WalkFirst at_first;
     at_shared.start(p, t0, i, w);
     at_first.start(p, t0, i);
-    const E *safe_x = at_x - own * p.x.step, *safe_delta = at_delta - own * p.delta.step, *safe_z = at_z - own * p.z.step;
     E x[OWN], delta[OWN], z[OWN];
     auto fetch = [&](int count) {
-        at_first.load(count);
+        at_first.load(p.first.data != nullptr, count);
         at_shared.load(count);
-        load_own<E, OWN>(at_x, p.x.step, safe_x, own, count, x);
-        load_own<E, OWN>(at_delta, p.delta.step, safe_delta, own, count, delta);
-        if (gate) load_own<E, OWN>(at_z, p.z.step, safe_z, own, count, z);
-        at_first.at += at_first.step;
-        at_shared.at += at_shared.step;
+        load_own<E, OWN>(at_x, p.x.step, own, count, x);
+        load_own<E, OWN>(at_delta, p.delta.step, own, count, delta);
+        if (gate) load_own<E, OWN>(at_z, p.z.step, own, count, z);
+        at_first.move(1);
+        at_shared.move(1);
         at_x += BLOCK * p.x.step;
         at_delta += BLOCK * p.delta.step;
         at_z += BLOCK * p.z.step;
@@ -278,12 +291,12 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
         at_shared.stage(shared_lds[wave], count);
 #pragma unroll
         for (int k = 0; k < OWN; ++k) {
-            x_now[k] = whole || own + k < count ? Elem<E>::up(x[k]) : 0.0f;
+            x_now[k] = Elem<E>::up(x[k]);
             z_now[k] = gate ? Elem<E>::up(z[k]) : 0.0f;
             float size = Elem<E>::up(delta[k]) + bias;
             if (p.softplus) size = softplus(size);
             // steps behind the end leave the state as it is
-            if (!whole && own + k >= count) size = 0.0f;
+            if (!whole && own + k >= count) size = x_now[k] = 0.0f;
             step_lds[wave][(own + k) * CHANNELS + mine] = make_float2(size, size * x_now[k]);
         }
         wave_fence();

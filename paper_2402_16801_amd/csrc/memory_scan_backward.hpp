@@ -114,20 +114,18 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
             WalkFirst at_first;
             at_first.start(p, t, i);
             at_sums += t * sum_step;
-            const E *safe_x = p.x.at(t0, i) + w.channel, *safe_delta = p.delta.at(t0, i) + w.channel, *safe_dy = p.dy.at(t0, i) + w.channel;
-            const E* safe_z = gate ? p.z.at(t0, i) + w.channel : nullptr;
             E next_x[OWN], next_delta[OWN], next_dy[OWN], next_z[OWN];
             float next_h[4];
             auto fetch = [&](int count) {
-                at_first.load(count);
+                at_first.load(p.first.data != nullptr, count);
                 at_shared.load(count);
-                load_own<E, OWN>(at_x, step_x, safe_x, own, count, next_x);
-                load_own<E, OWN>(at_delta, step_delta, safe_delta, own, count, next_delta);
-                load_own<E, OWN>(at_dy, step_dy, safe_dy, own, count, next_dy);
-                if (gate) load_own<E, OWN>(at_z, step_z, safe_z, own, count, next_z);
+                load_own<E, OWN>(at_x, step_x, own, count, next_x);
+                load_own<E, OWN>(at_delta, step_delta, own, count, next_delta);
+                load_own<E, OWN>(at_dy, step_dy, own, count, next_dy);
+                if (gate) load_own<E, OWN>(at_z, step_z, own, count, next_z);
                 load4(at_saved, next_h);
-                at_first.at -= at_first.step;
-                at_shared.at -= at_shared.step;
+                at_first.move(-1);
+                at_shared.move(-1);
                 at_x -= BLOCK * step_x;
                 at_delta -= BLOCK * step_delta;
                 at_dy -= BLOCK * step_dy;
@@ -324,7 +322,6 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
     const int own = w.quad * OWN;
     int t = t0 + (end - t0 - 1) / BLOCK * BLOCK;
     const E *at_delta = walk_from<const E, N>(p.delta, t, i, w), *at_dy = walk_from<const E, N>(p.dy, t, i, w), *at_z = walk_from<const E, N>(p.z, t, i, w);
-    const E *safe_delta = p.delta.at(t0, i) + w.channel, *safe_dy = p.dy.at(t0, i) + w.channel, *safe_z = p.z.data ? p.z.at(t0, i) + w.channel : nullptr;
     WalkShared<E, N> at_shared;
     WalkFirst at_first;
     at_shared.start(p, t, i, w);
@@ -332,14 +329,14 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
     for (; t0 < end && t >= t0; t -= BLOCK) {
         const int count = end - t < BLOCK ? end - t : BLOCK;
         E delta[OWN], dy[OWN], z[OWN];
-        at_first.load(count);
+        at_first.load(p.first.data != nullptr, count);
         at_shared.load(count);
-        load_own<E, OWN>(at_delta, p.delta.step, safe_delta, own, count, delta);
-        load_own<E, OWN>(at_dy, p.dy.step, safe_dy, own, count, dy);
-        if (p.z.data) load_own<E, OWN>(at_z, p.z.step, safe_z, own, count, z);
+        load_own<E, OWN>(at_delta, p.delta.step, own, count, delta);
+        load_own<E, OWN>(at_dy, p.dy.step, own, count, dy);
+        if (p.z.data) load_own<E, OWN>(at_z, p.z.step, own, count, z);
         const uint32_t cuts = at_first.cuts(count);
-        at_first.at -= at_first.step;
-        at_shared.at -= at_shared.step;
+        at_first.move(-1);
+        at_shared.move(-1);
         at_delta -= BLOCK * p.delta.step;
         at_dy -= BLOCK * p.dy.step;
         at_z -= BLOCK * p.z.step;
