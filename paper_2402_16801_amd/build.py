@@ -56,13 +56,36 @@ def build_library(verbose: bool = False, only_changed: bool = False, debug_bound
     return out
 
 
+MARSHAL_SRC = os.path.join(_PKG, "csrc", "marshal.cpp")
+MARSHAL_OUT = os.path.join(_PKG, "_marshal.so")
+
+
+def build_marshal() -> str:
+    """The Python extension that hands tensors to the C ABI (see memory.py)."""
+    import sysconfig
+
+    from torch.utils.cpp_extension import include_paths, library_paths
+
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    cmd = (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM"] +
+           ["-I" + p for p in (*include_paths(), os.path.join(rocm, "include"), sysconfig.get_paths()["include"])] +
+           ["-o", MARSHAL_OUT, MARSHAL_SRC] + ["-L" + p for p in library_paths()] +
+           ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"])
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stderr)
+    return MARSHAL_OUT
+
+
 def build_all(only_changed: bool = False):
-    """The release library and the bounds-checking debug library, side by side."""
+    """The release library, the bounds-checking debug library and the marshalling extension, side by side."""
     from concurrent.futures import ThreadPoolExecutor
 
-    with ThreadPoolExecutor(max_workers=2) as ex:
+    with ThreadPoolExecutor(max_workers=3) as ex:
         a = ex.submit(build_library, False, only_changed, False)
         b = ex.submit(build_library, False, only_changed, True)
+        c = ex.submit(build_marshal)
+        c.result()
         return a.result(), b.result()
 
 
