@@ -109,6 +109,12 @@ template <typename T, int N> __device__ __forceinline__ void pin(T (&v)[N])
     for (int k = 0; k < N; ++k) pin(v[k]);
 }
 
+template <typename T, int N, int M> __device__ __forceinline__ void pin(T (&v)[N][M])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) pin(v[k]);
+}
+
 // ---- moves across lanes ----------------------------------------------------------------------------
 template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {

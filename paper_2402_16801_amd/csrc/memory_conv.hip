@@ -1,12 +1,17 @@
-// Short causal convolution of every channel with an activation: whole sequences, single tokens
-// (a sequence of one step) and the backward pass.
+// Short causal convolution of every channel with an activation: whole sequences, single tokens and the
+// backward pass.
 //
 // Bound by memory: 2 (forward) or 3 (backward) activations move per step and channel against about 12
 // and 30 instructions.  A thread owns V neighbouring channels of one environment (16 bytes forward)
 // and walks along a stretch of steps with the last taps - 1 inputs in registers, so an input is read
 // once but for the taps - 1 in front of a stretch.  Stretches exist only to fill the chip.
+//
+// A row whose length is no multiple of V ends with a vector that overlaps the one before it: it is loaded whole,
+// and only its own values are stored and counted.  Rows of fewer than V channels go value by value.
 #include "memory_api.hpp"
 #include "memory_common.hpp"
+
+#include <type_traits>
 
 namespace mem {
 
@@ -32,28 +37,37 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int steps, int 
     return l < 0 ? 0 : (l > steps ? steps : l);
 }
 
-// The last K - 1 inputs before step t as they count at step t - 1, for V channels from `c` on.
-template <typename E, int K, int V>
-__device__ __forceinline__ void window_before(const ConvParams<E>& p, int t, int i, int c, int count, float (&win)[K - 1][V])
+// The channels of a thread: V from `c` on, of which the first `old` belong to the thread before it.
+struct Span {
+    int c, old;
+    template <int V> __device__ __forceinline__ static Span of(int vector, int channels)
+    {
+        const int c = vector * V, last = channels - V;
+        return c <= last ? Span{c, 0} : Span{last, c - last};
+    }
+};
+
+template <typename E, int V> __device__ __forceinline__ void fetch(Pack<E, V>& q, const E* p) { q = *reinterpret_cast<const Pack<E, V>*>(p); }
+template <typename E, int V> __device__ __forceinline__ void expand(const Pack<E, V>& q, float (&v)[V])
 {
 #pragma unroll
-    for (int k = 0; k < K - 1; ++k) {
-        const int s = t - (K - 1) + k;
-        if (s >= 0) {
-            if (p.first.data && *p.first.at(s, i)) {
+    for (int j = 0; j < V; ++j) v[j] = Elem<E>::up(q.v[j]);
+}
+template <typename E, int V> __device__ __forceinline__ Pack<E, V> shrink(const float (&v)[V])
+{
+    Pack<E, V> q;
 #pragma unroll
-                for (int m = 0; m < K - 1; ++m)
+    for (int j = 0; j < V; ++j) q.v[j] = Elem<E>::down(v[j]);
+    return q;
+}
+template <typename E, int V> __device__ __forceinline__ void put(E* p, const Span& w, const Pack<E, V>& q)
+{
+    if (w.old == 0) {
+        *reinterpret_cast<Pack<E, V>*>(p) = q;
+    } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        if (m < k) win[m][j] = 0.0f;
-            }
-            load_row<E, V>(p.x.at(s, i) + c, count, win[k]);
-        } else if (p.state_in) {
-            load_row<E, V>(p.state_in + ((int64_t)i * (K - 1) + (s + K - 1)) * p.channels + c, count, win[k]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) win[k][j] = 0.0f;
-        }
+        for (int j = 0; j < V; ++j)
+            if (j >= w.old) p[j] = q.v[j];
     }
 }
 
@@ -77,17 +91,49 @@ __device__ __forceinline__ void clear(float (&win)[K - 1][V])
         for (int j = 0; j < V; ++j) win[k][j] = 0.0f;
 }
 
+// The last K - 1 inputs before step t as they count at step t - 1.  All loads are under way together.
+template <typename E, int K, int V>
+__device__ __forceinline__ void window_before(const ConvParams<E>& p, int t, int i, const Span& w, float (&win)[K - 1][V])
+{
+    Pack<E, V> raw[K - 1];
+    bool begin[K - 1];
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) {
+        const int s = t - (K - 1) + k;
+        const E* from = s >= 0 || !p.state_in ? p.x.at(s < 0 ? 0 : s, i) : p.state_in + ((int64_t)i * (K - 1) + (s + K - 1)) * p.channels;
+        fetch<E, V>(raw[k], from + w.c);
+        begin[k] = p.first.data && s >= 0 && *p.first.at(s, i) != 0;
+    }
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) {
+        if (begin[k]) {
+#pragma unroll
+            for (int m = 0; m < K - 1; ++m)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (m < k) win[m][j] = 0.0f;
+        }
+        expand<E, V>(raw[k], win[k]);
+        if (t - (K - 1) + k < 0 && !p.state_in) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) win[k][j] = 0.0f;
+        }
+    }
+}
+
 template <int K, int V> struct Taps {
     float w[K][V], bias[V];
-    __device__ __forceinline__ void load(const float* weight, const float* b, int c, int count)
+    __device__ __forceinline__ void load(const float* weight, const float* b, int c)
     {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int d = c + (j < count ? j : 0);
+            Pack<float, K> q = *reinterpret_cast<const Pack<float, K>*>(weight + (int64_t)(c + j) * K);
 #pragma unroll
-            for (int k = 0; k < K; ++k) w[k][j] = weight[(int64_t)d * K + k];
-            bias[j] = b ? b[d] : 0.0f;
+            for (int k = 0; k < K; ++k) w[k][j] = q.v[k];
         }
+        const Pack<float, V> q = b ? *reinterpret_cast<const Pack<float, V>*>(b + c) : Pack<float, V>{};
+#pragma unroll
+        for (int j = 0; j < V; ++j) bias[j] = q.v[j];
     }
     __device__ __forceinline__ float sum(const float (&win)[K - 1][V], float x, int j) const
     {
@@ -98,57 +144,156 @@ template <int K, int V> struct Taps {
     }
 };
 
-template <typename E, int K, int V>
+// One sequence, read AHEAD steps in front of the step that is computed: raw[a] holds step t + a as it lies in memory and
+// is refilled as soon as it is used.  Behind the last step that one is read again.
+template <typename E, int V, int AHEAD> struct Stream {
+    const E *next, *last;
+    int64_t step;
+    Pack<E, V> raw[AHEAD];
+    __device__ __forceinline__ void refill(int a)
+    {
+        fetch<E, V>(raw[a], next);
+        next = next == last ? last : next + step;
+    }
+    __device__ __forceinline__ void start(const Seq<const E>& q, int t, int end, int i, int c)
+    {
+        step = q.step;
+        next = q.at(t, i) + c;
+        last = q.at(end - 1, i) + c;
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) refill(a);
+    }
+};
+// the same for the begins of episodes, where they are given
+template <int AHEAD> struct Begins {
+    const uint8_t *next, *last;
+    int64_t step;
+    uint32_t flag[AHEAD];
+    __device__ __forceinline__ void refill(int a)
+    {
+        flag[a] = *next;
+        next = next == last ? last : next + step;
+    }
+    __device__ __forceinline__ void start(const Seq<const uint8_t>& q, int t, int end, int i)
+    {
+        step = q.step;
+        next = q.at(t, i);
+        last = q.at(end - 1, i);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) refill(a);
+    }
+};
+
+// CUTS: begins of episodes are given
+template <typename E, int K, int V, bool CUTS>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv(const ConvParams<E> p)
 {
+    constexpr int AHEAD = 4;
     const uint32_t at = blockIdx.x * CONV_THREADS + threadIdx.x;
     const int i = (int)(at / (uint32_t)p.vectors);
     if (i >= p.n) return;
-    const int c = (int)(at % (uint32_t)p.vectors) * V;
-    const int count = p.channels - c < V ? p.channels - c : V;
+    const Span w = Span::of<V>((int)(at % (uint32_t)p.vectors), p.channels);
     const int t0 = (int)blockIdx.y * p.stretch;
     const int t1 = p.steps - t0 < p.stretch ? p.steps : t0 + p.stretch;
     const int length = length_of(p.lengths, p.steps, i);
     const int live = t1 < length ? t1 : length;       // steps of this stretch that count end here
-    Taps<K, V> taps;
-    taps.load(p.weight, p.bias, c, count);
     float win[K - 1][V];
-    if (t0 < live || t0 == 0) window_before<E, K, V>(p, t0, i, c, count, win);
-    constexpr int AHEAD = 4;
-    int t = t0;
-    for (; t < live; t += AHEAD) {
-        float x[AHEAD][V];
-        uint32_t starts = 0;
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            const int s = t + a < live ? t + a : live - 1;
-            load_row<E, V>(p.x.at(s, i) + c, count, x[a]);
-            if (p.first.data) starts |= (uint32_t)(*p.first.at(s, i) != 0) << a;
-        }
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            if (t + a >= live) break;
-            if (starts >> a & 1u) clear<K, V>(win);
-            float out[V];
+    if (t0 < live || t0 == 0) window_before<E, K, V>(p, t0, i, w, win);
+    if (t0 < live) {
+        Taps<K, V> taps;
+        Stream<E, V, AHEAD> in;
+        Begins<AHEAD> begins;
+        in.start(p.x, t0, live, i, w.c);
+        if (CUTS) begins.start(p.first, t0, live, i);
+        taps.load(p.weight, p.bias, w.c);
+        E* to = p.y.at(t0, i) + w.c;
+        auto one = [&](int a) {
+            float x[V], y[V];
+            expand<E, V>(in.raw[a], x);
+            in.refill(a);
+            if (CUTS) {
+                if (begins.flag[a]) clear<K, V>(win);
+                begins.refill(a);
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float v = taps.sum(win, x[a][j], j);
-                out[j] = p.silu ? v * sigmoid(v) : v;
+                const float v = taps.sum(win, x[j], j), g = sigmoid(v);
+                y[j] = v * (p.silu ? g : 1.0f);
             }
-            push<K, V>(win, x[a]);
-            store_row<E, V>(p.y.at(t + a, i) + c, count, out);
-        }
-    }
-    float none[V];
+            push<K, V>(win, x);
+            put<E, V>(to, w, shrink<E, V>(y));
+            to += p.y.step;
+            __builtin_amdgcn_sched_barrier(0);       // step by step: several at a time would take the registers of two more wavefronts
+        };
+        int t = t0;
+        for (; t + AHEAD <= live; t += AHEAD) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) none[j] = 0.0f;
-    for (t = t0 > live ? t0 : live; t < t1; ++t) store_row<E, V>(p.y.at(t, i) + c, count, none);
+            for (int a = 0; a < AHEAD; ++a) one(a);
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD - 1; ++a)
+            if (t + a < live) one(a);
+    }
+    for (int t = t0 > live ? t0 : live; t < t1; ++t) put<E, V>(p.y.at(t, i) + w.c, w, Pack<E, V>{});
     // The thread of the first stretch, which alone reads the state, writes the new one too, so that it can
     // be the same memory.  With one stretch the window is what is wanted.
     if (p.state_out && blockIdx.y == 0) {
-        if (live < length) window_before<E, K, V>(p, length, i, c, count, win);
+        if (live < length) window_before<E, K, V>(p, length, i, w, win);
 #pragma unroll
-        for (int k = 0; k < K - 1; ++k) store_row<E, V>(p.state_out + ((int64_t)i * (K - 1) + k) * p.channels + c, count, win[k]);
+        for (int k = 0; k < K - 1; ++k) put<E, V>(p.state_out + ((int64_t)i * (K - 1) + k) * p.channels + w.c, w, shrink<E, V>(win[k]));
+    }
+}
+
+// One token: the state is read and written once, 2 K activations per channel.  A thread takes several environments one
+// after the other, so that its weights (16 bytes per channel against 16 of activations) are read once.
+template <typename E, int K, int V>
+__global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E> p)
+{
+    const uint32_t at = blockIdx.x * CONV_THREADS + threadIdx.x;
+    int i = (int)(at / (uint32_t)p.vectors);
+    if (i >= p.stretch) return;                 // here: environments that are taken side by side
+    const Span w = Span::of<V>((int)(at % (uint32_t)p.vectors), p.channels);
+    Taps<K, V> taps;
+    taps.load(p.weight, p.bias, w.c);
+    Pack<E, V> raw[K];
+    uint32_t flag = 0;
+    int length = 1;
+    auto load = [&](int e) {
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k)
+            fetch<E, V>(raw[k], (p.state_in ? p.state_in + ((int64_t)e * (K - 1) + k) * p.channels : p.x.at(0, e)) + w.c);
+        fetch<E, V>(raw[K - 1], p.x.at(0, e) + w.c);
+        if (p.first.data) flag = *p.first.at(0, e);
+        if (p.lengths) length = p.lengths[e];
+    };
+    load(i);
+    for (; i < p.n; i += p.stretch) {
+        float win[K - 1][V], x[V], y[V];
+        const bool live = length > 0, empty = !p.state_in || (flag && live);
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) expand<E, V>(raw[k], win[k]);
+        expand<E, V>(raw[K - 1], x);
+        if (empty) clear<K, V>(win);
+        Pack<E, V> keep[K - 1];
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) {
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = !live ? win[k][j] : (k + 1 < K - 1 ? win[k + 1 < K - 1 ? k + 1 : 0][j] : x[j]);
+            keep[k] = shrink<E, V>(v);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float v = taps.sum(win, x[j], j), g = sigmoid(v);
+            y[j] = live ? v * (p.silu ? g : 1.0f) : 0.0f;
+        }
+        const int e = i;
+        if (i + p.stretch < p.n) load(i + p.stretch);
+        put<E, V>(p.y.at(0, e) + w.c, w, shrink<E, V>(y));
+        if (p.state_out) {
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k) put<E, V>(p.state_out + ((int64_t)e * (K - 1) + k) * p.channels + w.c, w, keep[k]);
+        }
     }
 }
 
@@ -158,15 +303,13 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv(const ConvParams<E> p)
 // step; a stretch goes K - 1 steps beyond its end for the inputs at its end, without counting those steps
 // for the weight.  A block sums its weight gradients in LDS and writes one partial row; rows are added in a
 // fixed order by a second kernel.
-template <typename E, int K, int V>
+template <typename E, int K, int V, bool CUTS>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams<E> p)
 {
-    constexpr int COLS = V * (K + 1);
+    constexpr int COLS = V * (K + 1), AHEAD = 4;
     __shared__ float sums[CONV_THREADS * COLS];
     const int lanes = 1 << p.lanes_log2, side = threadIdx.x >> p.lanes_log2, rows = CONV_THREADS >> p.lanes_log2;
     const int vec = (int)blockIdx.x * lanes + (threadIdx.x & (lanes - 1));
-    const int c = vec * V;
-    const int count = p.channels - c < V ? p.channels - c : V;
     const int stretches = (p.steps + p.stretch - 1) / p.stretch;
     float dw[K][V], db[V];
 #pragma unroll
@@ -175,72 +318,95 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams
 #pragma unroll
         for (int k = 0; k < K; ++k) dw[k][j] = 0.0f;
     }
-    if (count > 0) {
+    if (vec < p.vectors) {
+        const Span w = Span::of<V>(vec, p.channels);
         Taps<K, V> taps;
-        taps.load(p.weight, p.bias, c, count);
+        taps.load(p.weight, p.bias, w.c);
         const int64_t items = (int64_t)p.n * stretches;
         for (int64_t item = (int64_t)blockIdx.y * rows + side; item < items; item += (int64_t)gridDim.y * rows) {
-            const int i = (int)(item % p.n), t0 = (int)(item / p.n) * p.stretch;
+            const int i = (int)((uint64_t)item % (uint32_t)p.n), t0 = (int)((uint64_t)item / (uint32_t)p.n) * p.stretch;
             const int t1 = p.steps - t0 < p.stretch ? p.steps : t0 + p.stretch;
             const int length = length_of(p.lengths, p.steps, i);
             const int live = t1 < length ? t1 : length;
             const int end = length - t1 < K - 1 ? length : t1 + (K - 1);     // steps walked: up to here
-            float none[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) none[j] = 0.0f;
-            for (int t = t0 > live ? t0 : live; t < t1; ++t) store_row<E, V>(p.dx.at(t, i) + c, count, none);
+            for (int t = t0 > live ? t0 : live; t < t1; ++t) put<E, V>(p.dx.at(t, i) + w.c, w, Pack<E, V>{});
             if (t0 >= live && t0 > 0) continue;
+            auto state_at = [&](int s) { return p.dstate_in + ((int64_t)i * (K - 1) + (s + K - 1)) * p.channels + w.c; };
             float win[K - 1][V], due[K - 1][V];
-            window_before<E, K, V>(p, t0, i, c, count, win);
+            window_before<E, K, V>(p, t0, i, w, win);
             clear<K, V>(due);
             // steps since the last begin of an episode, as far as the window reaches back
             int age = K - 1;
-            if (p.first.data)
+            if (CUTS)
                 for (int s = t0 - (K - 1) > 0 ? t0 - (K - 1) : 0; s < t0; ++s)
                     age = *p.first.at(s, i) ? 0 : (age < K - 1 ? age + 1 : K - 1);
-            constexpr int AHEAD = 2;
-            for (int t = t0; t < end; t += AHEAD) {
-                float x[AHEAD][V], dy[AHEAD][V];
-                uint32_t starts = 0;
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) {
-                    const int s = t + a < end ? t + a : end - 1;
-                    load_row<E, V>(p.x.at(s, i) + c, count, x[a]);
-                    load_row<E, V>(p.dy.at(s, i) + c, count, dy[a]);
-                    if (p.first.data) starts |= (uint32_t)(*p.first.at(s, i) != 0) << a;
-                }
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) {
-                    if (t + a >= end) break;
-                    if (starts >> a & 1u) { clear<K, V>(win); age = 0; }
-                    else if (age < K - 1) ++age;
-                    const bool counts = t + a < t1;
-                    float now[V];
+            if (t0 < live) {
+                Stream<E, V, AHEAD> in_x, in_dy;
+                Begins<AHEAD> begins;
+                in_x.start(p.x, t0, live, i, w.c);
+                in_dy.start(p.dy, t0, live, i, w.c);
+                if (CUTS) begins.start(p.first, t0, live, i);
+                E* to = p.dx.at(t0, i) + w.c;            // of the oldest input in the window, once that is in the stretch
+                auto one = [&](int t, const Pack<E, V>& raw_x, const Pack<E, V>& raw_dy, bool begin, auto counts) {
+                    float x[V], dy[V], now[V];
+                    expand<E, V>(raw_x, x);
+                    expand<E, V>(raw_dy, dy);
+                    if (CUTS) {
+                        age = begin ? 0 : age < K - 1 ? age + 1 : K - 1;
+                        if (begin) clear<K, V>(win);
+                    }
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        float dp = dy[a][j];
-                        if (p.silu) {
-                            const float v = taps.sum(win, x[a][j], j), g = sigmoid(v);
-                            dp *= g * __builtin_fmaf(v, 1.0f - g, 1.0f);
-                        }
+                        const float v = taps.sum(win, x[j], j), g = sigmoid(v), slope = g * __builtin_fmaf(v, 1.0f - g, 1.0f);
+                        const float dp = dy[j] * (p.silu ? slope : 1.0f);
                         now[j] = taps.w[K - 1][j] * dp;
 #pragma unroll
                         for (int k = 0; k < K - 1; ++k)
-                            if (age >= K - 1 - k) due[k][j] = __builtin_fmaf(taps.w[k][j], dp, due[k][j]);
-                        if (counts) {
+                            due[k][j] = __builtin_fmaf(taps.w[k][j], !CUTS || age >= K - 1 - k ? dp : 0.0f, due[k][j]);
+                        if (decltype(counts)::value) {
                             db[j] += dp;
 #pragma unroll
                             for (int k = 0; k < K - 1; ++k) dw[k][j] = __builtin_fmaf(dp, win[k][j], dw[k][j]);
-                            dw[K - 1][j] = __builtin_fmaf(dp, x[a][j], dw[K - 1][j]);
+                            dw[K - 1][j] = __builtin_fmaf(dp, x[j], dw[K - 1][j]);
                         }
                     }
-                    // the oldest input, t + a - (K - 1), is complete
-                    const int s = t + a - (K - 1);
-                    if (s >= t0) store_row<E, V>(p.dx.at(s, i) + c, count, due[0]);
-                    else if (s < 0 && p.dstate_in)
-                        store_row<E, V>(p.dstate_in + ((int64_t)i * (K - 1) + (s + K - 1)) * p.channels + c, count, due[0]);
-                    push<K, V>(win, x[a]);
+                    // the oldest input, t - (K - 1), is complete
+                    const int s = t - (K - 1);
+                    if (s >= t0) {
+                        put<E, V>(to, w, shrink<E, V>(due[0]));
+                        to += p.dx.step;
+                    } else if (s < 0 && p.dstate_in) {
+                        put<E, V>(state_at(s), w, shrink<E, V>(due[0]));
+                    }
+                    push<K, V>(win, x);
                     push<K, V>(due, now);
+                    // all of a step is done in its turn: put off, the sums would keep several steps' factors in registers
+                    pin(dw);
+                    pin(db);
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                auto streamed = [&](int t, int a) {
+                    const Pack<E, V> raw_x = in_x.raw[a], raw_dy = in_dy.raw[a];
+                    const bool begin = CUTS && begins.flag[a] != 0;
+                    in_x.refill(a);
+                    in_dy.refill(a);
+                    if (CUTS) begins.refill(a);
+                    one(t, raw_x, raw_dy, begin, std::true_type{});
+                };
+                int t = t0;
+                for (; t + AHEAD <= live; t += AHEAD) {
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a) streamed(t + a, a);
+                }
+#pragma unroll
+                for (int a = 0; a < AHEAD - 1; ++a)
+                    if (t + a < live) streamed(t + a, a);
+                // steps behind the stretch, for its last inputs
+                for (t = live; t < end; ++t) {
+                    Pack<E, V> raw_x, raw_dy;
+                    fetch<E, V>(raw_x, p.x.at(t, i) + w.c);
+                    fetch<E, V>(raw_dy, p.dy.at(t, i) + w.c);
+                    one(t, raw_x, raw_dy, CUTS && *p.first.at(t, i) != 0, std::false_type{});
                 }
             }
             // What the walk left: the inputs end - (K - 1) .. end - 1.  At the end of the sequence they are also the new
@@ -250,14 +416,15 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams
                 for (int k = 0; k < K - 1; ++k) {
                     const int s = length - (K - 1) + k;
                     if (p.dstate_out && age >= K - 2 - k) {
+                        Pack<E, V> raw;
                         float add[V];
-                        load_row<E, V>(p.dstate_out + ((int64_t)i * (K - 1) + k) * p.channels + c, count, add);
+                        fetch<E, V>(raw, p.dstate_out + ((int64_t)i * (K - 1) + k) * p.channels + w.c);
+                        expand<E, V>(raw, add);
 #pragma unroll
                         for (int j = 0; j < V; ++j) due[k][j] += add[j];
                     }
-                    if (s >= t0 && s < t1) store_row<E, V>(p.dx.at(s, i) + c, count, due[k]);
-                    else if (s < 0 && p.dstate_in)
-                        store_row<E, V>(p.dstate_in + ((int64_t)i * (K - 1) + (s + K - 1)) * p.channels + c, count, due[k]);
+                    if (s >= t0 && s < t1) put<E, V>(p.dx.at(s, i) + w.c, w, shrink<E, V>(due[k]));
+                    else if (s < 0 && p.dstate_in) put<E, V>(state_at(s), w, shrink<E, V>(due[k]));
                 }
             }
         }
@@ -274,11 +441,13 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams
     float* row = p.part + (int64_t)blockIdx.y * (K + 1) * p.channels;
     for (int q = threadIdx.x; q < COLS * lanes; q += CONV_THREADS) {
         const int lane = q & (lanes - 1), value = q >> p.lanes_log2, j = value / (K + 1), k = value % (K + 1);
-        const int d = ((int)blockIdx.x * lanes + lane) * V + j;
-        if (d >= p.channels) continue;
+        const int v = (int)blockIdx.x * lanes + lane;
+        if (v >= p.vectors) continue;
+        const Span w = Span::of<V>(v, p.channels);
+        if (j < w.old) continue;
         float s = 0.0f;
         for (int r = 0; r < rows; ++r) s += sums[value * CONV_THREADS + (r << p.lanes_log2) + lane];
-        row[(int64_t)k * p.channels + d] = s;
+        row[(int64_t)k * p.channels + w.c + j] = s;
     }
 }
 
@@ -344,21 +513,42 @@ static int stretch_of(int steps, int64_t threads_per_step, int64_t threads)
 
 constexpr int64_t CONV_FILL = (int64_t)CHIP_SIMDS * 4 * WAVE;     // four wavefronts per SIMD
 
+// calls f with the taps and the channels per thread as constants
+template <int WIDE, typename F> static void with_taps(const craftax_conv_args* a, F&& f)
+{
+    auto wide = [&](auto taps) {
+        if (a->channels >= WIDE) f(taps, std::integral_constant<int, WIDE>{});
+        else f(taps, std::integral_constant<int, 1>{});
+    };
+    if (a->taps == 2) wide(std::integral_constant<int, 2>{});
+    else if (a->taps == 3) wide(std::integral_constant<int, 3>{});
+    else wide(std::integral_constant<int, 4>{});
+}
+
 int conv(const craftax_conv_args* a, void* stream, const char** why)
 {
     if (int rc = conv_check(a, false, why)) return rc;
+    const hipStream_t st = (hipStream_t)stream;
     with_type(a->dtype, [&](auto e) {
         using E = decltype(e);
-        constexpr int V = 16 / sizeof(E);
-        ConvParams<E> p = conv_params<E>(a);
-        p.vectors = (int)ceil_div(a->channels, V);
-        const int64_t threads = (int64_t)a->n * p.vectors;
-        p.stretch = stretch_of(a->steps, threads, CONV_FILL);
-        const dim3 grid((unsigned)ceil_div(threads, CONV_THREADS), (unsigned)ceil_div(a->steps, p.stretch));
-        const hipStream_t st = (hipStream_t)stream;
-        if (a->taps == 2) hipLaunchKernelGGL((k_conv<E, 2, V>), grid, dim3(CONV_THREADS), 0, st, p);
-        else if (a->taps == 3) hipLaunchKernelGGL((k_conv<E, 3, V>), grid, dim3(CONV_THREADS), 0, st, p);
-        else hipLaunchKernelGGL((k_conv<E, 4, V>), grid, dim3(CONV_THREADS), 0, st, p);
+        with_taps<16 / sizeof(E)>(a, [&](auto taps, auto width) {
+            constexpr int K = decltype(taps)::value, V = decltype(width)::value;
+            ConvParams<E> p = conv_params<E>(a);
+            p.vectors = (int)ceil_div(a->channels, V);
+            const int64_t threads = (int64_t)a->n * p.vectors;
+            if (a->steps == 1) {
+                // environments side by side: two wavefronts per SIMD, each with several environments in turn, or all of them
+                const int64_t side = ceil_div(CONV_FILL / 2, p.vectors);
+                p.stretch = (int)(side < a->n ? side : a->n);
+                const dim3 grid((unsigned)ceil_div((int64_t)p.stretch * p.vectors, CONV_THREADS));
+                hipLaunchKernelGGL((k_conv_token<E, K, V>), grid, dim3(CONV_THREADS), 0, st, p);
+                return;
+            }
+            p.stretch = stretch_of(a->steps, threads, CONV_FILL);
+            const dim3 grid((unsigned)ceil_div(threads, CONV_THREADS), (unsigned)ceil_div(a->steps, p.stretch));
+            if (p.first.data) hipLaunchKernelGGL((k_conv<E, K, V, true>), grid, dim3(CONV_THREADS), 0, st, p);
+            else hipLaunchKernelGGL((k_conv<E, K, V, false>), grid, dim3(CONV_THREADS), 0, st, p);
+        });
     });
     return launched(why);
 }
@@ -370,7 +560,7 @@ struct ConvBack { int vectors, lanes_log2, stretch; unsigned x, y; };
 static ConvBack conv_back(const craftax_conv_args* a)
 {
     ConvBack b;
-    b.vectors = (int)ceil_div(a->channels, CONV_BACK_V);
+    b.vectors = (int)ceil_div(a->channels, a->channels >= CONV_BACK_V ? CONV_BACK_V : 1);
     b.lanes_log2 = 2;
     while (b.lanes_log2 < 6 && (1 << b.lanes_log2) < b.vectors) ++b.lanes_log2;
     const int lanes = 1 << b.lanes_log2, rows = CONV_THREADS / lanes;
@@ -406,9 +596,11 @@ int conv_backward(const craftax_conv_args* a, void* stream, const char** why)
         p.vectors = b.vectors; p.lanes_log2 = b.lanes_log2; p.stretch = b.stretch;
         p.part = need ? static_cast<float*>(a->workspace) : nullptr;
         const dim3 grid(b.x, b.y);
-        if (a->taps == 2) hipLaunchKernelGGL((k_conv_backward<E, 2, CONV_BACK_V>), grid, dim3(CONV_THREADS), 0, st, p);
-        else if (a->taps == 3) hipLaunchKernelGGL((k_conv_backward<E, 3, CONV_BACK_V>), grid, dim3(CONV_THREADS), 0, st, p);
-        else hipLaunchKernelGGL((k_conv_backward<E, 4, CONV_BACK_V>), grid, dim3(CONV_THREADS), 0, st, p);
+        with_taps<CONV_BACK_V>(a, [&](auto taps, auto width) {
+            constexpr int K = decltype(taps)::value, V = decltype(width)::value;
+            if (p.first.data) hipLaunchKernelGGL((k_conv_backward<E, K, V, true>), grid, dim3(CONV_THREADS), 0, st, p);
+            else hipLaunchKernelGGL((k_conv_backward<E, K, V, false>), grid, dim3(CONV_THREADS), 0, st, p);
+        });
     });
     if (int rc = launched(why)) return rc;
     if (need)
