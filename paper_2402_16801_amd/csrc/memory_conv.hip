@@ -2,7 +2,7 @@
 // backward pass.
 //
 // Bound by memory: 2 (forward) or 3 (backward) activations move per step and channel against about 12
-// and 30 instructions.  A thread owns V neighbouring channels of one environment (16 bytes forward)
+// and 30 instructions.  A thread owns four neighbouring channels of one environment
 // and walks along a stretch of steps with the last taps - 1 inputs in registers, so an input is read
 // once but for the taps - 1 in front of a stretch.  Stretches exist only to fill the chip.
 //
@@ -212,8 +212,12 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv(const ConvParams<E> p)
             expand<E, V>(in.raw[a], x);
             in.refill(a);
             if (CUTS) {
-                if (begins.flag[a]) clear<K, V>(win);
+                const bool begin = begins.flag[a] != 0;
                 begins.refill(a);
+#pragma unroll
+                for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) win[k][j] = begin ? 0.0f : win[k][j];
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -531,7 +535,7 @@ int conv(const craftax_conv_args* a, void* stream, const char** why)
     const hipStream_t st = (hipStream_t)stream;
     with_type(a->dtype, [&](auto e) {
         using E = decltype(e);
-        with_taps<16 / sizeof(E)>(a, [&](auto taps, auto width) {
+        with_taps<4>(a, [&](auto taps, auto width) {
             constexpr int K = decltype(taps)::value, V = decltype(width)::value;
             ConvParams<E> p = conv_params<E>(a);
             p.vectors = (int)ceil_div(a->channels, V);
@@ -544,7 +548,7 @@ int conv(const craftax_conv_args* a, void* stream, const char** why)
                 hipLaunchKernelGGL((k_conv_token<E, K, V>), grid, dim3(CONV_THREADS), 0, st, p);
                 return;
             }
-            p.stretch = stretch_of(a->steps, threads, CONV_FILL);
+            p.stretch = stretch_of(a->steps, threads, 2 * CONV_FILL);
             const dim3 grid((unsigned)ceil_div(threads, CONV_THREADS), (unsigned)ceil_div(a->steps, p.stretch));
             if (p.first.data) hipLaunchKernelGGL((k_conv<E, K, V, true>), grid, dim3(CONV_THREADS), 0, st, p);
             else hipLaunchKernelGGL((k_conv<E, K, V, false>), grid, dim3(CONV_THREADS), 0, st, p);

@@ -3,7 +3,7 @@
 //
 // Bound by memory: a row is read once, kept in registers, and written once (forward 3 in, 2 out with a gate;
 // backward 5 in, 3 out).  The backward pass computes the two roots again from the row, which is there
-// anyway, so nothing is saved between the passes.  A row belongs to W wavefronts, as few as hold it with 16
+// anyway, so nothing is saved between the passes.  A row belongs to W wavefronts, as few as hold it with 8
 // values per lane; with one wavefront every sum stays inside it, with more the sums meet in LDS.
 // Blocks go on to further rows with the weights, and in the backward pass their gradients, in registers.
 #include "memory_api.hpp"
@@ -41,17 +41,18 @@ __device__ __forceinline__ float row_sum(float v, float* slots)
     return v;
 }
 
+// act(gate) and its derivative; written as selections, so that no branch stands between the elements of a row
 __device__ __forceinline__ float gate_value(float g, int act)
 {
-    if (act == CRAFTAX_GATE_LINEAR) return g;
-    const float s = sigmoid(g);
-    return act == CRAFTAX_GATE_SIGMOID ? s : g * s;
+    const float s = sigmoid(g), both = g * s;
+    const float v = act == CRAFTAX_GATE_SILU ? both : s;
+    return act == CRAFTAX_GATE_LINEAR ? g : v;
 }
 __device__ __forceinline__ float gate_slope(float g, int act)
 {
-    if (act == CRAFTAX_GATE_LINEAR) return 1.0f;
-    const float s = sigmoid(g);
-    return act == CRAFTAX_GATE_SIGMOID ? s * (1.0f - s) : s * __builtin_fmaf(g, 1.0f - s, 1.0f);
+    const float s = sigmoid(g), t = 1.0f - s, of_sigmoid = s * t, of_silu = s * __builtin_fmaf(g, t, 1.0f);
+    const float v = act == CRAFTAX_GATE_SILU ? of_silu : of_sigmoid;
+    return act == CRAFTAX_GATE_LINEAR ? 1.0f : v;
 }
 
 // What is left of g without its part along the unit row, g - unit * mean(g * unit).  The mean of unit * unit is
@@ -69,61 +70,120 @@ template <int W> struct RowBlock {
     static constexpr int ROWS = THREADS / (W * WAVE);      // rows a block works on at once
 };
 
-template <int CHUNKS, int V> struct RowPlace {
-    int at[CHUNKS], count[CHUNKS];       // first value and number of values of this lane's chunks
-    __device__ __forceinline__ RowPlace(int channels, int side, int width)
+// Where a lane's chunks of V values lie in a row.  A chunk that passes the end of the row is moved back to end with it, and
+// its first `old` values are not this lane's (those of a lane with nothing left: all V).  Rows shorter than V are read
+// value by value.
+template <int CHUNKS, int V, bool WHOLE> struct RowPlace {
+    int at[CHUNKS], old[CHUNKS], channels;
+    __device__ __forceinline__ RowPlace(int n, int side, int width) : channels(n)
     {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            at[c] = (c * width + side) * V;
-            const int left = channels - at[c];
-            count[c] = left < 0 ? 0 : (left < V ? left : V);
+            const int first = (c * width + side) * V, last = n - V;
+            at[c] = WHOLE || first <= last ? first : (last < 0 ? 0 : last);
+            const int gone = first - at[c];
+            old[c] = WHOLE ? 0 : (gone < V ? gone : V);
+            if (!WHOLE && last < 0) old[c] = first == 0 ? 0 : V;
         }
+    }
+    __device__ __forceinline__ bool mine(int c, int j) const
+    {
+        return WHOLE || (j >= old[c] && (channels >= V || j < channels));
     }
 };
 
-template <int CHUNKS, int V, typename P, typename T>
-__device__ __forceinline__ void load_chunks(const RowPlace<CHUNKS, V>& place, const P* p, T (&v)[CHUNKS][V])
+template <typename P, int CHUNKS, int V, bool WHOLE>
+__device__ __forceinline__ void fetch(const RowPlace<CHUNKS, V, WHOLE>& w, const P* p, Pack<P, V> (&q)[CHUNKS])
+{
+    if (WHOLE || w.channels >= V) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) q[c] = *reinterpret_cast<const Pack<P, V>*>(p + w.at[c]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) q[c].v[j] = p[j < w.channels ? j : 0];
+    }
+}
+// the lane's own values, 0 elsewhere
+template <typename P, int CHUNKS, int V, bool WHOLE>
+__device__ __forceinline__ void expand(const RowPlace<CHUNKS, V, WHOLE>& w, const Pack<P, V> (&q)[CHUNKS], float (&v)[CHUNKS][V])
 {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) load_row<P, V>(p + place.at[c], place.count[c], v[c]);
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[c][j] = w.mine(c, j) ? Elem<P>::up(q[c].v[j]) : 0.0f;
 }
-template <int CHUNKS, int V, typename P>
-__device__ __forceinline__ void store_chunks(const RowPlace<CHUNKS, V>& place, P* p, const float (&v)[CHUNKS][V])
+template <typename P, int CHUNKS, int V, bool WHOLE>
+__device__ __forceinline__ void put(const RowPlace<CHUNKS, V, WHOLE>& w, P* p, const float (&v)[CHUNKS][V])
 {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) store_row<P, V>(p + place.at[c], place.count[c], v[c]);
+    for (int c = 0; c < CHUNKS; ++c) {
+        if (WHOLE || (w.old[c] == 0 && w.channels >= V)) {
+            Pack<P, V> q;
+#pragma unroll
+            for (int j = 0; j < V; ++j) q.v[j] = Elem<P>::down(v[c][j]);
+            *reinterpret_cast<Pack<P, V>*>(p + w.at[c]) = q;
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (w.mine(c, j)) p[w.at[c] + j] = Elem<P>::down(v[c][j]);
+        }
+    }
 }
-template <int CHUNKS, int V>
-__device__ __forceinline__ void load_weight(const RowPlace<CHUNKS, V>& place, const float* p, float (&v)[CHUNKS][V])
+template <int CHUNKS, int V, bool WHOLE>
+__device__ __forceinline__ void load_weight(const RowPlace<CHUNKS, V, WHOLE>& w, const float* p, float (&v)[CHUNKS][V])
 {
-    if (p) { load_chunks<CHUNKS, V>(place, p, v); return; }
+    Pack<float, V> q[CHUNKS];
+    if (p) {
+        fetch(w, p, q);
+        expand(w, q, v);
+        return;
+    }
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int j = 0; j < V; ++j) v[c][j] = 1.0f;
 }
+// the values have arrived
+template <typename P, int CHUNKS, int V> __device__ __forceinline__ void pin(Pack<P, V> (&q)[CHUNKS])
+{
+    uint32_t words[sizeof(q) / 4];
+    __builtin_memcpy(words, q, sizeof(q));
+    pin(words);
+    __builtin_memcpy(q, words, sizeof(q));
+}
 
-template <typename E, typename R, int W, int CHUNKS>
+template <typename E, typename R, int W, int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<E, R> p)
 {
     constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS;
     __shared__ float slots[2][ROWS][W];
     const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (W * WAVE));
-    const RowPlace<CHUNKS, V> place(p.channels, threadIdx.x % (W * WAVE), W * WAVE);
-    float w1[CHUNKS][V], scale[CHUNKS][V], w2[CHUNKS][V];
-    load_weight<CHUNKS, V>(place, p.post_weight, w1);
-    load_weight<CHUNKS, V>(place, p.scale, scale);
-    load_weight<CHUNKS, V>(place, p.pre_weight, w2);
-    const float mean = 1.0f / (float)p.channels;
-    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += gridDim.x * ROWS) {
-        const bool on = base + which < p.rows;
-        const uint32_t row = on ? base + which : p.rows - 1;
+    const RowPlace<CHUNKS, V, WHOLE> w(p.channels, threadIdx.x % (W * WAVE), W * WAVE);
+    const bool gated = p.gate.data != nullptr;
+    Pack<E, V> raw_y[CHUNKS], raw_g[CHUNKS];
+    Pack<R, V> raw_r[CHUNKS];
+    auto load = [&](uint32_t row) {
         const int t = (int)(row / p.n), i = (int)(row % p.n);
-        float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V];
-        load_chunks<CHUNKS, V>(place, p.y.at(t, i), y);
-        load_chunks<CHUNKS, V>(place, p.residual.at(t, i), r);
-        if (p.gate.data) load_chunks<CHUNKS, V>(place, p.gate.at(t, i), g);
+        fetch(w, p.y.at(t, i), raw_y);
+        fetch(w, p.residual.at(t, i), raw_r);
+        if (gated) fetch(w, p.gate.at(t, i), raw_g);
+    };
+    const uint32_t first = blockIdx.x * ROWS + which, stride = gridDim.x * ROWS, last = p.rows - 1;
+    load(first < last ? first : last);
+    float w1[CHUNKS][V], scale[CHUNKS][V], w2[CHUNKS][V];
+    load_weight(w, p.post_weight, w1);
+    load_weight(w, p.scale, scale);
+    load_weight(w, p.pre_weight, w2);
+    const float mean = 1.0f / (float)p.channels;
+    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += stride) {
+        const uint32_t row = base + which;
+        float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V] = {};
+        expand(w, raw_y, y);
+        expand(w, raw_r, r);
+        if (gated) expand(w, raw_g, g);
+        if (base + stride < p.rows) load(row + stride < last ? row + stride : last);
         float root = 1.0f;
         if (p.post_weight) {
             float s = 0.0f;
@@ -138,48 +198,65 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                float branch = y[c][j] * root * w1[c][j] * scale[c][j];
-                if (p.gate.data) branch *= gate_value(g[c][j], p.gate_act);
-                r[c][j] += branch;
-                if (j < place.count[c]) s = __builtin_fmaf(r[c][j], r[c][j], s);
+                const float act = gate_value(g[c][j], p.gate_act);
+                r[c][j] = __builtin_fmaf(y[c][j] * root * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
+                s = __builtin_fmaf(r[c][j], r[c][j], s);
             }
         root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
-        if (on) {
-            store_chunks<CHUNKS, V>(place, p.out.at(t, i), r);
+        // the next row's values, waited for in front of the stores: behind them the wait would be for those too
+        pin(raw_y);
+        pin(raw_r);
+        if (gated) pin(raw_g);
+        if (row < p.rows) {
+            const int t = (int)(row / p.n), i = (int)(row % p.n);
+            put(w, p.out.at(t, i), r);
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
                 for (int j = 0; j < V; ++j) r[c][j] = r[c][j] * root * w2[c][j];
-            store_chunks<CHUNKS, V>(place, p.u.at(t, i), r);
+            put(w, p.u.at(t, i), r);
         }
         if (W > 1) __syncthreads();
     }
 }
 
-template <typename E, typename R, int W, int CHUNKS>
+template <typename E, typename R, int W, int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const NormParams<E, R> p)
 {
     constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS, THREADS = RowBlock<W>::THREADS;
     __shared__ float slots[4][ROWS][W];
     __shared__ float sums[ROWS > 1 ? THREADS * CHUNKS * V : 1];
     const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (W * WAVE)), side = threadIdx.x % (W * WAVE);
-    const RowPlace<CHUNKS, V> place(p.channels, side, W * WAVE);
+    const RowPlace<CHUNKS, V, WHOLE> w(p.channels, side, W * WAVE);
+    const bool gated = p.gate.data != nullptr, through = p.dout.data != nullptr;
+    Pack<E, V> raw_y[CHUNKS], raw_g[CHUNKS], raw_du[CHUNKS];
+    Pack<R, V> raw_r[CHUNKS], raw_dr[CHUNKS];
+    auto load = [&](uint32_t row) {
+        const int t = (int)(row / p.n), i = (int)(row % p.n);
+        fetch(w, p.y.at(t, i), raw_y);
+        fetch(w, p.residual.at(t, i), raw_r);
+        if (gated) fetch(w, p.gate.at(t, i), raw_g);
+        fetch(w, p.du.at(t, i), raw_du);
+        if (through) fetch(w, p.dout.at(t, i), raw_dr);
+    };
+    const uint32_t first = blockIdx.x * ROWS + which, stride = gridDim.x * ROWS, last = p.rows - 1;
+    load(first < last ? first : last);
     float w1[CHUNKS][V], scale[CHUNKS][V], w2[CHUNKS][V];
-    load_weight<CHUNKS, V>(place, p.post_weight, w1);
-    load_weight<CHUNKS, V>(place, p.scale, scale);
-    load_weight<CHUNKS, V>(place, p.pre_weight, w2);
+    load_weight(w, p.post_weight, w1);
+    load_weight(w, p.scale, scale);
+    load_weight(w, p.pre_weight, w2);
     float d1[CHUNKS][V] = {}, ds[CHUNKS][V] = {}, d2[CHUNKS][V] = {};
     const float mean = 1.0f / (float)p.channels;
-    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += gridDim.x * ROWS) {
-        const bool on = base + which < p.rows;
-        const uint32_t row = on ? base + which : p.rows - 1;
-        const int t = (int)(row / p.n), i = (int)(row % p.n);
-        float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V], du[CHUNKS][V], dr[CHUNKS][V];
-        load_chunks<CHUNKS, V>(place, p.y.at(t, i), y);
-        load_chunks<CHUNKS, V>(place, p.residual.at(t, i), r);
-        if (p.gate.data) load_chunks<CHUNKS, V>(place, p.gate.at(t, i), g);
-        load_chunks<CHUNKS, V>(place, p.du.at(t, i), du);
-        if (p.dout.data) load_chunks<CHUNKS, V>(place, p.dout.at(t, i), dr);
+    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += stride) {
+        const uint32_t row = base + which;
+        const float on = row < p.rows ? 1.0f : 0.0f;       // a row that is none adds nothing to the weights' gradients
+        float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V] = {}, du[CHUNKS][V], dr[CHUNKS][V] = {};
+        expand(w, raw_y, y);
+        expand(w, raw_r, r);
+        if (gated) expand(w, raw_g, g);
+        expand(w, raw_du, du);
+        if (through) expand(w, raw_dr, dr);
+        if (base + stride < p.rows) load(row + stride < last ? row + stride : last);
         float root_y = 1.0f;
         if (p.post_weight) {
             float s = 0.0f;
@@ -196,10 +273,9 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 y[c][j] *= root_y;                                   // from here on without its scale
-                float branch = y[c][j] * w1[c][j] * scale[c][j];
-                if (p.gate.data) branch *= gate_value(g[c][j], p.gate_act);
-                r[c][j] += branch;
-                if (j < place.count[c]) s = __builtin_fmaf(r[c][j], r[c][j], s);
+                const float act = gate_value(g[c][j], p.gate_act);
+                r[c][j] = __builtin_fmaf(y[c][j] * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
+                s = __builtin_fmaf(r[c][j], r[c][j], s);
             }
         const float root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
 #pragma unroll
@@ -207,9 +283,9 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 r[c][j] *= root;
-                if (on && j < place.count[c]) d2[c][j] = __builtin_fmaf(du[c][j], r[c][j], d2[c][j]);
+                d2[c][j] = __builtin_fmaf(du[c][j] * on, r[c][j], d2[c][j]);
                 du[c][j] *= w2[c][j];
-                if (j < place.count[c]) m = __builtin_fmaf(du[c][j], r[c][j], m);
+                m = __builtin_fmaf(du[c][j], r[c][j], m);
             }
         m = row_sum<W>(m, slots[2][which]) * mean;
         float q = 0.0f;
@@ -217,21 +293,16 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = __builtin_fmaf(root, off_axis<W>(p, du[c][j], r[c][j], m, root), p.dout.data ? dr[c][j] : 0.0f);
+                const float d = __builtin_fmaf(root, off_axis<W>(p, du[c][j], r[c][j], m, root), dr[c][j]);
                 dr[c][j] = d;
-                const float act = p.gate.data ? gate_value(g[c][j], p.gate_act) : 1.0f;
-                const float v = y[c][j] * w1[c][j];
-                if (on && j < place.count[c]) ds[c][j] = __builtin_fmaf(d * v, act, ds[c][j]);
-                const float dv = d * scale[c][j] * act;
-                if (p.gate.data) g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
-                if (on && j < place.count[c]) d1[c][j] = __builtin_fmaf(dv, y[c][j], d1[c][j]);
+                const float value = gate_value(g[c][j], p.gate_act), act = gated ? value : 1.0f;
+                const float v = y[c][j] * w1[c][j], dv = d * scale[c][j] * act;
+                ds[c][j] = __builtin_fmaf(d * v * on, act, ds[c][j]);
+                g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
+                d1[c][j] = __builtin_fmaf(dv * on, y[c][j], d1[c][j]);
                 du[c][j] = dv * w1[c][j];
-                if (j < place.count[c]) q = __builtin_fmaf(du[c][j], y[c][j], q);
+                q = __builtin_fmaf(du[c][j], y[c][j], q);
             }
-        if (on) {
-            store_chunks<CHUNKS, V>(place, p.dresidual.at(t, i), dr);
-            if (p.gate.data) store_chunks<CHUNKS, V>(place, p.dgate.at(t, i), g);
-        }
         if (p.post_weight) {
             q = row_sum<W>(q, slots[3][which]) * mean;
 #pragma unroll
@@ -239,15 +310,26 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
                 for (int j = 0; j < V; ++j) du[c][j] = root_y * off_axis<W>(p, du[c][j], y[c][j], q, root_y);
         }
-        if (on) store_chunks<CHUNKS, V>(place, p.dy.at(t, i), du);
+        // the next row's values, waited for in front of the stores: behind them the wait would be for those too
+        pin(raw_y);
+        pin(raw_r);
+        if (gated) pin(raw_g);
+        pin(raw_du);
+        if (through) pin(raw_dr);
+        if (row < p.rows) {
+            const int t = (int)(row / p.n), i = (int)(row % p.n);
+            put(w, p.dresidual.at(t, i), dr);
+            if (gated) put(w, p.dgate.at(t, i), g);
+            put(w, p.dy.at(t, i), du);
+        }
         if (W > 1) __syncthreads();
     }
     if (p.part == nullptr) return;
     // one partial row per block and weight; the rows that a block works on at once are added up in LDS
-    auto put = [&](int weight, const float (&v)[CHUNKS][V]) {
+    auto sum_up = [&](int weight, const float (&v)[CHUNKS][V]) {
         float* out = p.part + ((int64_t)blockIdx.x * 3 + weight) * p.channels;
         if constexpr (ROWS == 1) {
-            store_chunks<CHUNKS, V>(place, out, v);
+            put(w, out, v);
         } else {
             __syncthreads();
 #pragma unroll
@@ -265,13 +347,13 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
                         for (int k = 0; k < ROWS; ++k) total[c][j] += sums[(c * V + j) * THREADS + k * (W * WAVE) + side];
                     }
-                store_chunks<CHUNKS, V>(place, out, total);
+                put(w, out, total);
             }
         }
     };
-    put(0, d1);
-    put(1, ds);
-    put(2, d2);
+    sum_up(0, d1);
+    sum_up(1, ds);
+    sum_up(2, d2);
 }
 
 struct PutNorm {
@@ -329,11 +411,11 @@ template <typename E, typename R> static NormParams<E, R> norm_params(const craf
     return p;
 }
 
-// Wavefronts per row: as few (1, 2, 4, 8) as hold it with 16 values per lane.
+// Wavefronts per row: as few (1, 2, 4, 8) as hold it with 8 values per lane; beyond 4,096 values eight with 16.
 static int row_waves(int channels)
 {
     int w = 1;
-    while (w < 8 && w * WAVE * 16 < channels) w *= 2;
+    while (w < 8 && w * WAVE * 8 < channels) w *= 2;
     return w;
 }
 static int row_threads(int w) { return w * WAVE > 256 ? w * WAVE : 256; }
@@ -348,7 +430,7 @@ static unsigned row_blocks(const craftax_norm_args* a, int waves_per_simd)
 }
 constexpr int NORM_WAVES = 8, NORM_BACK_WAVES = 4;
 
-// calls f with the element types, the wavefronts per row and the chunks per lane as constants
+// calls f with the element types, the wavefronts per row, the chunks per lane and whether they fill it as constants
 template <typename F> static void with_row(const craftax_norm_args* a, F&& f)
 {
     const int w = row_waves(a->channels);
@@ -357,9 +439,14 @@ template <typename F> static void with_row(const craftax_norm_args* a, F&& f)
         constexpr int V = 16 / sizeof(E);
         auto chunks = [&](auto r, auto wc) {
             constexpr int W = decltype(wc)::value;
-            if (a->channels <= W * WAVE * V) f(e, r, wc, std::integral_constant<int, 1>{});
-            else if (V == 8 || a->channels <= W * WAVE * V * 2) f(e, r, wc, std::integral_constant<int, 2>{});
-            else f(e, r, wc, std::integral_constant<int, V == 8 ? 2 : 4>{});
+            auto whole = [&](auto count) {
+                if (a->channels == W * WAVE * V * decltype(count)::value) f(e, r, wc, count, std::true_type{});
+                else f(e, r, wc, count, std::false_type{});
+            };
+            constexpr int EIGHT = 8 / V;          // chunks of eight values
+            if (V < 8 && a->channels <= W * WAVE * V) whole(std::integral_constant<int, 1>{});
+            else if (W < 8 || a->channels <= W * WAVE * 8) whole(std::integral_constant<int, EIGHT>{});
+            else if constexpr (W == 8) whole(std::integral_constant<int, 2 * EIGHT>{});
         };
         auto waves = [&](auto r) {
             if (w == 1) chunks(r, std::integral_constant<int, 1>{});
@@ -375,11 +462,11 @@ template <typename F> static void with_row(const craftax_norm_args* a, F&& f)
 int norm(const craftax_norm_args* a, void* stream, const char** why)
 {
     if (int rc = norm_check(a, false, why)) return rc;
-    with_row(a, [&](auto e, auto r, auto w, auto chunks) {
+    with_row(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
         using E = decltype(e);
         using R = decltype(r);
         constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
-        hipLaunchKernelGGL((k_norm<E, R, W, C>), dim3(row_blocks(a, NORM_WAVES)), dim3(RowBlock<W>::THREADS), 0, (hipStream_t)stream,
+        hipLaunchKernelGGL((k_norm<E, R, W, C, decltype(whole)::value>), dim3(row_blocks(a, NORM_WAVES)), dim3(RowBlock<W>::THREADS), 0, (hipStream_t)stream,
                            (norm_params<E, R>(a)));
     });
     return launched(why);
@@ -401,13 +488,13 @@ int norm_backward(const craftax_norm_args* a, void* stream, const char** why)
     if (a->workspace_bytes < need) return refuse(CRAFTAX_E_COUNT, "workspace smaller than craftax_residual_norm_workspace_bytes", why);
     const unsigned blocks = row_blocks(a, NORM_BACK_WAVES);
     const hipStream_t st = (hipStream_t)stream;
-    with_row(a, [&](auto e, auto r, auto w, auto chunks) {
+    with_row(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
         using E = decltype(e);
         using R = decltype(r);
         constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
         NormParams<E, R> p = norm_params<E, R>(a);
         p.part = need ? static_cast<float*>(a->workspace) : nullptr;
-        hipLaunchKernelGGL((k_norm_backward<E, R, W, C>), dim3(blocks), dim3(RowBlock<W>::THREADS), 0, st, p);
+        hipLaunchKernelGGL((k_norm_backward<E, R, W, C, decltype(whole)::value>), dim3(blocks), dim3(RowBlock<W>::THREADS), 0, st, p);
     });
     if (int rc = launched(why)) return rc;
     if (need)
