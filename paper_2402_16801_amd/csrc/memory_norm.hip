@@ -70,9 +70,10 @@ template <int W> struct RowBlock {
     static constexpr int ROWS = THREADS / (W * WAVE);      // rows a block works on at once
 };
 
-// Where a lane's chunks of V values lie in a row.  A chunk that passes the end of the row is moved back to end with it, and
-// its first `old` values are not this lane's (those of a lane with nothing left: all V).  Rows shorter than V are read
-// value by value.
+// Where a lane's chunks of V values lie in a row.  A chunk that passes the end of the row is moved back to end with it:
+// its first `old` values are another lane's too (those of a lane with nothing left: all V).  They are computed and stored
+// like the other lane's, bit for bit, and only left out of the sums.  Rows shorter than V are read and written value
+// by value.
 template <int CHUNKS, int V, bool WHOLE> struct RowPlace {
     int at[CHUNKS], old[CHUNKS], channels;
     __device__ __forceinline__ RowPlace(int n, int side, int width) : channels(n)
@@ -83,7 +84,6 @@ template <int CHUNKS, int V, bool WHOLE> struct RowPlace {
             at[c] = WHOLE || first <= last ? first : (last < 0 ? 0 : last);
             const int gone = first - at[c];
             old[c] = WHOLE ? 0 : (gone < V ? gone : V);
-            if (!WHOLE && last < 0) old[c] = first == 0 ? 0 : V;
         }
     }
     __device__ __forceinline__ bool mine(int c, int j) const
@@ -105,31 +105,40 @@ __device__ __forceinline__ void fetch(const RowPlace<CHUNKS, V, WHOLE>& w, const
             for (int j = 0; j < V; ++j) q[c].v[j] = p[j < w.channels ? j : 0];
     }
 }
-// the lane's own values, 0 elsewhere
-template <typename P, int CHUNKS, int V, bool WHOLE>
-__device__ __forceinline__ void expand(const RowPlace<CHUNKS, V, WHOLE>& w, const Pack<P, V> (&q)[CHUNKS], float (&v)[CHUNKS][V])
+template <typename P, int CHUNKS, int V>
+__device__ __forceinline__ void expand(const Pack<P, V> (&q)[CHUNKS], float (&v)[CHUNKS][V])
 {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[c][j] = w.mine(c, j) ? Elem<P>::up(q[c].v[j]) : 0.0f;
+        for (int j = 0; j < V; ++j) v[c][j] = Elem<P>::up(q[c].v[j]);
 }
 template <typename P, int CHUNKS, int V, bool WHOLE>
 __device__ __forceinline__ void put(const RowPlace<CHUNKS, V, WHOLE>& w, P* p, const float (&v)[CHUNKS][V])
 {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        if (WHOLE || (w.old[c] == 0 && w.channels >= V)) {
+        if (WHOLE || w.channels >= V) {
             Pack<P, V> q;
 #pragma unroll
             for (int j = 0; j < V; ++j) q.v[j] = Elem<P>::down(v[c][j]);
-            *reinterpret_cast<Pack<P, V>*>(p + w.at[c]) = q;
+            if (WHOLE || w.old[c] < V) *reinterpret_cast<Pack<P, V>*>(p + w.at[c]) = q;
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (w.mine(c, j)) p[w.at[c] + j] = Elem<P>::down(v[c][j]);
+                if (w.mine(c, j)) p[j] = Elem<P>::down(v[c][j]);
         }
     }
+}
+// sums over rows: a value belongs to one lane
+template <int CHUNKS, int V, bool WHOLE>
+__device__ __forceinline__ void put_mine(const RowPlace<CHUNKS, V, WHOLE>& w, float* p, const float (&v)[CHUNKS][V])
+{
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (w.mine(c, j)) p[w.at[c] + j] = v[c][j];
 }
 template <int CHUNKS, int V, bool WHOLE>
 __device__ __forceinline__ void load_weight(const RowPlace<CHUNKS, V, WHOLE>& w, const float* p, float (&v)[CHUNKS][V])
@@ -137,7 +146,7 @@ __device__ __forceinline__ void load_weight(const RowPlace<CHUNKS, V, WHOLE>& w,
     Pack<float, V> q[CHUNKS];
     if (p) {
         fetch(w, p, q);
-        expand(w, q, v);
+        expand(q, v);
         return;
     }
 #pragma unroll
@@ -176,13 +185,18 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
     load_weight(w, p.post_weight, w1);
     load_weight(w, p.scale, scale);
     load_weight(w, p.pre_weight, w2);
+    float share[CHUNKS][V];                    // 1 where a value counts in this lane, else 0
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < V; ++j) share[c][j] = w.mine(c, j) ? 1.0f : 0.0f;
     const float mean = 1.0f / (float)p.channels;
     for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += stride) {
         const uint32_t row = base + which;
         float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V] = {};
-        expand(w, raw_y, y);
-        expand(w, raw_r, r);
-        if (gated) expand(w, raw_g, g);
+        expand(raw_y, y);
+        expand(raw_r, r);
+        if (gated) expand(raw_g, g);
         if (base + stride < p.rows) load(row + stride < last ? row + stride : last);
         float root = 1.0f;
         if (p.post_weight) {
@@ -190,7 +204,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = __builtin_fmaf(y[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = __builtin_fmaf(WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
             root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         float s = 0.0f;
@@ -200,7 +214,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
             for (int j = 0; j < V; ++j) {
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * root * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = __builtin_fmaf(r[c][j], r[c][j], s);
+                s = __builtin_fmaf(WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
             }
         root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
         // the next row's values, waited for in front of the stores: behind them the wait would be for those too
@@ -224,6 +238,7 @@ template <typename E, typename R, int W, int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const NormParams<E, R> p)
 {
     constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS, THREADS = RowBlock<W>::THREADS;
+    constexpr bool EARLY = CHUNKS * V <= 8;        // the next row is read while one is computed, where the registers hold both
     __shared__ float slots[4][ROWS][W];
     __shared__ float sums[ROWS > 1 ? THREADS * CHUNKS * V : 1];
     const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (W * WAVE)), side = threadIdx.x % (W * WAVE);
@@ -245,25 +260,31 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
     load_weight(w, p.post_weight, w1);
     load_weight(w, p.scale, scale);
     load_weight(w, p.pre_weight, w2);
+    float share[CHUNKS][V];                    // 1 where a value counts in this lane, else 0
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < V; ++j) share[c][j] = w.mine(c, j) ? 1.0f : 0.0f;
     float d1[CHUNKS][V] = {}, ds[CHUNKS][V] = {}, d2[CHUNKS][V] = {};
     const float mean = 1.0f / (float)p.channels;
     for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += stride) {
         const uint32_t row = base + which;
         const float on = row < p.rows ? 1.0f : 0.0f;       // a row that is none adds nothing to the weights' gradients
+        if (!EARLY && base != blockIdx.x * ROWS) load(row < last ? row : last);
         float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V] = {}, du[CHUNKS][V], dr[CHUNKS][V] = {};
-        expand(w, raw_y, y);
-        expand(w, raw_r, r);
-        if (gated) expand(w, raw_g, g);
-        expand(w, raw_du, du);
-        if (through) expand(w, raw_dr, dr);
-        if (base + stride < p.rows) load(row + stride < last ? row + stride : last);
+        expand(raw_y, y);
+        expand(raw_r, r);
+        if (gated) expand(raw_g, g);
+        expand(raw_du, du);
+        if (through) expand(raw_dr, dr);
+        if (EARLY && base + stride < p.rows) load(row + stride < last ? row + stride : last);
         float root_y = 1.0f;
         if (p.post_weight) {
             float s = 0.0f;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = __builtin_fmaf(y[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = __builtin_fmaf(WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
             root_y = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         // out again, its root, and the sum over the row of (du w2) (out root)
@@ -275,7 +296,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 y[c][j] *= root_y;                                   // from here on without its scale
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = __builtin_fmaf(r[c][j], r[c][j], s);
+                s = __builtin_fmaf(WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
             }
         const float root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
 #pragma unroll
@@ -285,7 +306,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 r[c][j] *= root;
                 d2[c][j] = __builtin_fmaf(du[c][j] * on, r[c][j], d2[c][j]);
                 du[c][j] *= w2[c][j];
-                m = __builtin_fmaf(du[c][j], r[c][j], m);
+                m = __builtin_fmaf(WHOLE ? du[c][j] : du[c][j] * share[c][j], r[c][j], m);
             }
         m = row_sum<W>(m, slots[2][which]) * mean;
         float q = 0.0f;
@@ -301,7 +322,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
                 d1[c][j] = __builtin_fmaf(dv * on, y[c][j], d1[c][j]);
                 du[c][j] = dv * w1[c][j];
-                q = __builtin_fmaf(du[c][j], y[c][j], q);
+                q = __builtin_fmaf(WHOLE ? du[c][j] : du[c][j] * share[c][j], y[c][j], q);
             }
         if (p.post_weight) {
             q = row_sum<W>(q, slots[3][which]) * mean;
@@ -310,12 +331,14 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
                 for (int j = 0; j < V; ++j) du[c][j] = root_y * off_axis<W>(p, du[c][j], y[c][j], q, root_y);
         }
-        // the next row's values, waited for in front of the stores: behind them the wait would be for those too
-        pin(raw_y);
-        pin(raw_r);
-        if (gated) pin(raw_g);
-        pin(raw_du);
-        if (through) pin(raw_dr);
+        if (EARLY) {
+            // the next row's values, waited for in front of the stores: behind them the wait would be for those too
+            pin(raw_y);
+            pin(raw_r);
+            if (gated) pin(raw_g);
+            pin(raw_du);
+            if (through) pin(raw_dr);
+        }
         if (row < p.rows) {
             const int t = (int)(row / p.n), i = (int)(row % p.n);
             put(w, p.dresidual.at(t, i), dr);
@@ -329,7 +352,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
     auto sum_up = [&](int weight, const float (&v)[CHUNKS][V]) {
         float* out = p.part + ((int64_t)blockIdx.x * 3 + weight) * p.channels;
         if constexpr (ROWS == 1) {
-            put(w, out, v);
+            put_mine(w, out, v);
         } else {
             __syncthreads();
 #pragma unroll
@@ -347,7 +370,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
                         for (int k = 0; k < ROWS; ++k) total[c][j] += sums[(c * V + j) * THREADS + k * (W * WAVE) + side];
                     }
-                put(w, out, total);
+                put_mine(w, out, total);
             }
         }
     };
@@ -370,6 +393,7 @@ struct PutNorm {
 namespace host {
 
 constexpr int NORM_CHANNELS = 8192;
+constexpr int NORM_WAVES = 6, NORM_BACK_WAVES = 2;       // wavefronts per SIMD that are launched at most: those that are there at once
 
 static int norm_check(const craftax_norm_args* a, bool backward, const char** why)
 {
@@ -411,29 +435,30 @@ template <typename E, typename R> static NormParams<E, R> norm_params(const craf
     return p;
 }
 
-// Wavefronts per row: as few (1, 2, 4, 8) as hold it with 8 values per lane; beyond 4,096 values eight with 16.
-static int row_waves(int channels)
+// Wavefronts per row: as few (1, 2, 4, 8) as hold it with 16 values per lane, or with 8 in the backward pass, which holds five
+// rows and three gradients (beyond 4,096 values 16 there too).
+static int row_waves(int channels, bool backward)
 {
     int w = 1;
-    while (w < 8 && w * WAVE * 8 < channels) w *= 2;
+    while (w < 8 && w * WAVE * (backward ? 8 : 16) < channels) w *= 2;
     return w;
 }
 static int row_threads(int w) { return w * WAVE > 256 ? w * WAVE : 256; }
 
 // Blocks: all that the chip holds at once, then on to further rows.
-static unsigned row_blocks(const craftax_norm_args* a, int waves_per_simd)
+static unsigned row_blocks(const craftax_norm_args* a, bool backward)
 {
-    const int w = row_waves(a->channels), threads = row_threads(w);
+    const int waves_per_simd = backward ? NORM_BACK_WAVES : NORM_WAVES;
+    const int w = row_waves(a->channels, backward), threads = row_threads(w);
     const int64_t need = ceil_div((int64_t)a->steps * a->n, threads / (w * WAVE));
     const int64_t most = (int64_t)CHIP_SIMDS * waves_per_simd * WAVE / threads;
     return (unsigned)(need < most ? need : most);
 }
-constexpr int NORM_WAVES = 8, NORM_BACK_WAVES = 4;
 
 // calls f with the element types, the wavefronts per row, the chunks per lane and whether they fill it as constants
-template <typename F> static void with_row(const craftax_norm_args* a, F&& f)
+template <bool BACKWARD, typename F> static void with_row(const craftax_norm_args* a, F&& f)
 {
-    const int w = row_waves(a->channels);
+    const int w = row_waves(a->channels, BACKWARD);
     with_type(a->dtype, [&](auto e) {
         using E = decltype(e);
         constexpr int V = 16 / sizeof(E);
@@ -445,8 +470,8 @@ template <typename F> static void with_row(const craftax_norm_args* a, F&& f)
             };
             constexpr int EIGHT = 8 / V;          // chunks of eight values
             if (V < 8 && a->channels <= W * WAVE * V) whole(std::integral_constant<int, 1>{});
-            else if (W < 8 || a->channels <= W * WAVE * 8) whole(std::integral_constant<int, EIGHT>{});
-            else if constexpr (W == 8) whole(std::integral_constant<int, 2 * EIGHT>{});
+            else if ((BACKWARD && W < 8) || a->channels <= W * WAVE * 8) whole(std::integral_constant<int, EIGHT>{});
+            else if constexpr (!BACKWARD || W == 8) whole(std::integral_constant<int, 2 * EIGHT>{});
         };
         auto waves = [&](auto r) {
             if (w == 1) chunks(r, std::integral_constant<int, 1>{});
@@ -462,11 +487,11 @@ template <typename F> static void with_row(const craftax_norm_args* a, F&& f)
 int norm(const craftax_norm_args* a, void* stream, const char** why)
 {
     if (int rc = norm_check(a, false, why)) return rc;
-    with_row(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
+    with_row<false>(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
         using E = decltype(e);
         using R = decltype(r);
         constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
-        hipLaunchKernelGGL((k_norm<E, R, W, C, decltype(whole)::value>), dim3(row_blocks(a, NORM_WAVES)), dim3(RowBlock<W>::THREADS), 0, (hipStream_t)stream,
+        hipLaunchKernelGGL((k_norm<E, R, W, C, decltype(whole)::value>), dim3(row_blocks(a, false)), dim3(RowBlock<W>::THREADS), 0, (hipStream_t)stream,
                            (norm_params<E, R>(a)));
     });
     return launched(why);
@@ -476,7 +501,7 @@ size_t norm_workspace_bytes(const craftax_norm_args* a)
 {
     if (!a || a->steps < 1 || a->n < 1 || a->channels < 1 || a->channels > NORM_CHANNELS) return 0;
     if (!a->dpost_weight && !a->dscale && !a->dpre_weight) return 0;
-    return round256((size_t)row_blocks(a, NORM_BACK_WAVES) * 3 * a->channels * sizeof(float));
+    return round256((size_t)row_blocks(a, true) * 3 * a->channels * sizeof(float));
 }
 
 int norm_backward(const craftax_norm_args* a, void* stream, const char** why)
@@ -486,9 +511,9 @@ int norm_backward(const craftax_norm_args* a, void* stream, const char** why)
     if (need && !a->workspace) return refuse(CRAFTAX_E_NULL, "workspace is NULL", why);
     if (need && !aligned(a->workspace, 256)) return refuse(CRAFTAX_E_ALIGN, "workspace must be 256-byte aligned", why);
     if (a->workspace_bytes < need) return refuse(CRAFTAX_E_COUNT, "workspace smaller than craftax_residual_norm_workspace_bytes", why);
-    const unsigned blocks = row_blocks(a, NORM_BACK_WAVES);
+    const unsigned blocks = row_blocks(a, true);
     const hipStream_t st = (hipStream_t)stream;
-    with_row(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
+    with_row<true>(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
         using E = decltype(e);
         using R = decltype(r);
         constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
