@@ -70,32 +70,33 @@ template <int W> struct RowBlock {
     static constexpr int ROWS = THREADS / (W * WAVE);      // rows a block works on at once
 };
 
-// Where a lane's chunks of V values lie in a row.  A chunk that passes the end of the row is moved back to end with it:
-// its first `old` values are another lane's too (those of a lane with nothing left: all V).  They are computed and stored
-// like the other lane's, bit for bit, and only left out of the sums.  Rows shorter than V are read and written value
-// by value.
-template <int CHUNKS, int V, bool WHOLE> struct RowPlace {
+// How rows fit the lanes' chunks of V values.  WHOLE: exactly.  TAIL: a chunk that passes the end of the row is moved back to
+// end with it: its first `old` values are another lane's too (those of a lane with nothing left: all V).  They are computed
+// and stored like the other lane's, bit for bit, and only left out of the sums.  SHORT: rows of fewer than V values are
+// read and written value by value, by one lane.
+enum Fit { WHOLE, TAIL, SHORT };
+template <int CHUNKS, int V, Fit FIT> struct RowPlace {
     int at[CHUNKS], old[CHUNKS], channels;
     __device__ __forceinline__ RowPlace(int n, int side, int width) : channels(n)
     {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int first = (c * width + side) * V, last = n - V;
-            at[c] = WHOLE || first <= last ? first : (last < 0 ? 0 : last);
+            const int first = (c * width + side) * V, last = FIT == SHORT ? 0 : n - V;
+            at[c] = FIT == WHOLE || first <= last ? first : last;
             const int gone = first - at[c];
-            old[c] = WHOLE ? 0 : (gone < V ? gone : V);
+            old[c] = FIT == WHOLE ? 0 : (gone < V ? gone : V);
         }
     }
     __device__ __forceinline__ bool mine(int c, int j) const
     {
-        return WHOLE || (j >= old[c] && (channels >= V || j < channels));
+        return FIT == WHOLE || (j >= old[c] && (FIT == TAIL || j < channels));
     }
 };
 
-template <typename P, int CHUNKS, int V, bool WHOLE>
-__device__ __forceinline__ void fetch(const RowPlace<CHUNKS, V, WHOLE>& w, const P* p, Pack<P, V> (&q)[CHUNKS])
+template <typename P, int CHUNKS, int V, Fit FIT>
+__device__ __forceinline__ void fetch(const RowPlace<CHUNKS, V, FIT>& w, const P* p, Pack<P, V> (&q)[CHUNKS])
 {
-    if (WHOLE || w.channels >= V) {
+    if (FIT != SHORT) {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) q[c] = *reinterpret_cast<const Pack<P, V>*>(p + w.at[c]);
     } else {
@@ -113,16 +114,16 @@ __device__ __forceinline__ void expand(const Pack<P, V> (&q)[CHUNKS], float (&v)
 #pragma unroll
         for (int j = 0; j < V; ++j) v[c][j] = Elem<P>::up(q[c].v[j]);
 }
-template <typename P, int CHUNKS, int V, bool WHOLE>
-__device__ __forceinline__ void put(const RowPlace<CHUNKS, V, WHOLE>& w, P* p, const float (&v)[CHUNKS][V])
+template <typename P, int CHUNKS, int V, Fit FIT>
+__device__ __forceinline__ void put(const RowPlace<CHUNKS, V, FIT>& w, P* p, const float (&v)[CHUNKS][V])
 {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        if (WHOLE || w.channels >= V) {
+        if (FIT != SHORT) {
             Pack<P, V> q;
 #pragma unroll
             for (int j = 0; j < V; ++j) q.v[j] = Elem<P>::down(v[c][j]);
-            if (WHOLE || w.old[c] < V) *reinterpret_cast<Pack<P, V>*>(p + w.at[c]) = q;
+            if (FIT == WHOLE || w.old[c] < V) *reinterpret_cast<Pack<P, V>*>(p + w.at[c]) = q;
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)
@@ -131,8 +132,8 @@ __device__ __forceinline__ void put(const RowPlace<CHUNKS, V, WHOLE>& w, P* p, c
     }
 }
 // sums over rows: a value belongs to one lane
-template <int CHUNKS, int V, bool WHOLE>
-__device__ __forceinline__ void put_mine(const RowPlace<CHUNKS, V, WHOLE>& w, float* p, const float (&v)[CHUNKS][V])
+template <int CHUNKS, int V, Fit FIT>
+__device__ __forceinline__ void put_mine(const RowPlace<CHUNKS, V, FIT>& w, float* p, const float (&v)[CHUNKS][V])
 {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
@@ -140,8 +141,8 @@ __device__ __forceinline__ void put_mine(const RowPlace<CHUNKS, V, WHOLE>& w, fl
         for (int j = 0; j < V; ++j)
             if (w.mine(c, j)) p[w.at[c] + j] = v[c][j];
 }
-template <int CHUNKS, int V, bool WHOLE>
-__device__ __forceinline__ void load_weight(const RowPlace<CHUNKS, V, WHOLE>& w, const float* p, float (&v)[CHUNKS][V])
+template <int CHUNKS, int V, Fit FIT>
+__device__ __forceinline__ void load_weight(const RowPlace<CHUNKS, V, FIT>& w, const float* p, float (&v)[CHUNKS][V])
 {
     Pack<float, V> q[CHUNKS];
     if (p) {
@@ -163,13 +164,13 @@ template <typename P, int CHUNKS, int V> __device__ __forceinline__ void pin(Pac
     __builtin_memcpy(q, words, sizeof(q));
 }
 
-template <typename E, typename R, int W, int CHUNKS, bool WHOLE>
+template <typename E, typename R, int W, int CHUNKS, Fit FIT>
 __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<E, R> p)
 {
     constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS;
     __shared__ float slots[2][ROWS][W];
     const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (W * WAVE));
-    const RowPlace<CHUNKS, V, WHOLE> w(p.channels, threadIdx.x % (W * WAVE), W * WAVE);
+    const RowPlace<CHUNKS, V, FIT> w(p.channels, threadIdx.x % (W * WAVE), W * WAVE);
     const bool gated = p.gate.data != nullptr;
     Pack<E, V> raw_y[CHUNKS], raw_g[CHUNKS];
     Pack<R, V> raw_r[CHUNKS];
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = __builtin_fmaf(WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = __builtin_fmaf(FIT == WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
             root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         float s = 0.0f;
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
             for (int j = 0; j < V; ++j) {
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * root * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = __builtin_fmaf(WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
+                s = __builtin_fmaf(FIT == WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
             }
         root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
         // the next row's values, waited for in front of the stores: behind them the wait would be for those too
@@ -234,28 +235,43 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
     }
 }
 
-template <typename E, typename R, int W, int CHUNKS, bool WHOLE>
+template <typename E, typename R, int W, int CHUNKS, Fit FIT>
 __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const NormParams<E, R> p)
 {
     constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS, THREADS = RowBlock<W>::THREADS;
-    constexpr bool EARLY = CHUNKS * V <= 8;        // the next row is read while one is computed, where the registers hold both
+    // Rows that are read ahead of the one that is computed, as many as the registers hold: two of 16-bit values (two
+    // wavefronts per SIMD with one row each under way are 10 MB, what the memory's latency takes at its rate), one of floats,
+    // none with 16 values per lane.
+    constexpr int AHEAD = CHUNKS * V > 8 ? 0 : sizeof(E) == 2 ? 2 : 1, SLOTS = AHEAD ? AHEAD : 1;
     __shared__ float slots[4][ROWS][W];
     __shared__ float sums[ROWS > 1 ? THREADS * CHUNKS * V : 1];
     const int which = __builtin_amdgcn_readfirstlane(threadIdx.x / (W * WAVE)), side = threadIdx.x % (W * WAVE);
-    const RowPlace<CHUNKS, V, WHOLE> w(p.channels, side, W * WAVE);
+    const RowPlace<CHUNKS, V, FIT> w(p.channels, side, W * WAVE);
     const bool gated = p.gate.data != nullptr, through = p.dout.data != nullptr;
-    Pack<E, V> raw_y[CHUNKS], raw_g[CHUNKS], raw_du[CHUNKS];
-    Pack<R, V> raw_r[CHUNKS], raw_dr[CHUNKS];
-    auto load = [&](uint32_t row) {
+    struct Raw {
+        Pack<E, V> y[CHUNKS], g[CHUNKS], du[CHUNKS];
+        Pack<R, V> r[CHUNKS], dr[CHUNKS];
+    } raw[SLOTS];
+    const uint32_t stride = gridDim.x * ROWS, last = p.rows - 1;
+    auto load = [&](Raw& q, uint32_t base) {
+        const uint32_t row = base + which < last ? base + which : last;
         const int t = (int)(row / p.n), i = (int)(row % p.n);
-        fetch(w, p.y.at(t, i), raw_y);
-        fetch(w, p.residual.at(t, i), raw_r);
-        if (gated) fetch(w, p.gate.at(t, i), raw_g);
-        fetch(w, p.du.at(t, i), raw_du);
-        if (through) fetch(w, p.dout.at(t, i), raw_dr);
+        fetch(w, p.y.at(t, i), q.y);
+        fetch(w, p.residual.at(t, i), q.r);
+        if (gated) fetch(w, p.gate.at(t, i), q.g);
+        fetch(w, p.du.at(t, i), q.du);
+        if (through) fetch(w, p.dout.at(t, i), q.dr);
     };
-    const uint32_t first = blockIdx.x * ROWS + which, stride = gridDim.x * ROWS, last = p.rows - 1;
-    load(first < last ? first : last);
+    // the values have arrived: waited for in front of stores, since behind them the wait would be for those too
+    auto arrive = [&](Raw& q) {
+        pin(q.y);
+        pin(q.r);
+        if (gated) pin(q.g);
+        pin(q.du);
+        if (through) pin(q.dr);
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) load(raw[k], blockIdx.x * ROWS + k * stride < p.rows ? blockIdx.x * ROWS + k * stride : last);
     float w1[CHUNKS][V], scale[CHUNKS][V], w2[CHUNKS][V];
     load_weight(w, p.post_weight, w1);
     load_weight(w, p.scale, scale);
@@ -267,24 +283,24 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
         for (int j = 0; j < V; ++j) share[c][j] = w.mine(c, j) ? 1.0f : 0.0f;
     float d1[CHUNKS][V] = {}, ds[CHUNKS][V] = {}, d2[CHUNKS][V] = {};
     const float mean = 1.0f / (float)p.channels;
-    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += stride) {
+    auto one = [&](uint32_t base, Raw& mine, Raw& next) {
         const uint32_t row = base + which;
         const float on = row < p.rows ? 1.0f : 0.0f;       // a row that is none adds nothing to the weights' gradients
-        if (!EARLY && base != blockIdx.x * ROWS) load(row < last ? row : last);
+        if (AHEAD == 0) load(mine, base);
         float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V] = {}, du[CHUNKS][V], dr[CHUNKS][V] = {};
-        expand(raw_y, y);
-        expand(raw_r, r);
-        if (gated) expand(raw_g, g);
-        expand(raw_du, du);
-        if (through) expand(raw_dr, dr);
-        if (EARLY && base + stride < p.rows) load(row + stride < last ? row + stride : last);
+        expand(mine.y, y);
+        expand(mine.r, r);
+        if (gated) expand(mine.g, g);
+        expand(mine.du, du);
+        if (through) expand(mine.dr, dr);
+        if (AHEAD > 0 && base + AHEAD * stride < p.rows) load(mine, base + AHEAD * stride);
         float root_y = 1.0f;
         if (p.post_weight) {
             float s = 0.0f;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = __builtin_fmaf(WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = __builtin_fmaf(FIT == WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
             root_y = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         // out again, its root, and the sum over the row of (du w2) (out root)
@@ -296,7 +312,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 y[c][j] *= root_y;                                   // from here on without its scale
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = __builtin_fmaf(WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
+                s = __builtin_fmaf(FIT == WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
             }
         const float root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
 #pragma unroll
@@ -306,7 +322,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 r[c][j] *= root;
                 d2[c][j] = __builtin_fmaf(du[c][j] * on, r[c][j], d2[c][j]);
                 du[c][j] *= w2[c][j];
-                m = __builtin_fmaf(WHOLE ? du[c][j] : du[c][j] * share[c][j], r[c][j], m);
+                m = __builtin_fmaf(FIT == WHOLE ? du[c][j] : du[c][j] * share[c][j], r[c][j], m);
             }
         m = row_sum<W>(m, slots[2][which]) * mean;
         float q = 0.0f;
@@ -322,7 +338,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
                 d1[c][j] = __builtin_fmaf(dv * on, y[c][j], d1[c][j]);
                 du[c][j] = dv * w1[c][j];
-                q = __builtin_fmaf(WHOLE ? du[c][j] : du[c][j] * share[c][j], y[c][j], q);
+                q = __builtin_fmaf(FIT == WHOLE ? du[c][j] : du[c][j] * share[c][j], y[c][j], q);
             }
         if (p.post_weight) {
             q = row_sum<W>(q, slots[3][which]) * mean;
@@ -331,14 +347,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
                 for (int j = 0; j < V; ++j) du[c][j] = root_y * off_axis<W>(p, du[c][j], y[c][j], q, root_y);
         }
-        if (EARLY) {
-            // the next row's values, waited for in front of the stores: behind them the wait would be for those too
-            pin(raw_y);
-            pin(raw_r);
-            if (gated) pin(raw_g);
-            pin(raw_du);
-            if (through) pin(raw_dr);
-        }
+        if (AHEAD > 0) arrive(next);
         if (row < p.rows) {
             const int t = (int)(row / p.n), i = (int)(row % p.n);
             put(w, p.dresidual.at(t, i), dr);
@@ -346,6 +355,11 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
             put(w, p.dy.at(t, i), du);
         }
         if (W > 1) __syncthreads();
+    };
+    for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += SLOTS * stride) {
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k)
+            if (base + k * stride < p.rows) one(base + k * stride, raw[k], raw[(k + 1) % SLOTS]);
     }
     if (p.part == nullptr) return;
     // one partial row per block and weight; the rows that a block works on at once are added up in LDS
@@ -455,7 +469,7 @@ static unsigned row_blocks(const craftax_norm_args* a, bool backward)
     return (unsigned)(need < most ? need : most);
 }
 
-// calls f with the element types, the wavefronts per row, the chunks per lane and whether they fill it as constants
+// calls f with the element types, the wavefronts per row, the chunks per lane and how they fit as constants
 template <bool BACKWARD, typename F> static void with_row(const craftax_norm_args* a, F&& f)
 {
     const int w = row_waves(a->channels, BACKWARD);
@@ -465,8 +479,10 @@ template <bool BACKWARD, typename F> static void with_row(const craftax_norm_arg
         auto chunks = [&](auto r, auto wc) {
             constexpr int W = decltype(wc)::value;
             auto whole = [&](auto count) {
-                if (a->channels == W * WAVE * V * decltype(count)::value) f(e, r, wc, count, std::true_type{});
-                else f(e, r, wc, count, std::false_type{});
+                constexpr int C = decltype(count)::value;
+                if (a->channels == W * WAVE * V * C) f(e, r, wc, count, std::integral_constant<Fit, WHOLE>{});
+                else if (a->channels >= V) f(e, r, wc, count, std::integral_constant<Fit, TAIL>{});
+                else if constexpr (W == 1 && C == 1) f(e, r, wc, count, std::integral_constant<Fit, SHORT>{});
             };
             constexpr int EIGHT = 8 / V;          // chunks of eight values
             if (V < 8 && a->channels <= W * WAVE * V) whole(std::integral_constant<int, 1>{});
@@ -487,11 +503,11 @@ template <bool BACKWARD, typename F> static void with_row(const craftax_norm_arg
 int norm(const craftax_norm_args* a, void* stream, const char** why)
 {
     if (int rc = norm_check(a, false, why)) return rc;
-    with_row<false>(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
+    with_row<false>(a, [&](auto e, auto r, auto w, auto chunks, auto fit) {
         using E = decltype(e);
         using R = decltype(r);
         constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
-        hipLaunchKernelGGL((k_norm<E, R, W, C, decltype(whole)::value>), dim3(row_blocks(a, false)), dim3(RowBlock<W>::THREADS), 0, (hipStream_t)stream,
+        hipLaunchKernelGGL((k_norm<E, R, W, C, decltype(fit)::value>), dim3(row_blocks(a, false)), dim3(RowBlock<W>::THREADS), 0, (hipStream_t)stream,
                            (norm_params<E, R>(a)));
     });
     return launched(why);
@@ -513,13 +529,13 @@ int norm_backward(const craftax_norm_args* a, void* stream, const char** why)
     if (a->workspace_bytes < need) return refuse(CRAFTAX_E_COUNT, "workspace smaller than craftax_residual_norm_workspace_bytes", why);
     const unsigned blocks = row_blocks(a, true);
     const hipStream_t st = (hipStream_t)stream;
-    with_row<true>(a, [&](auto e, auto r, auto w, auto chunks, auto whole) {
+    with_row<true>(a, [&](auto e, auto r, auto w, auto chunks, auto fit) {
         using E = decltype(e);
         using R = decltype(r);
         constexpr int W = decltype(w)::value, C = decltype(chunks)::value;
         NormParams<E, R> p = norm_params<E, R>(a);
         p.part = need ? static_cast<float*>(a->workspace) : nullptr;
-        hipLaunchKernelGGL((k_norm_backward<E, R, W, C, decltype(whole)::value>), dim3(blocks), dim3(RowBlock<W>::THREADS), 0, st, p);
+        hipLaunchKernelGGL((k_norm_backward<E, R, W, C, decltype(fit)::value>), dim3(blocks), dim3(RowBlock<W>::THREADS), 0, st, p);
     });
     if (int rc = launched(why)) return rc;
     if (need)
