@@ -382,7 +382,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_carry(const ScanParams<E>
     float* out = BACK ? p.dstate_in : p.state_out;
     if (in) load4(state_of<N>(in, p.channels, i, w), h);
     else zero(h);
-    constexpr int GO = 8;
+    constexpr int GO = 32;       // parts whose effects are loaded together: few wavefronts, so the trips to memory are what counts
     for (int q0 = 0; q0 < p.parts; q0 += GO) {
         float end[GO][4];
         float2 decay[GO];
@@ -709,7 +709,8 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
                 hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3(blocks), dim3(SCAN_THREADS), 0, st, p);
             }
             const dim3 grid((unsigned)((int64_t)(s.rows / p.parts) * a->groups * s.group_blocks), (unsigned)p.parts);
-            hipLaunchKernelGGL((k_scan_back<E, N>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
+            if (p.z.data) hipLaunchKernelGGL((k_scan_back<E, N, true>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
+            else hipLaunchKernelGGL((k_scan_back<E, N, false>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
             const int64_t values = (int64_t)a->steps * a->n * a->groups * 2 * N;
             hipLaunchKernelGGL((k_scan_shared<E, N>), dim3((unsigned)ceil_div(values, SCAN_THREADS)), dim3(SCAN_THREADS), 0, st, p,
                                seq<E>(a->db), seq<E>(a->dc));

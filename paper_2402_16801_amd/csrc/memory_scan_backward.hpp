@@ -15,27 +15,67 @@
 // The order is fixed, there are no atomics.
 
 constexpr int SCAN_BACK_WAVES = 8;       // wavefronts of a block at most
-constexpr int DPP_SHL4 = 0x104;
 
-// Sums of v over the channels of the wavefront.  Value k ends in the lanes with fold_value(lane) == k that
-// fold_writes<LANES>(lane) (the sums in the other lanes are not complete).
-template <int LANES>
-__device__ __forceinline__ float fold_channels(float (&v)[8])
+// Two values each to the halves of a row of 16 lanes (bank masks name the quarters that an addition writes): lanes with bit 3
+// clear get a's sum over bit 3, the others b's.  Then the same with bit 2.  Nothing else may stand between the
+// instructions' registers and the moves across lanes that read them for two wait states, hence the s_nop.
+__device__ __forceinline__ void fold_bit3(const float (&v)[8], float (&t)[4])
 {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) { const Pair q = swap32(v[k], v[k + 4]); v[k] = q.a + q.b; }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) { const Pair q = swap16(v[k], v[k + 2]); v[k] = q.a + q.b; }
-    const float a = v[0] + dpp<DPP_ROR8>(v[0]), b = v[1] + dpp<DPP_ROR8>(v[1]);
-    float r = threadIdx.x & 8 ? b : a;
-    if constexpr (LANES <= 4) r += dpp<DPP_SHL4>(r);
-    if constexpr (LANES <= 2) r += dpp<DPP_XOR2>(r);
-    return r;
+    asm("s_nop 1\n\t"
+        "v_add_f32_dpp %0, %4, %4 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %0, %8, %8 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %1, %5, %5 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %1, %9, %9 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %2, %6, %6 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %2, %10, %10 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "v_add_f32_dpp %3, %7, %7 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+        "v_add_f32_dpp %3, %11, %11 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+        "s_nop 1"
+        : "=&v"(t[0]), "=&v"(t[1]), "=&v"(t[2]), "=&v"(t[3])
+        : "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "v"(v[4]), "v"(v[5]), "v"(v[6]), "v"(v[7]));
 }
-__device__ __forceinline__ int fold_value(int lane) { return (lane >> 5 & 1) * 4 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1); }
+__device__ __forceinline__ void fold_bit2(const float (&t)[4], float (&r)[2])
+{
+    asm("s_nop 1\n\t"
+        "v_add_f32_dpp %0, %2, %2 row_shl:4 row_mask:0xf bank_mask:0x5\n\t"
+        "v_add_f32_dpp %0, %4, %4 row_shr:4 row_mask:0xf bank_mask:0xa\n\t"
+        "v_add_f32_dpp %1, %3, %3 row_shl:4 row_mask:0xf bank_mask:0x5\n\t"
+        "v_add_f32_dpp %1, %5, %5 row_shr:4 row_mask:0xf bank_mask:0xa\n\t"
+        "s_nop 1"
+        : "=&v"(r[0]), "=&v"(r[1])
+        : "v"(t[0]), "v"(t[1]), "v"(t[2]), "v"(t[3]));
+}
+
+// Sums of v over the channels of the wavefront.  Value k ends in the lanes with fold_value<LANES>(lane) == k that
+// fold_writes<LANES>(lane).
+template <int LANES>
+__device__ __forceinline__ float fold_channels(const float (&v)[8])
+{
+    float t[4], r[2];
+    fold_bit3(v, t);
+    Pair q;
+    if constexpr (LANES == 8) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) { q = swap16(t[k], t[k + 2]); r[k] = q.a + q.b; }
+        q = swap32(r[0], r[1]);
+        return q.a + q.b;
+    } else {
+        fold_bit2(t, r);
+        q = swap16(r[0], r[1]);
+        float s = q.a + q.b;
+        q = swap32(s, s);
+        s = q.a + q.b;
+        if constexpr (LANES == 2) s += dpp<DPP_XOR2>(s);
+        return s;
+    }
+}
+template <int LANES> __device__ __forceinline__ int fold_value(int lane)
+{
+    return (lane >> 3 & 1) * 4 + (LANES == 8 ? (lane >> 4 & 1) * 2 + (lane >> 5 & 1) : (lane >> 2 & 1) * 2 + (lane >> 4 & 1));
+}
 template <int LANES> __device__ __forceinline__ bool fold_writes(int lane)
 {
-    return LANES == 8 || (LANES == 4 ? (lane & 4) == 0 : (lane & 6) == 0);
+    return LANES == 8 || (LANES == 4 ? (lane & 32) == 0 : (lane & 34) == 0);
 }
 
 // LDS of a wavefront: b and c of a block of steps, what a step needs of each channel, and two turns of sums for db and dc.
@@ -53,7 +93,7 @@ template <typename E> __device__ __forceinline__ const ScanParams<E>& arguments_
     return *(const ScanParams<E>*)(const __attribute__((address_space(4))) void*)at;
 }
 
-template <typename E, int N>
+template <typename E, int N, bool GATE>
 __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_per_eu(2))) void k_scan_back(const ScanParams<E> given)
 {
     constexpr int LANES = Lay<N>::LANES, CHANNELS = Lay<N>::CHANNELS, OWN = Lay<N>::OWN, SUMS = BLOCK * 2 * N;
@@ -76,8 +116,10 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
     zero(da);
     const float skip = given.d ? given.d[w.channel] : 0.0f;
     const float bias = given.delta_bias ? given.delta_bias[w.channel] : 0.0f;
-    const int slot = fold_value(lane) / 4 * N + w.quad * 4 + fold_value(lane) % 4;       // among the 2 N sums of a step
+    const int slot = fold_value<LANES>(lane) / 4 * N + w.quad * 4 + fold_value<LANES>(lane) % 4;       // among the 2 N sums of a step
     const int own = w.quad * OWN;
+    // the sums of a step that this thread adds up over the block's wavefronts, and how many steps it goes on
+    const int sum_row = (int)threadIdx.x / (2 * N), sum_value = (int)threadIdx.x % (2 * N), sum_rows = (int)blockDim.x / (2 * N);
     int turn = 0;
     for (int i = env_row; i < given.n; i += env_rows) {
         const ScanParams<E>& p = arguments_again<E>();
@@ -85,17 +127,15 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
         const int length = scan_length(p, i);
         const int end = t1 < length ? t1 : length;
         const int dead = t0 > end ? t0 : end;
-        const bool gate = p.z.data;
         if (owns)
             for (int t = dead + w.quad; t < t1; t += LANES) {
                 p.dx.at(t, i)[w.channel] = Elem<E>::down(0.0f);
                 p.ddelta.at(t, i)[w.channel] = Elem<E>::down(0.0f);
-                if (gate) p.dz.at(t, i)[w.channel] = Elem<E>::down(0.0f);
+                if (GATE) p.dz.at(t, i)[w.channel] = Elem<E>::down(0.0f);
             }
         const int64_t sum_step = (int64_t)p.n * blocks * (2 * N);          // from one step's sums to the next one's
-        float* at_sums = p.shared_part + ((int64_t)i * blocks + group_block) * (2 * N);
-        for (int q = (int)threadIdx.x; q < (t1 - dead) * 2 * N; q += (int)blockDim.x)
-            at_sums[(dead + q / (2 * N)) * sum_step + q % (2 * N)] = 0.0f;
+        float* at_sums = p.shared_part + ((int64_t)i * blocks + group_block) * (2 * N) + sum_value;
+        for (int t = dead + sum_row; t < t1; t += sum_rows) at_sums[t * sum_step] = 0.0f;
         if (p.parts > 1) load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), g);
         else if (p.dstate_out) load4(state_of<N>(p.dstate_out, p.channels, i, w), g);
         else zero(g);
@@ -122,7 +162,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                 load_own<E, OWN>(at_x, step_x, own, count, next_x);
                 load_own<E, OWN>(at_delta, step_delta, own, count, next_delta);
                 load_own<E, OWN>(at_dy, step_dy, own, count, next_dy);
-                if (gate) load_own<E, OWN>(at_z, step_z, own, count, next_z);
+                if (GATE) load_own<E, OWN>(at_z, step_z, own, count, next_z);
                 load4(at_saved, next_h);
                 at_first.move(-1);
                 at_shared.move(-1);
@@ -146,7 +186,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                     float size = soft ? softplus(pre) : pre;
                     slope[k] = soft ? sigmoid(pre) : 1.0f;
                     float dout = Elem<E>::up(next_dy[k]), x = Elem<E>::up(next_x[k]);
-                    if (gate) {
+                    if (GATE) {
                         const float z = Elem<E>::up(next_z[k]), s = sigmoid(z);
                         dz[k] = dout * (s * __builtin_fmaf(z, 1.0f - s, 1.0f));
                         dout *= z * s;
@@ -165,7 +205,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                     float4 step = step_lds[mine];
                     float b[4], c[4];
                     load4(&shared_lds[w.quad], b);
-                    if (gate) load4(&shared_lds[N / 4 + w.quad], c);
+                    if (GATE) load4(&shared_lds[N / 4 + w.quad], c);
 #pragma unroll
                     for (int k = 0; k < BLOCK; ++k) {
                         float4 next_step = step;
@@ -173,7 +213,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                         if (k + 1 < BLOCK) {
                             next_step = step_lds[(k + 1) * CHANNELS + mine];
                             load4(&shared_lds[(k + 1) * (N / 2) + w.quad], next_b);
-                            if (gate) load4(&shared_lds[(k + 1) * (N / 2) + N / 4 + w.quad], next_c);
+                            if (GATE) load4(&shared_lds[(k + 1) * (N / 2) + N / 4 + w.quad], next_c);
                         }
                         if (decltype(check)::value && (cuts >> k & 1u)) zero(h);
 #pragma unroll
@@ -182,7 +222,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                             kept[k][m] = decay[k][m] * h[m];
                             h[m] = __builtin_fmaf(step.y, b[m], kept[k][m]);
                         }
-                        if (gate) {
+                        if (GATE) {
                             y[k] = h[0] * c[0];
 #pragma unroll
                             for (int m = 1; m < 4; ++m) y[k] = __builtin_fmaf(h[m], c[m], y[k]);
@@ -197,7 +237,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                 if (cuts == 0) states(std::false_type{});
                 else states(std::true_type{});
                 wave_fence();       // what is in LDS is read again rather than kept in registers: 64 more of them
-                if (gate) {
+                if (GATE) {
                     fold_steps<LANES>(y);
 #pragma unroll
                     for (int k = 0; k < OWN; ++k) {
@@ -257,7 +297,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                 pin(next_x);
                 pin(next_delta);
                 pin(next_dy);
-                if (gate) pin(next_z);
+                if (GATE) pin(next_z);
                 pin(next_h);
                 if (owns) {
 #pragma unroll
@@ -272,11 +312,11 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                 at_dz -= BLOCK * step_dz;
                 __syncthreads();
                 // sums over the block's wavefronts; the next turn writes the other half, so one barrier is enough
-                const float* from = sum_lds + turn * waves * SUMS;
-                for (int q = (int)threadIdx.x; q < count * 2 * N; q += (int)blockDim.x) {
-                    float s = from[q];
-                    for (int v = 1; v < waves; ++v) s += from[v * SUMS + q];
-                    at_sums[(q / (2 * N)) * sum_step + q % (2 * N)] = s;
+                const float* from = sum_lds + turn * waves * SUMS + sum_value;
+                for (int k = sum_row; k < count; k += sum_rows) {
+                    float s = from[k * 2 * N];
+                    for (int v = 1; v < waves; ++v) s += from[v * SUMS + k * 2 * N];
+                    at_sums[k * sum_step] = s;
                 }
                 at_sums -= BLOCK * sum_step;
                 turn ^= 1;
