@@ -365,45 +365,70 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
     if (p.state_out && p.parts == 1) store4(state_of<N>(p.state_out, p.channels, i, w), h);
 }
 
-// Carries the state through the parts: starts[part] turns from the part's own end into the state at its
-// start.  Backward in time for the gradient of the state.
+// Carries the state through the parts: starts[part] turns from the part's own end into the state at its start.  Backward in
+// time for the gradient of the state.  A block is a tile of an environment; each of its wavefronts takes a run of
+// parts, first adds up what they do together, and, once it knows what the runs before it do, goes through them again.
+// Two trips to memory for any number of parts up to 128, where one wavefront would make one for every eight
+// (157 parts: 22 us).
+constexpr int CARRY_WAVES = 16;
 template <typename E, int N, bool BACK>
-__global__ __launch_bounds__(SCAN_THREADS) void k_scan_carry(const ScanParams<E> p)
+__global__ __launch_bounds__(CARRY_WAVES* WAVE) void k_scan_carry(const ScanParams<E> p)
 {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + wave;
-    if (item >= (int64_t)p.n * p.tiles) return;
-    const int i = (int)(item / p.tiles);
-    const Tile w = tile_of<N>(p, (int)(item % p.tiles));
-    const int mine = (int)(threadIdx.x & (WAVE - 1)) / Lay<N>::LANES;
+    constexpr int GO = 8;                       // parts whose effects are loaded together
+    __shared__ float4 ends[CARRY_WAVES][WAVE];
+    __shared__ float2 decays[CARRY_WAVES][WAVE];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), waves = (int)blockDim.x / WAVE;
+    const int lane = (int)(threadIdx.x & (WAVE - 1));
+    const int i = (int)(blockIdx.x / (unsigned)p.tiles);
+    const Tile w = tile_of<N>(p, (int)(blockIdx.x % (unsigned)p.tiles));
+    const int mine = lane / Lay<N>::LANES;
     float a2[4], h[4];
     load_rates<N>(p.a, w, a2);
+    const int run = (p.parts + waves - 1) / waves, from = wave * run, to = from + run < p.parts ? from + run : p.parts;
+    auto index_of = [&](int q) { return (int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i; };
+    auto step = [&](float2 decay, const float (&end)[4]) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) h[m] = decay.y != 0.0f ? end[m] : __builtin_fmaf(exp2_fast(decay.x * a2[m]), h[m], end[m]);
+    };
+    // the run from zero, and its decay
+    auto walk = [&](auto&& each) {
+        for (int q0 = from; q0 < to; q0 += GO) {
+            float end[GO][4];
+            float2 decay[GO];
+#pragma unroll
+            for (int k = 0; k < GO; ++k) {
+                const int64_t index = index_of(q0 + k < to ? q0 + k : to - 1);
+                load4(tiled(p.starts, index, w, p.tiles), end[k]);
+                decay[k] = p.decays[(index * p.tiles + w.tile) * Lay<N>::CHANNELS + mine];
+            }
+#pragma unroll
+            for (int k = 0; k < GO; ++k)
+                if (q0 + k < to) each(q0 + k, decay[k], end[k]);
+        }
+    };
+    zero(h);
+    float2 all = make_float2(0.0f, 0.0f);
+    walk([&](int, float2 decay, const float (&end)[4]) {
+        step(decay, end);
+        all = decay.y != 0.0f ? decay : make_float2(all.x + decay.x, all.y);
+    });
+    store4(&ends[wave][lane], h);
+    decays[wave][lane] = all;
+    __syncthreads();
     const float* in = BACK ? p.dstate_out : p.state_in;
-    float* out = BACK ? p.dstate_in : p.state_out;
     if (in) load4(state_of<N>(in, p.channels, i, w), h);
     else zero(h);
-    constexpr int GO = 32;       // parts whose effects are loaded together: few wavefronts, so the trips to memory are what counts
-    for (int q0 = 0; q0 < p.parts; q0 += GO) {
-        float end[GO][4];
-        float2 decay[GO];
-#pragma unroll
-        for (int k = 0; k < GO; ++k) {
-            const int q = q0 + k < p.parts ? q0 + k : p.parts - 1;
-            const int64_t index = (int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i;
-            load4(tiled(p.starts, index, w, p.tiles), end[k]);
-            decay[k] = p.decays[(index * p.tiles + w.tile) * Lay<N>::CHANNELS + mine];
-        }
-#pragma unroll
-        for (int k = 0; k < GO; ++k) {
-            const int q = q0 + k;
-            if (q >= p.parts) break;
-            const int64_t index = (int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i;
-            store4(tiled(p.starts, index, w, p.tiles), h);
-#pragma unroll
-            for (int m = 0; m < 4; ++m) h[m] = decay[k].y != 0.0f ? end[k][m] : __builtin_fmaf(exp2_fast(decay[k].x * a2[m]), h[m], end[k][m]);
-        }
+    for (int v = 0; v < wave; ++v) {
+        float end[4];
+        load4(&ends[v][lane], end);
+        step(decays[v][lane], end);
     }
-    if (out && w.owns) store4(state_of<N>(out, p.channels, i, w), h);
+    walk([&](int q, float2 decay, const float (&end)[4]) {
+        store4(tiled(p.starts, index_of(q), w, p.tiles), h);
+        step(decay, end);
+    });
+    float* out = BACK ? p.dstate_in : p.state_out;
+    if (out && w.owns && to == p.parts && from < to) store4(state_of<N>(out, p.channels, i, w), h);
 }
 
 // ---- one token -------------------------------------------------------------------------------------------
@@ -538,29 +563,27 @@ static ScanTiles scan_tiles(const craftax_scan_args* a)
     return t;
 }
 
-// Steps per part, a multiple of 64 (the begins of episodes are read 64 steps at a time).
+// Steps per part, whole blocks of steps, for about `want` parts.
 struct ScanParts { int part, parts; };
-static ScanParts scan_parts(const craftax_scan_args* a, int tiles, int64_t wavefronts)
+static ScanParts scan_parts(const craftax_scan_args* a, int64_t want)
 {
-    const int64_t waves = (int64_t)a->n * tiles;
-    ScanParts s = {a->steps, 1};
-    // Split steps cost the state's recurrence twice (about 1.7 times the work), so a chip half full is left as it is.
-    if (2 * waves > wavefronts || a->steps <= WAVE) return s;
-    const int64_t want = wavefronts / waves;
-    int64_t part = (ceil_div(a->steps, want) + WAVE - 1) / WAVE * WAVE;
-    if (ceil_div(a->steps, part) > 65535) part = (ceil_div(a->steps, 65535) + WAVE - 1) / WAVE * WAVE;
-    s.part = (int)part;
-    s.parts = (int)ceil_div(a->steps, part);
-    if (s.parts == 1) s.part = a->steps;
-    return s;
+    if (want < 2 || a->steps < 4 * BLOCK) return {a->steps, 1};
+    int64_t part = ceil_div(ceil_div(a->steps, want), BLOCK) * BLOCK;
+    if (part < 2 * BLOCK) part = 2 * BLOCK;
+    if (ceil_div(a->steps, part) > 65535) part = ceil_div(ceil_div(a->steps, 65535), BLOCK) * BLOCK;
+    const int64_t parts = ceil_div(a->steps, part);
+    return parts == 1 ? ScanParts{a->steps, 1} : ScanParts{(int)part, (int)parts};
 }
+
+static unsigned carry_threads(int parts) { return (unsigned)(parts < CARRY_WAVES ? parts : CARRY_WAVES) * WAVE; }
 
 // States above this size (three quarters of the last-level cache) would push each other out of it between two tokens: 268 MB
 // streamed 109 us, through the caches 120, 2.1 GB 981 and 1,052; below it a token finds the state of the one before
 // (33 MB through the caches 13.3 us, streamed 14.4).
 constexpr int64_t TOKEN_STREAMED = (int64_t)192 << 20;
-constexpr int64_t SCAN_FILL = (int64_t)CHIP_SIMDS * 8;           // wavefronts that fill the chip
-constexpr int64_t SCAN_BACK_FILL = (int64_t)CHIP_SIMDS * 4;
+constexpr int64_t SCAN_FILL = (int64_t)CHIP_SIMDS * 5;           // wavefronts that the chip holds of k_scan,
+constexpr int64_t SCAN_BACK_FILL = (int64_t)CHIP_SIMDS * 2;      // of k_scan_back,
+constexpr int64_t TOKEN_FILL = (int64_t)CHIP_SIMDS * 8;          // of k_scan_token
 
 static bool scan_shape_ok(const craftax_scan_args* a)
 {
@@ -583,7 +606,24 @@ static ScanSpace scan_space(const craftax_scan_args* a, bool backward)
 {
     const ScanTiles t = scan_tiles(a);
     ScanSpace s{};
-    s.parts = scan_parts(a, t.tiles, backward ? SCAN_BACK_FILL : SCAN_FILL);
+    if (backward) {
+        // wavefronts of a block: as many as leave no more than a fifth of them without a tile
+        s.waves = SCAN_BACK_WAVES;
+        while (s.waves > 1 && ceil_div(t.group_tiles, s.waves) * s.waves * 4 > t.group_tiles * 5) s.waves /= 2;
+        s.group_blocks = (int)ceil_div(t.group_tiles, s.waves);
+        // Blocks are to be there all at once: a few more than that take twice the time.  Too few environments are split into parts
+        // (the walk before costs a third); of too many, a block takes several one after the other, which also keeps the rows
+        // of partial sums few.
+        const int64_t room = SCAN_BACK_FILL / s.waves, each = (int64_t)a->groups * s.group_blocks;
+        s.parts = scan_parts(a, room / (each * a->n));
+        const int64_t side = each < room ? room / each : 1, turns = ceil_div(a->n, side);
+        s.rows = (int)ceil_div(a->n, turns) * s.parts.parts;
+    } else {
+        // Split steps cost the recurrence of the states twice, 1.7 times the work: a quarter of the chip is filled better without
+        // (100 steps of 64 environments of 512 channels: 24 us, in two parts 46).
+        const int64_t want = SCAN_FILL / ((int64_t)a->n * t.tiles);
+        s.parts = scan_parts(a, want < 4 ? 1 : want);
+    }
     size_t at = 0;
     if (s.parts.parts > 1) {
         s.starts = at;
@@ -592,15 +632,6 @@ static ScanSpace scan_space(const craftax_scan_args* a, bool backward)
         at += round256((size_t)s.parts.parts * a->n * t.tiles * (WAVE / (a->states / 4)) * sizeof(float2));
     }
     if (backward) {
-        s.waves = 1;
-        while (s.waves < SCAN_BACK_WAVES && s.waves < t.group_tiles) s.waves *= 2;
-        s.group_blocks = (int)ceil_div(t.group_tiles, s.waves);
-        // a block takes several environments one after the other, so that no more rows of partial sums are written than
-        // fill the chip
-        const int64_t waves = (int64_t)a->n * a->groups * s.group_blocks * s.waves;
-        int64_t turns = s.parts.parts > 1 ? 1 : waves / SCAN_BACK_FILL;
-        if (turns < 1) turns = 1;
-        s.rows = (int)ceil_div(a->n, turns) * s.parts.parts;
         s.shared = at;
         at += round256((size_t)a->steps * a->n * a->groups * s.group_blocks * 2 * a->states * sizeof(float));
         s.weights = at;
@@ -662,7 +693,7 @@ int scan(const craftax_scan_args* a, void* stream, const char** why)
             constexpr int N = decltype(states)::value;
             if (a->steps == 1 && !a->saved) {
                 // environments side by side: as many threads as the chip holds, each with several of them in turn, or all
-                const int64_t per_env = (int64_t)a->channels * (N / 4), side = ceil_div(SCAN_FILL * WAVE, per_env);
+                const int64_t per_env = (int64_t)a->channels * (N / 4), side = ceil_div(TOKEN_FILL * WAVE, per_env);
                 p.part = (int)(side < a->n ? side : a->n);
                 const dim3 grid((unsigned)ceil_div(p.part * per_env, SCAN_THREADS));
                 if (a->n * per_env * (int64_t)sizeof(float4) > TOKEN_STREAMED) hipLaunchKernelGGL((k_scan_token<E, N, true>), grid, dim3(SCAN_THREADS), 0, st, p);
@@ -678,7 +709,7 @@ int scan(const craftax_scan_args* a, void* stream, const char** why)
                 p.starts = reinterpret_cast<float4*>(base + s.starts);
                 p.decays = reinterpret_cast<float2*>(base + s.decays);
                 hipLaunchKernelGGL((k_scan<E, N, true>), grid, dim3(SCAN_THREADS), 0, st, p);
-                hipLaunchKernelGGL((k_scan_carry<E, N, false>), dim3(blocks), dim3(SCAN_THREADS), 0, st, p);
+                hipLaunchKernelGGL((k_scan_carry<E, N, false>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
             }
             hipLaunchKernelGGL((k_scan<E, N, false>), grid, dim3(SCAN_THREADS), 0, st, p);
         });
@@ -706,7 +737,7 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
             if (p.parts > 1) {
                 const unsigned blocks = (unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES);
                 hipLaunchKernelGGL((k_scan_back_part<E, N>), dim3(blocks, (unsigned)p.parts), dim3(SCAN_THREADS), 0, st, p);
-                hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3(blocks), dim3(SCAN_THREADS), 0, st, p);
+                hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
             }
             const dim3 grid((unsigned)((int64_t)(s.rows / p.parts) * a->groups * s.group_blocks), (unsigned)p.parts);
             if (p.z.data) hipLaunchKernelGGL((k_scan_back<E, N, true>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
