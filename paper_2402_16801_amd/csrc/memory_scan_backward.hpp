@@ -163,7 +163,8 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                 load_own<E, OWN>(at_delta, step_delta, own, count, next_delta);
                 load_own<E, OWN>(at_dy, step_dy, own, count, next_dy);
                 if (GATE) load_own<E, OWN>(at_z, step_z, own, count, next_z);
-                load4(at_saved, next_h);
+                const Four v = __builtin_nontemporal_load(reinterpret_cast<const Four*>(at_saved));
+                next_h[0] = v.x; next_h[1] = v.y; next_h[2] = v.z; next_h[3] = v.w;
                 at_first.move(-1);
                 at_shared.move(-1);
                 at_x -= BLOCK * step_x;
