@@ -1,0 +1,54 @@
+"""The policy memory operators refuse what is not on a GPU, and their structures match the C header's (no GPU needed)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2402_16801_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def mem():
+    from paper_2402_16801_amd import memory
+    return memory
+
+
+def test_tensors_on_the_cpu_are_refused(mem):
+    x, state = torch.zeros(2, 3, 8), torch.zeros(3, 3, 8)
+    with pytest.raises(binding.CraftaxError):
+        mem.causal_conv(x, torch.zeros(8, 4))
+    with pytest.raises(binding.CraftaxError):
+        mem.causal_conv_step(x[0], torch.zeros(8, 4), None, state)
+    with pytest.raises(binding.CraftaxError):
+        mem.selective_scan(x, x, torch.zeros(8, 16), torch.zeros(2, 3, 1, 16), torch.zeros(2, 3, 1, 16))
+    with pytest.raises(binding.CraftaxError):
+        mem.residual_norm(x, x)
+
+
+def test_an_unknown_gate_is_refused(mem):
+    with pytest.raises(binding.CraftaxError, match="gate_act"):
+        mem.residual_norm(torch.zeros(1, 1, 8), torch.zeros(1, 1, 8), gate_act="tanh")
+
+
+def test_structures_match_the_header(tmp_path):
+    pairs = [("craftax_conv_args", binding.ConvArgs), ("craftax_scan_args", binding.ScanArgs),
+             ("craftax_norm_args", binding.NormArgs)]
+    lines, want = [], []
+    for name, struct in pairs:
+        lines.append(f'printf("%zu\\n", sizeof({name}));')
+        want.append(ctypes.sizeof(struct))
+        fields = [field[0] for field in struct._fields_]
+        for field in fields:
+            base, _, last = field.rpartition("_")          # a view's members lie side by side: x, x_step, x_env
+            member = f"{base}.{last}" if last in ("step", "env") and base in fields else field
+            lines.append(f'printf("%zu\\n", offsetof({name}, {member}));')
+            want.append(getattr(struct, field).offset)
+    source = tmp_path / "sizes.c"
+    source.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "craftax.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0; }\n")
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), "-o", str(tmp_path / "sizes"), str(source)], check=True)
+    got = subprocess.run([str(tmp_path / "sizes")], check=True, capture_output=True, text=True).stdout.split()
+    assert [int(v) for v in got] == want
