@@ -401,7 +401,7 @@ int craftax_stats_static(const void *state, craftax_metrics *out, int n, void *s
  * Conventions of this header hold: DEVICE pointers, no allocation, work is only enqueued on
  * `stream`, nothing is launched on an error.  No result depends on the order in which blocks run.
  * Pointers and strides only have to be aligned to their elements unless something else is said.
- * Outputs must not overlap inputs, except that a state may be updated in place.  A workspace is
+ * Outputs must not overlap inputs, except that state_out may be state_in.  A workspace is
  * DEVICE scratch, 256-byte aligned, contents irrelevant before and after; its size, for the same
  * arguments, comes from the *_workspace_bytes call (0: none is needed).  Errors: CRAFTAX_E_NULL,
  * CRAFTAX_E_ALIGN, CRAFTAX_E_COUNT (a size outside its range or a workspace too small),
@@ -457,7 +457,7 @@ typedef struct craftax_scan_args {
     craftax_view first;         /* uint8, or absent */
     const int32_t *lengths;     /* or NULL */
     craftax_view x, delta, z, y;   /* z may be absent */
-    craftax_view b, c;          /* [groups][states] values per step and environment, 4-byte aligned rows */
+    craftax_view b, c;          /* [groups][states] values per step and environment */
     const float *state_in;      /* or NULL: 0; 16-byte aligned */
     float *state_out;           /* or NULL; may be state_in; 16-byte aligned */
     void *saved;                /* or NULL: no backward pass follows */

@@ -261,7 +261,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
     const float skip = p.d ? p.d[w.channel] : 0.0f;
     const float bias = p.delta_bias ? p.delta_bias[w.channel] : 0.0f;
     if (PART) zero(h);
-    else if (part > 0) load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), h);
+    else if (p.parts > 1) load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), h);       // state_in may be state_out, which is written by now
     else if (p.state_in) load4(state_of<N>(p.state_in, p.channels, i, w), h);
     else zero(h);
     float total = 0.0f, cut = 0.0f;

@@ -67,6 +67,38 @@ def test_scan_of_many_parts(mem, case):
         close("gradient of " + name, value, want[name], chain + D)
 
 
+@pytest.mark.parametrize("T", [1, 8, 40, 2000])
+@pytest.mark.parametrize("operator", ["scan", "conv"])
+def test_a_state_is_updated_in_place(mem, operator, T):
+    """At the C entry state_out may be state_in, for one part of steps as for many."""
+    from paper_2402_16801_amd import binding as cx
+    lib, n, D = cx.load(), 2, 66
+    src = Source(T, torch.float32)
+    seqs = {k: src.gpu(src.seq(T, n, D)) for k in ("x", "y")}
+    seqs.update({k: src.gpu(src.seq(T, n, 16)) for k in ("b", "c")})
+    views = {f: v for k, t in seqs.items() for f, v in ((k, t.data_ptr()), (k + "_step", t.stride(0)), (k + "_env", t.stride(1)))}
+    x = seqs["x"]
+    if operator == "scan":
+        a, state = -torch.rand(D, 16, device="cuda") * 0.1, torch.randn(n, D, 16, device="cuda")
+        want_y, want, _ = mem.selective_scan(x, x, a, seqs["b"].unsqueeze(2), seqs["c"].unsqueeze(2), state=state)
+        args = cx.ScanArgs(dtype=0, softplus=1, steps=T, n=n, channels=D, states=16, groups=1, a=a.data_ptr(), delta=x.data_ptr(),
+                           delta_step=x.stride(0), delta_env=x.stride(1), state_in=state.data_ptr(), state_out=state.data_ptr(), **views)
+        need = lib.craftax_selective_scan_workspace_bytes(args, 0)
+        work = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        args.workspace, args.workspace_bytes = work.data_ptr(), need
+        call = lib.craftax_selective_scan
+    else:
+        weight, state = torch.randn(D, 4, device="cuda"), torch.randn(n, 3, D, device="cuda")
+        want_y, want = mem.causal_conv(x, weight, state=state)
+        args = cx.ConvArgs(dtype=0, silu=1, steps=T, n=n, channels=D, taps=4, weight=weight.data_ptr(), state_in=state.data_ptr(),
+                           state_out=state.data_ptr(), **{k: v for k, v in views.items() if k[0] in "xy"})
+        call = lib.craftax_causal_conv
+    torch.cuda.synchronize()
+    assert call(args, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(seqs["y"], want_y) and torch.equal(state, want)
+
+
 def rollout(example, dtype, n=300, steps=40):
     """A policy and what it saw while episodes of 15 steps end, some of them within the rollout's first steps."""
     from paper_2402_16801_amd import binding as cx, synth
