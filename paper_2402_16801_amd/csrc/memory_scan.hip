@@ -51,6 +51,7 @@ template <typename E> struct ScanParams {
     float* weight_part;    // backward: [rows][channels][N + 2] sums for da, dd and ddelta_bias
     int steps, n, channels, groups, group_channels, group_tiles, tiles, softplus;
     int part, parts;       // steps per part (whole blocks), number of parts
+    int own_starts;        // wavefronts find the starts of their parts themselves (see part_start)
     int rows, group_blocks;          // backward: rows of weight_part, blocks per group
 };
 
@@ -232,6 +233,43 @@ __device__ __forceinline__ void fold_steps(float (&v)[BLOCK])
     }
 }
 
+// The state behind a part, from the one before it and what the part does.
+__device__ __forceinline__ void pass_part(const float (&a2)[4], float2 decay, const float (&end)[4], float (&h)[4])
+{
+#pragma unroll
+    for (int m = 0; m < 4; ++m) h[m] = decay.y != 0.0f ? end[m] : __builtin_fmaf(exp2_fast(decay.x * a2[m]), h[m], end[m]);
+}
+
+// The state at the start of a part.  Of few parts (`own_starts`) every wavefront goes through the parts before its own, behind it
+// backward in time, and is spared a kernel between the two; of many, that kernel, k_scan_carry, has left it in `starts`.
+template <typename E, int N, bool BACK>
+__device__ __forceinline__ void part_start(const ScanParams<E>& p, int part, int i, const Tile& w, const float (&a2)[4], float (&h)[4])
+{
+    constexpr int GO = 4;                       // parts whose effects are loaded together
+    if (p.parts > 1 && !p.own_starts) {
+        load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), h);
+        return;
+    }
+    const float* in = BACK ? p.dstate_out : p.state_in;
+    if (in) load4(state_of<N>(in, p.channels, i, w), h);
+    else zero(h);
+    const int before = BACK ? p.parts - 1 - part : part;
+    for (int q0 = 0; q0 < before; q0 += GO) {
+        float end[GO][4];
+        float2 decay[GO];
+#pragma unroll
+        for (int k = 0; k < GO; ++k) {
+            const int q = q0 + k < before ? q0 + k : before - 1;
+            const int64_t index = (int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i;
+            load4(tiled(p.starts, index, w, p.tiles), end[k]);
+            decay[k] = p.decays[(index * p.tiles + w.tile) * Lay<N>::CHANNELS + (int)(threadIdx.x & (WAVE - 1)) / Lay<N>::LANES];
+        }
+#pragma unroll
+        for (int k = 0; k < GO; ++k)
+            if (q0 + k < before) pass_part(a2, decay[k], end[k], h);
+    }
+}
+
 // ---- forward ------------------------------------------------------------------------------------------
 // One wavefront: the steps of one part of one tile of one environment.  PART: only the part's effect on the
 // state.  SAVE: the states before every block are kept for a backward pass (streamed: they are read long after).  The
@@ -261,9 +299,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
     const float skip = p.d ? p.d[w.channel] : 0.0f;
     const float bias = p.delta_bias ? p.delta_bias[w.channel] : 0.0f;
     if (PART) zero(h);
-    else if (p.parts > 1) load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), h);       // state_in may be state_out, which is written by now
-    else if (p.state_in) load4(state_of<N>(p.state_in, p.channels, i, w), h);
-    else zero(h);
+    else part_start<E, N, false>(p, part, i, w, a2, h);
     float total = 0.0f, cut = 0.0f;
     const int own = w.quad * OWN;
     const E *at_x = walk_from<const E, N>(p.x, t0, i, w), *at_delta = walk_from<const E, N>(p.delta, t0, i, w);
@@ -368,19 +404,18 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
     }
     if (!w.owns) return;
     for (int t = (t0 > end ? t0 : end) + w.quad; t < t1; t += LANES) p.y.at(t, i)[w.channel] = Elem<E>::down(0.0f);
-    if (p.state_out && p.parts == 1) store4(state_of<N>(p.state_out, p.channels, i, w), h);
+    if (p.state_out && part == p.parts - 1) store4(state_of<N>(p.state_out, p.channels, i, w), h);
 }
 
-// Carries the state through the parts: starts[part] turns from the part's own end into the state at its start.  Backward in
+// Carries the state through the parts: starts[part] turns from what the part does into the state at its start.  Backward in
 // time for the gradient of the state.  A block is a tile of an environment; each of its wavefronts takes a run of
 // parts, first adds up what they do together, and, once it knows what the runs before it do, goes through them again.
-// Two trips to memory for any number of parts up to 128, where one wavefront would make one for every eight
-// (157 parts: 22 us).
+// One trip to memory for up to 192 parts (157 parts: CARRY_TIME us; 22 us where one wavefront makes one for every eight).
 constexpr int CARRY_WAVES = 16;
 template <typename E, int N, bool BACK>
 __global__ __launch_bounds__(CARRY_WAVES* WAVE) void k_scan_carry(const ScanParams<E> p)
 {
-    constexpr int GO = 8;                       // parts whose effects are loaded together
+    constexpr int GO = 12;                      // parts whose effects are loaded together
     __shared__ float4 ends[CARRY_WAVES][WAVE];
     __shared__ float2 decays[CARRY_WAVES][WAVE];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), waves = (int)blockDim.x / WAVE;
@@ -388,53 +423,55 @@ __global__ __launch_bounds__(CARRY_WAVES* WAVE) void k_scan_carry(const ScanPara
     const int i = (int)(blockIdx.x / (unsigned)p.tiles);
     const Tile w = tile_of<N>(p, (int)(blockIdx.x % (unsigned)p.tiles));
     const int mine = lane / Lay<N>::LANES;
-    float a2[4], h[4];
+    float a2[4], h[4], start[4];
     load_rates<N>(p.a, w, a2);
+    const float* in = BACK ? p.dstate_out : p.state_in;
+    if (in) load4(state_of<N>(in, p.channels, i, w), start);
+    else zero(start);
     const int run = (p.parts + waves - 1) / waves, from = wave * run, to = from + run < p.parts ? from + run : p.parts;
     auto index_of = [&](int q) { return (int64_t)(BACK ? p.parts - 1 - q : q) * p.n + i; };
-    auto step = [&](float2 decay, const float (&end)[4]) {
+    float end[GO][4];
+    float2 decay[GO];
+    // what the last part does nobody asks for, and it is not there
+    auto load = [&](int q0) {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) h[m] = decay.y != 0.0f ? end[m] : __builtin_fmaf(exp2_fast(decay.x * a2[m]), h[m], end[m]);
-    };
-    // the run from zero, and its decay
-    auto walk = [&](auto&& each) {
-        for (int q0 = from; q0 < to; q0 += GO) {
-            float end[GO][4];
-            float2 decay[GO];
-#pragma unroll
-            for (int k = 0; k < GO; ++k) {
-                const int64_t index = index_of(q0 + k < to ? q0 + k : to - 1);
-                load4(tiled(p.starts, index, w, p.tiles), end[k]);
-                decay[k] = p.decays[(index * p.tiles + w.tile) * Lay<N>::CHANNELS + mine];
-            }
-#pragma unroll
-            for (int k = 0; k < GO; ++k)
-                if (q0 + k < to) each(q0 + k, decay[k], end[k]);
+        for (int k = 0; k < GO; ++k) {
+            const int64_t index = index_of(q0 + k < p.parts - 1 ? q0 + k : p.parts - 2);
+            load4(tiled(p.starts, index, w, p.tiles), end[k]);
+            decay[k] = p.decays[(index * p.tiles + w.tile) * Lay<N>::CHANNELS + mine];
         }
     };
+    // the run from zero, and its decay
     zero(h);
     float2 all = make_float2(0.0f, 0.0f);
-    walk([&](int, float2 decay, const float (&end)[4]) {
-        step(decay, end);
-        all = decay.y != 0.0f ? decay : make_float2(all.x + decay.x, all.y);
-    });
+    for (int q0 = from; q0 < to; q0 += GO) {
+        load(q0);
+#pragma unroll
+        for (int k = 0; k < GO; ++k)
+            if (q0 + k < to) {
+                pass_part(a2, decay[k], end[k], h);
+                all = decay[k].y != 0.0f ? decay[k] : make_float2(all.x + decay[k].x, all.y);
+            }
+    }
     store4(&ends[wave][lane], h);
     decays[wave][lane] = all;
     __syncthreads();
-    const float* in = BACK ? p.dstate_out : p.state_in;
-    if (in) load4(state_of<N>(in, p.channels, i, w), h);
-    else zero(h);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) h[m] = start[m];
     for (int v = 0; v < wave; ++v) {
-        float end[4];
-        load4(&ends[v][lane], end);
-        step(decays[v][lane], end);
+        float before[4];
+        load4(&ends[v][lane], before);
+        pass_part(a2, decays[v][lane], before, h);
     }
-    walk([&](int q, float2 decay, const float (&end)[4]) {
-        store4(tiled(p.starts, index_of(q), w, p.tiles), h);
-        step(decay, end);
-    });
-    float* out = BACK ? p.dstate_in : p.state_out;
-    if (out && w.owns && to == p.parts && from < to) store4(state_of<N>(out, p.channels, i, w), h);
+    for (int q0 = from; q0 < to; q0 += GO) {
+        if (run > GO) load(q0);
+#pragma unroll
+        for (int k = 0; k < GO; ++k)
+            if (q0 + k < to) {
+                store4(tiled(p.starts, index_of(q0 + k), w, p.tiles), h);
+                pass_part(a2, decay[k], end[k], h);
+            }
+    }
 }
 
 // ---- one token -------------------------------------------------------------------------------------------
@@ -580,6 +617,8 @@ static ScanParts scan_parts(const craftax_scan_args* a, int64_t want)
     return parts == 1 ? ScanParts{a->steps, 1} : ScanParts{(int)part, (int)parts};
 }
 
+// Parts that are few enough for every wavefront to go through them: OWN_MEASURED.
+constexpr int OWN_STARTS = 16;
 static unsigned carry_threads(int parts) { return (unsigned)(parts < CARRY_WAVES ? parts : CARRY_WAVES) * WAVE; }
 
 // States above this size (three quarters of the last-level cache) would push each other out of it between two tokens: 268 MB
@@ -713,8 +752,10 @@ int scan(const craftax_scan_args* a, void* stream, const char** why)
             if (p.parts > 1) {
                 p.starts = reinterpret_cast<float4*>(base + s.starts);
                 p.decays = reinterpret_cast<float2*>(base + s.decays);
-                hipLaunchKernelGGL((k_scan<E, N, PART_ONLY, false>), grid, dim3(SCAN_THREADS), 0, st, p);
-                hipLaunchKernelGGL((k_scan_carry<E, N, false>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
+                hipLaunchKernelGGL((k_scan<E, N, PART_ONLY, false>), dim3(blocks, (unsigned)p.parts - 1), dim3(SCAN_THREADS), 0, st, p);
+                // a state that is written in place is not there any more when the last parts ask for it
+                p.own_starts = p.parts <= OWN_STARTS && !(p.state_in && p.state_in == p.state_out);
+                if (!p.own_starts) hipLaunchKernelGGL((k_scan_carry<E, N, false>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
             }
             if (p.saved && p.z.data) hipLaunchKernelGGL((k_scan<E, N, SAVE, true>), grid, dim3(SCAN_THREADS), 0, st, p);
             else if (p.saved) hipLaunchKernelGGL((k_scan<E, N, SAVE, false>), grid, dim3(SCAN_THREADS), 0, st, p);
@@ -744,8 +785,9 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
             constexpr int N = decltype(states)::value;
             if (p.parts > 1) {
                 const unsigned blocks = (unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES);
-                hipLaunchKernelGGL((k_scan_back_part<E, N>), dim3(blocks, (unsigned)p.parts), dim3(SCAN_THREADS), 0, st, p);
-                hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
+                hipLaunchKernelGGL((k_scan_back_part<E, N>), dim3(blocks, (unsigned)p.parts - 1), dim3(SCAN_THREADS), 0, st, p);
+                p.own_starts = p.parts <= OWN_STARTS;
+                if (!p.own_starts) hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
             }
             const dim3 grid((unsigned)((int64_t)(s.rows / p.parts) * a->groups * s.group_blocks), (unsigned)p.parts);
             if (p.z.data) hipLaunchKernelGGL((k_scan_back<E, N, true>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);

@@ -140,9 +140,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
         const int64_t sum_step = (int64_t)p.n * blocks * (2 * N);          // from one step's sums to the next one's
         float* at_sums = p.shared_part + ((int64_t)i * blocks + group_block) * (2 * N) + sum_value;
         for (int t = dead + sum_row; t < t1; t += sum_rows) at_sums[t * sum_step] = 0.0f;
-        if (p.parts > 1) load4(tiled(p.starts, (int64_t)part * p.n + i, w, p.tiles), g);
-        else if (p.dstate_out) load4(state_of<N>(p.dstate_out, p.channels, i, w), g);
-        else zero(g);
+        part_start<E, N, true>(p, part, i, w, a2, g);
         if (t0 < end) {
             int t = t0 + (end - t0 - 1) / BLOCK * BLOCK;       // the last block of steps
             const E *at_x = walk_from<const E, N>(p.x, t, i, w), *at_delta = walk_from<const E, N>(p.delta, t, i, w);
@@ -253,12 +251,19 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                 float gb[BLOCK], rate[BLOCK];
                 float* sums = sum_lds + (turn * waves + wave) * SUMS;
                 auto back = [&](auto check) {
+                    float4 step = step_lds[(BLOCK - 1) * CHANNELS + mine];
+                    float b[4], c[4];
+                    load4(&shared_lds[(BLOCK - 1) * (N / 2) + w.quad], b);
+                    load4(&shared_lds[(BLOCK - 1) * (N / 2) + N / 4 + w.quad], c);
 #pragma unroll
                     for (int k = BLOCK - 1; k >= 0; --k) {
-                        const float4 step = step_lds[k * CHANNELS + mine];
-                        float b[4], c[4], v[8];
-                        load4(&shared_lds[k * (N / 2) + w.quad], b);
-                        load4(&shared_lds[k * (N / 2) + N / 4 + w.quad], c);
+                        float4 next_step = step;
+                        float next_b[4] = {}, next_c[4] = {}, v[8];
+                        if (k > 0) {
+                            next_step = step_lds[(k - 1) * CHANNELS + mine];
+                            load4(&shared_lds[(k - 1) * (N / 2) + w.quad], next_b);
+                            load4(&shared_lds[(k - 1) * (N / 2) + N / 4 + w.quad], next_c);
+                        }
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
                             v[4 + m] = step.z * __builtin_fmaf(step.y, b[m], kept[k][m]);
@@ -278,6 +283,9 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                         pin(rate[k]);
 #pragma unroll
                         for (int m = 0; m < 4; ++m) pin(da_span[m]);
+                        step = next_step;
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) { b[m] = next_b[m]; c[m] = next_c[m]; }
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 };
@@ -335,7 +343,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
                 turn ^= 1;
             }
         }
-        if (p.parts == 1 && p.dstate_in && owns) store4(state_of<N>(p.dstate_in, p.channels, i, w), g);
+        if (part == 0 && p.dstate_in && owns) store4(state_of<N>(p.dstate_in, p.channels, i, w), g);
     }
     // a channel's lanes hold the sums of their own steps
     dd += dpp<DPP_XOR1>(dd);
@@ -363,7 +371,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
     const int i = (int)(item / p.tiles);
     const Tile w = tile_of<N>(p, (int)(item % p.tiles));
     const int mine = (int)(threadIdx.x & (WAVE - 1)) / LANES;
-    const int part = (int)blockIdx.y, t0 = part * p.part;
+    const int part = (int)blockIdx.y + 1, t0 = part * p.part;          // what the first one does nobody asks for
     const int t1 = p.steps - t0 < p.part ? p.steps : t0 + p.part;
     const int length = scan_length(p, i);
     const int end = t1 < length ? t1 : length;
