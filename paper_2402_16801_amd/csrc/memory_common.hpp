@@ -32,35 +32,6 @@ template <> struct Elem<_Float16> {
 // address in global memory, so only elements are aligned.
 template <typename E, int V> struct alignas(sizeof(E)) Pack { E v[V]; };
 
-// loads `count` (uniform or not) of V elements, 0 for the rest: one access where all are there
-template <typename E, int V>
-__device__ __forceinline__ void load_row(const E* p, int count, float (&out)[V])
-{
-    if (count >= V) {
-        const Pack<E, V> q = *reinterpret_cast<const Pack<E, V>*>(p);
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = Elem<E>::up(q.v[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = j < count ? Elem<E>::up(p[j]) : 0.0f;
-    }
-}
-
-template <typename E, int V>
-__device__ __forceinline__ void store_row(E* p, int count, const float (&in)[V])
-{
-    if (count >= V) {
-        Pack<E, V> q;
-#pragma unroll
-        for (int j = 0; j < V; ++j) q.v[j] = Elem<E>::down(in[j]);
-        *reinterpret_cast<Pack<E, V>*>(p) = q;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (j < count) p[j] = Elem<E>::down(in[j]);
-    }
-}
-
 // a view on the device
 template <typename P> struct Seq {
     P* data;

@@ -410,7 +410,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
 // Carries the state through the parts: starts[part] turns from what the part does into the state at its start.  Backward in
 // time for the gradient of the state.  A block is a tile of an environment; each of its wavefronts takes a run of
 // parts, first adds up what they do together, and, once it knows what the runs before it do, goes through them again.
-// One trip to memory for up to 192 parts (157 parts: CARRY_TIME us; 22 us where one wavefront makes one for every eight).
+// One trip to memory for up to 192 parts (157 parts: 10.6 us; 22 where one wavefront makes one for every eight).
 constexpr int CARRY_WAVES = 16;
 template <typename E, int N, bool BACK>
 __global__ __launch_bounds__(CARRY_WAVES* WAVE) void k_scan_carry(const ScanParams<E> p)
@@ -617,8 +617,9 @@ static ScanParts scan_parts(const craftax_scan_args* a, int64_t want)
     return parts == 1 ? ScanParts{a->steps, 1} : ScanParts{(int)part, (int)parts};
 }
 
-// Parts that are few enough for every wavefront to go through them: OWN_MEASURED.
-constexpr int OWN_STARTS = 16;
+// Parts that are few enough for every wavefront to go through them: 5 parts 28 us where the kernel between made it 37, 32 parts 41
+// and 42, 53 parts 29 and 29.
+constexpr int OWN_STARTS = 32;
 static unsigned carry_threads(int parts) { return (unsigned)(parts < CARRY_WAVES ? parts : CARRY_WAVES) * WAVE; }
 
 // States above this size (three quarters of the last-level cache) would push each other out of it between two tokens: 268 MB
@@ -651,15 +652,29 @@ static ScanSpace scan_space(const craftax_scan_args* a, bool backward)
     const ScanTiles t = scan_tiles(a);
     ScanSpace s{};
     if (backward) {
-        // wavefronts of a block: as many as leave no more than a fifth of them without a tile
+        // wavefronts of a block: as many as leave no more than a fifth of them without a tile, and fewer where more
+        // parts of smaller blocks fit, which are shorter by a fifth at least (333 steps of 19 environments of 200 channels and 32
+        // states: 73 us with blocks of two in four parts, 84 with blocks of four in three)
         s.waves = SCAN_BACK_WAVES;
         while (s.waves > 1 && ceil_div(t.group_tiles, s.waves) * s.waves * 4 > t.group_tiles * 5) s.waves /= 2;
-        s.group_blocks = (int)ceil_div(t.group_tiles, s.waves);
         // Blocks are to be there all at once: a few more than that take twice the time.  Too few environments are split into parts
         // (the walk before costs a third); of too many, a block takes several one after the other, which also keeps the rows
         // of partial sums few.
-        const int64_t room = SCAN_BACK_FILL / s.waves, each = (int64_t)a->groups * s.group_blocks;
-        s.parts = scan_parts(a, room / (each * a->n));
+        int64_t room, each;
+        auto split = [&](int waves) {
+            room = SCAN_BACK_FILL / waves;
+            each = (int64_t)a->groups * ceil_div(t.group_tiles, waves);
+            return scan_parts(a, room / (each * a->n));
+        };
+        s.parts = split(s.waves);
+        while (s.waves > 1 && s.parts.parts > 1) {
+            const ScanParts half = split(s.waves / 2);
+            if (half.part * 5 > s.parts.part * 4) break;
+            s.waves /= 2;
+            s.parts = half;
+        }
+        s.parts = split(s.waves);           // room and each are those of the blocks taken
+        s.group_blocks = (int)ceil_div(t.group_tiles, s.waves);
         const int64_t side = each < room ? room / each : 1, turns = ceil_div(a->n, side);
         s.rows = (int)ceil_div(a->n, turns) * s.parts.parts;
     } else {

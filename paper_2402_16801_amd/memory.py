@@ -17,7 +17,7 @@ of the scan float32; a convolution's state has the type of its input.
 
 Argument marshalling only (in csrc/marshal.cpp): outputs and workspaces are allocated, the work runs
 in the HIP kernels, on the current stream of the tensors' device.  `conv`, `scan` and `norm` are the
-same operators as differentiable functions.
+same operators as functions that can be differentiated once.
 """
 from __future__ import annotations
 
@@ -25,6 +25,7 @@ import ctypes
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 from .binding import CraftaxError
@@ -156,6 +157,7 @@ class _Conv(torch.autograd.Function):
         return y, out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dstate):
         x, weight, bias, state, first, lengths = ctx.saved_tensors
         g = causal_conv_backward(_side_by_side(dy, x), x, weight, bias, state=state, first=first, lengths=lengths, silu=ctx.silu,
@@ -173,6 +175,7 @@ class _Scan(torch.autograd.Function):
         return y, out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dstate):
         saved, x, delta, a, b, c, d, z, delta_bias, state, first, lengths = ctx.saved_tensors
         g = selective_scan_backward(_side_by_side(dy, x), saved, x, delta, a, b, c, d=d, z=z, delta_bias=delta_bias, softplus=ctx.softplus,
@@ -188,6 +191,7 @@ class _Norm(torch.autograd.Function):
         return residual_norm(y, residual, gate=gate, post_weight=post_weight, scale=scale, pre_weight=pre_weight, **ctx.how)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, du):
         y, residual, gate, post_weight, scale, pre_weight = ctx.saved_tensors
         g = residual_norm_backward(_side_by_side(dout, residual), _side_by_side(du, y), y, residual, gate=gate, post_weight=post_weight,
