@@ -150,10 +150,10 @@ template <typename E, int V, int AHEAD> struct Stream {
     const E *next, *last;
     int64_t step;
     Pack<E, V> raw[AHEAD];
-    __device__ __forceinline__ void refill(int a)
+    template <bool MORE = false> __device__ __forceinline__ void refill(int a)       // MORE: there is a step behind this one
     {
         fetch<E, V>(raw[a], next);
-        next = next == last ? last : next + step;
+        next = !MORE && next == last ? last : next + step;
     }
     __device__ __forceinline__ void start(const Seq<const E>& q, int t, int end, int i, int c)
     {
@@ -169,10 +169,10 @@ template <int AHEAD> struct Begins {
     const uint8_t *next, *last;
     int64_t step;
     uint32_t flag[AHEAD];
-    __device__ __forceinline__ void refill(int a)
+    template <bool MORE = false> __device__ __forceinline__ void refill(int a)
     {
         flag[a] = *next;
-        next = next == last ? last : next + step;
+        next = !MORE && next == last ? last : next + step;
     }
     __device__ __forceinline__ void start(const Seq<const uint8_t>& q, int t, int end, int i)
     {
@@ -352,10 +352,12 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams
                 if (CUTS) begins.start(p.first, t0, live, i);
                 E* to = p.dx.at(t0, i) + w.c;            // of the oldest input in the window, once that is in the stretch
                 auto one = [&](int t, const Pack<E, V>& raw_x, const Pack<E, V>& raw_dy, bool begin, auto counts) {
-                    float x[V], dy[V], now[V];
+                    float x[V], dy[V], now[V], grad[V];
                     expand<E, V>(raw_x, x);
                     expand<E, V>(raw_dy, dy);
-                    if (CUTS) {
+                    // most steps of a wavefront are in nobody's first K - 1 of an episode and run like those without begins
+                    const bool early = CUTS && __any(begin || age < K - 1);
+                    if (early) {
                         age = begin ? 0 : age < K - 1 ? age + 1 : K - 1;
                         if (begin) clear<K, V>(win);
                     }
@@ -364,15 +366,26 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams
                         const float v = taps.sum(win, x[j], j), g = sigmoid(v), slope = g * __builtin_fmaf(v, 1.0f - g, 1.0f);
                         const float dp = dy[j] * (p.silu ? slope : 1.0f);
                         now[j] = taps.w[K - 1][j] * dp;
-#pragma unroll
-                        for (int k = 0; k < K - 1; ++k)
-                            due[k][j] = __builtin_fmaf(taps.w[k][j], !CUTS || age >= K - 1 - k ? dp : 0.0f, due[k][j]);
+                        grad[j] = dp;
                         if (decltype(counts)::value) {
                             db[j] += dp;
 #pragma unroll
                             for (int k = 0; k < K - 1; ++k) dw[k][j] = __builtin_fmaf(dp, win[k][j], dw[k][j]);
                             dw[K - 1][j] = __builtin_fmaf(dp, x[j], dw[K - 1][j]);
                         }
+                    }
+                    if (!early) {
+#pragma unroll
+                        for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                            for (int j = 0; j < V; ++j) due[k][j] = __builtin_fmaf(taps.w[k][j], grad[j], due[k][j]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < K - 1; ++k)
+                            if (age >= K - 1 - k) {
+#pragma unroll
+                                for (int j = 0; j < V; ++j) due[k][j] = __builtin_fmaf(taps.w[k][j], grad[j], due[k][j]);
+                            }
                     }
                     // the oldest input, t - (K - 1), is complete
                     const int s = t - (K - 1);
@@ -389,22 +402,28 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams
                     pin(db);
                     __builtin_amdgcn_sched_barrier(0);
                 };
-                auto streamed = [&](int t, int a) {
+                auto streamed = [&](int t, int a, auto more) {
+                    constexpr bool MORE = decltype(more)::value;
                     const Pack<E, V> raw_x = in_x.raw[a], raw_dy = in_dy.raw[a];
                     const bool begin = CUTS && begins.flag[a] != 0;
-                    in_x.refill(a);
-                    in_dy.refill(a);
-                    if (CUTS) begins.refill(a);
+                    in_x.template refill<MORE>(a);
+                    in_dy.template refill<MORE>(a);
+                    if (CUTS) begins.template refill<MORE>(a);
                     one(t, raw_x, raw_dy, begin, std::true_type{});
                 };
                 int t = t0;
+                // what is read ahead by these is in the stretch and not its last step
+                for (; t + 2 * AHEAD < live; t += AHEAD) {
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a) streamed(t + a, a, std::true_type{});
+                }
                 for (; t + AHEAD <= live; t += AHEAD) {
 #pragma unroll
-                    for (int a = 0; a < AHEAD; ++a) streamed(t + a, a);
+                    for (int a = 0; a < AHEAD; ++a) streamed(t + a, a, std::false_type{});
                 }
 #pragma unroll
                 for (int a = 0; a < AHEAD - 1; ++a)
-                    if (t + a < live) streamed(t + a, a);
+                    if (t + a < live) streamed(t + a, a, std::false_type{});
                 // steps behind the stretch, for its last inputs
                 for (t = live; t < end; ++t) {
                     Pack<E, V> raw_x, raw_dy;
@@ -515,7 +534,8 @@ static int stretch_of(int steps, int64_t threads_per_step, int64_t threads)
     return (int)(s < steps ? s : steps);
 }
 
-constexpr int64_t CONV_FILL = (int64_t)CHIP_SIMDS * 4 * WAVE;     // four wavefronts per SIMD
+constexpr int64_t CONV_FILL = (int64_t)CHIP_SIMDS * 4 * WAVE;          // four wavefronts per SIMD
+constexpr int64_t CONV_BACK_FILL = (int64_t)CHIP_SIMDS * 2 * WAVE;     // two of k_conv_backward, what the registers leave room for
 
 // calls f with the taps and the channels per thread as constants
 template <int WIDE, typename F> static void with_taps(const craftax_conv_args* a, F&& f)
@@ -570,9 +590,9 @@ static ConvBack conv_back(const craftax_conv_args* a)
     const int lanes = 1 << b.lanes_log2, rows = CONV_THREADS / lanes;
     b.x = (unsigned)ceil_div(b.vectors, lanes);
     const int64_t wide = (int64_t)b.x * lanes;
-    b.stretch = stretch_of(a->steps, wide * a->n, CONV_FILL);
+    b.stretch = stretch_of(a->steps, wide * a->n, CONV_BACK_FILL);
     const int64_t items = (int64_t)a->n * ceil_div(a->steps, b.stretch);
-    const int64_t most = ceil_div(CONV_FILL, wide * rows);       // no more partial rows than fill the chip
+    const int64_t most = ceil_div(CONV_BACK_FILL, wide * rows);       // no more partial rows than fill the chip
     const int64_t y = ceil_div(items, rows);
     b.y = (unsigned)(y < most ? y : most);
     return b;
