@@ -1,10 +1,13 @@
 // Short causal convolution of every channel with an activation: whole sequences, single tokens and the
 // backward pass.
 //
-// Bound by memory: 2 (forward) or 3 (backward) activations move per step and channel against about 12
-// and 30 instructions.  A thread owns four neighbouring channels of one environment
+//   p_t = bias + sum over k of weight[k] x_(t - taps + 1 + k), of inputs since the last begin of an episode,  y = p sigmoid(p)
+//
+// Bound by memory: 2 (forward) or 3 (backward) activations move per step and channel against 18 and about 40
+// vector instructions.  A thread owns four neighbouring channels of one environment (eight of 16-bit types were no faster)
 // and walks along a stretch of steps with the last taps - 1 inputs in registers, so an input is read
-// once but for the taps - 1 in front of a stretch.  Stretches exist only to fill the chip.
+// once but for the taps - 1 in front of a stretch.  Stretches exist only to fill the chip.  Four steps are read ahead; eight
+// were no faster.
 //
 // A row whose length is no multiple of V ends with a vector that overlaps the one before it: it is loaded whole,
 // and only its own values are stored and counted.  Rows of fewer than V channels go value by value.
@@ -184,7 +187,8 @@ template <int AHEAD> struct Begins {
     }
 };
 
-// CUTS: begins of episodes are given
+// CUTS: begins of episodes are given.  64 steps of 4,096 environments of 512 channels in bfloat16: 150 us, 3.6 TB/s; 2,048
+// environments in float32 117 us, 4.6 TB/s.
 template <typename E, int K, int V, bool CUTS>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv(const ConvParams<E> p)
 {
@@ -249,7 +253,8 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv(const ConvParams<E> p)
 }
 
 // One token: the state is read and written once, 2 K activations per channel.  A thread takes several environments one
-// after the other, so that its weights (16 bytes per channel against 16 of activations) are read once.
+// after the other, so that its weights (16 bytes per channel against 16 of activations) are read once.  4,096 environments of
+// 1,024 channels in bfloat16: 15 us, 4.5 TB/s.
 template <typename E, int K, int V>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E> p)
 {
@@ -306,7 +311,9 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E>
 // forward, `due` holds the gradients of the last K - 1 inputs, of which the oldest is complete with every
 // step; a stretch goes K - 1 steps beyond its end for the inputs at its end, without counting those steps
 // for the weight.  A block sums its weight gradients in LDS and writes one partial row; rows are added in a
-// fixed order by a second kernel.
+// fixed order by a second kernel.  Two wavefronts per SIMD is what the registers leave room for (weights, their gradients,
+// both windows and what is read ahead); vector issue is at about 0.8 of the time.  64 steps of 4,096 environments of 512 channels in
+// bfloat16: 196 us, 4.1 TB/s, with begins 238.
 template <typename E, int K, int V, bool CUTS>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams<E> p)
 {

@@ -1,11 +1,18 @@
 // Between two blocks: norm after the block, gate, scale, residual, norm before the next block, in one
 // pass over a row, and the backward pass.
 //
+//   out = residual + act(gate) scale post_weight y / rms(y),  u = pre_weight out / rms(out),  rms(v) = sqrt(mean(v v) + eps)
+//
+// and backward, with g = dL/dout + (pre_weight du)' through the second norm, where the gradient through a norm of v is
+// (h - unit mean(h unit)) / rms(v) for h = weight times the gradient of its result and unit = v / rms(v).
+//
 // Bound by memory: a row is read once, kept in registers, and written once (forward 3 in, 2 out with a gate;
 // backward 5 in, 3 out).  The backward pass computes the two roots again from the row, which is there
-// anyway, so nothing is saved between the passes.  A row belongs to W wavefronts, as few as hold it with 8
-// values per lane; with one wavefront every sum stays inside it, with more the sums meet in LDS.
+// anyway, so nothing is saved between the passes.  A row belongs to W wavefronts, as few as hold it with 16
+// values per lane (backward 8); with one wavefront every sum stays inside it, with more the sums meet in LDS.
 // Blocks go on to further rows with the weights, and in the backward pass their gradients, in registers.
+// 262,144 rows of 512 values in bfloat16 with a gate: forward 250 us, 5.3 TB/s; backward 500 us, 4.3 TB/s, with vector issue
+// at about half beside it (131,072 rows in float32: 259 us, 5.2 TB/s, and 418, 5.1).
 #include "memory_api.hpp"
 #include "memory_common.hpp"
 

@@ -3,9 +3,8 @@
 //   h = exp(D a) h + D x b,  y = (c . h + d x) z sigmoid(z)      per environment, channel and state
 //
 // Work: per step and channel 3 activations are read or written (4 with a gate), and per state there are
-// an exponential and four multiplications and additions.  With 16 states that is 24 issue cycles times 16 against 6
-// to 12 bytes: vector issue bounds sequences, memory bounds single tokens (the state is read and written
-// for one step of work).
+// an exponential and four multiplications and additions: with 16 states about 320 issue cycles of a lane against 6 to 12
+// bytes.  Vector issue bounds sequences, memory bounds single tokens (the state is read and written for one step of work).
 //
 // Sequences: a lane holds four states of a channel, so N / 4 neighbouring lanes are a channel and a wavefront
 // is 64 / (N / 4) channels of one group of one environment.  It goes on by blocks of eight steps.  What a step
@@ -14,8 +13,8 @@
 // channel's lanes by folding, which leaves each lane the steps it owns.  Everything in LDS belongs to one
 // wavefront, so there are no barriers.  Where environments and channels do not fill the chip, the steps are
 // split too ("parts"): a first kernel gives every part's effect on the state (its end from zero, and the
-// sum of D, which is the exponent of the decay), a second carries the states through the parts, and the
-// third runs the parts from their own starts.
+// sum of D, which is the exponent of the decay), and a second runs the parts from their own starts, which it finds from the
+// effects of the parts before; of many parts a kernel in between does (see part_start).
 #include "memory_api.hpp"
 #include "memory_common.hpp"
 
@@ -275,7 +274,8 @@ __device__ __forceinline__ void part_start(const ScanParams<E>& p, int part, int
 // state.  SAVE: the states before every block are kept for a backward pass (streamed: they are read long after).  The
 // activations of the next block are under way while a block is computed.  Eight wavefronts to a block of threads put the
 // rows of 128 channels side by side in time.  64 steps of 4,096 environments of 512 channels in 16 bits, with a gate:
-// 740 us, with saved states 878 (998 with four wavefronts and cached stores); vector instructions issue 3/4 of the time.
+// 750 us, with saved states 875 (998 with four wavefronts and cached stores); vector instructions issue 3/4 of the time.  Where
+// wavefronts are fewer than two per SIMD, a step takes one 175 ns, its own rate of issue.
 enum ScanMode { RUN, SAVE, PART_ONLY };
 template <typename E, int N, ScanMode MODE, bool GATE>
 __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5))) void k_scan(const ScanParams<E> p)
@@ -478,7 +478,7 @@ __global__ __launch_bounds__(CARRY_WAVES* WAVE) void k_scan_carry(const ScanPara
 // Bound by the state, 2 * N * 4 bytes per channel: a thread takes four states of a channel (16 bytes, in the
 // order of memory), N / 4 neighbouring threads add up their part of y.  It goes on to further environments with
 // its rates in registers (another 16 bytes per thread otherwise), the next one's values under way.  65,536 environments of 512
-// channels and 16 states: 981 us, 4.7 TB/s (1,153 with a thread for every four states and no second environment).
+// channels and 16 states: 935 us, 4.9 TB/s (1,153 with a thread for every four states and no second environment).
 // STREAMED: the state passes the caches by (see TOKEN_STREAMED).
 template <typename E, int N, bool STREAMED>
 __global__ __launch_bounds__(SCAN_THREADS) void k_scan_token(const ScanParams<E> p)
@@ -623,8 +623,8 @@ constexpr int OWN_STARTS = 32;
 static unsigned carry_threads(int parts) { return (unsigned)(parts < CARRY_WAVES ? parts : CARRY_WAVES) * WAVE; }
 
 // States above this size (three quarters of the last-level cache) would push each other out of it between two tokens: 268 MB
-// streamed 109 us, through the caches 120, 2.1 GB 981 and 1,052; below it a token finds the state of the one before
-// (33 MB through the caches 13.3 us, streamed 14.4).
+// streamed 106 us, through the caches 117, 2.1 GB 924 and 998; below it a token finds the state of the one before
+// (33 MB through the caches 12.6 us, streamed 14.8).
 constexpr int64_t TOKEN_STREAMED = (int64_t)192 << 20;
 constexpr int64_t SCAN_FILL = (int64_t)CHIP_SIMDS * 5;           // wavefronts that the chip holds of k_scan,
 constexpr int64_t SCAN_BACK_FILL = (int64_t)CHIP_SIMDS * 2;      // of k_scan_back,

@@ -13,6 +13,10 @@
 // over the wavefront's channels, halving values and lanes at once; the wavefronts of a block, tiles of one group,
 // meet in LDS once per block of steps, and what the blocks of a group leave is added up by a second kernel.
 // The order is fixed, there are no atomics.
+//
+// Bound by vector issue: about 105 instructions per step of a wavefront (16 channels of 16 states), of which 20 are the states again
+// and 20 the sums over channels, at two wavefronts per SIMD, what some 230 registers leave room for.  64 steps of 4,096 environments of
+// 512 channels in bfloat16 with a gate: 2,050 us, and 50 for the second kernel.
 
 constexpr int SCAN_BACK_WAVES = 8;       // wavefronts of a block at most
 // The sums for da, dd and ddelta_bias over so many steps are added up apart before they join a wavefront's total: over
@@ -358,7 +362,8 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
     }
 }
 
-// What a part does to the gradient of the state that comes from behind it: see k_scan with PART.
+// What a part does to the gradient of the state that comes from behind it: see k_scan with PART.  No sums over channels and no
+// parameters here, a third of the time of the walk behind it.
 template <typename E, int N>
 __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParams<E> p)
 {
