@@ -3,7 +3,7 @@
 //
 //   p_t = bias + sum over k of weight[k] x_(t - taps + 1 + k), of inputs since the last begin of an episode,  y = p sigmoid(p)
 //
-// Bound by memory: 2 (forward) or 3 (backward) activations move per step and channel against 18 and about 40
+// Bound by memory: 2 (forward) or 3 (backward) activations move per step and channel against 18 and 34
 // vector instructions.  A thread owns four neighbouring channels of one environment (eight of 16-bit types were no faster)
 // and walks along a stretch of steps with the last taps - 1 inputs in registers, so an input is read
 // once but for the taps - 1 in front of a stretch.  Stretches exist only to fill the chip.  Four steps are read ahead; eight
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E>
 // step; a stretch goes K - 1 steps beyond its end for the inputs at its end, without counting those steps
 // for the weight.  A block sums its weight gradients in LDS and writes one partial row; rows are added in a
 // fixed order by a second kernel.  Two wavefronts per SIMD is what the registers leave room for (weights, their gradients,
-// both windows and what is read ahead); vector issue is at about 0.8 of the time.  64 steps of 4,096 environments of 512 channels in
+// both windows and what is read ahead); vector issue is at about two thirds of the time.  64 steps of 4,096 environments of 512 channels in
 // bfloat16: 196 us, 4.1 TB/s, with begins 238.
 template <typename E, int K, int V, bool CUTS>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams<E> p)
