@@ -152,12 +152,19 @@ template <typename T> T* dense(const Tensor* t, const char* name, std::initializ
 }
 
 // ---- outputs ----------------------------------------------------------------------------------------------
-// Laid out as t is, the channels (and the groups in front of them) side by side.
+// Laid out as t is, the channels side by side.
 Tensor like(const Tensor& t)
 {
     if (t.is_contiguous()) return at::empty(t.sizes(), t.options());
     Tensor out = at::empty_like(t);
-    if (out.stride(-1) != 1 || (out.dim() == 4 && out.stride(2) != out.size(3))) out = at::empty(t.sizes(), t.options());
+    if (out.stride(-1) != 1) out = at::empty(t.sizes(), t.options());
+    return out;
+}
+// Laid out as b or c, the groups of a token side by side, for sequences as for one token: a view has no stride for them.
+Tensor shared_like(const Tensor& t)
+{
+    Tensor out = like(t);
+    if (out.stride(-2) != out.size(-1)) out = at::empty(t.sizes(), t.options());
     return out;
 }
 Tensor like_or_none(const Tensor* t) { return t ? like(*t) : Tensor(); }
@@ -318,7 +325,7 @@ PyObject* selective_scan_backward(PyObject* const* v)
         (size_t)saved->numel() < g_lib.scan_saved(&a))
         refuse("saved is not what selective_scan(..., save=True) returned for these inputs");
     a.saved = saved->data_ptr();
-    const Tensor dx = like(x), ddelta = like(delta), da = like(rates), db = like(need(v[3], "b")), dc = like(need(v[4], "c"));
+    const Tensor dx = like(x), ddelta = like(delta), da = like(rates), db = shared_like(need(v[3], "b")), dc = shared_like(need(v[4], "c"));
     const Tensor dd = like_or_none(d), dz = like_or_none(z), dbias = like_or_none(delta_bias), dstate = like_or_none(state);
     a.dy = sequence(&need(v[13], "dy"), "dy", c, c.type);
     a.dx = place(dx, c);

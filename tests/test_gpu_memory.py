@@ -206,6 +206,35 @@ def test_scan_forgets_infinities_and_ignores_dead_steps(mem, T):
         assert bool((value[T - 7:, 2] == 0).all())
 
 
+@pytest.mark.parametrize("odd", ["b", "c", "both"])
+@pytest.mark.parametrize("token", [True, False], ids=["token", "sequence"])
+def test_scan_gradients_where_the_groups_are_the_outer_dimension(mem, token, odd):
+    """b and c as views of [groups][..][states] tensors: the gradients are those of the same values laid out in order."""
+    src = Source(45, torch.float32)
+    T, n, D, N, G = (1 if token else 19), 5, 66, 16, 2
+    t = scan_inputs(src, T, n, D, N, G, True, True)
+    dy, dstate = src.seq(T, n, D), src.normal(n, D, N)
+    _, want = ref.gradients(ref.scan, t, (dy, dstate))
+    g = scan_gpu(src, t)
+    for k in ("b", "c"):
+        if odd in (k, "both"):
+            g[k] = g[k].movedim(2, 0).contiguous().movedim(0, 2)
+    dy = plain(dy)
+    if token:
+        g.update({k: g[k][0] for k in ("x", "delta", "b", "c", "z")})
+        dy = dy[0]
+    how = {k: g[k] for k in ("d", "z", "delta_bias", "state")}
+    args = [g[k] for k in ("x", "delta", "a", "b", "c")]
+    _, _, saved = mem.selective_scan(*args, save=True, **how)
+    got = mem.selective_scan_backward(dy, saved, *args, dstate=plain(dstate), **how)
+    leaf = [v.requires_grad_(True) for v in args]
+    y, h = mem.scan(*leaf, **how)
+    auto = torch.autograd.grad([y, h], leaf, [dy, plain(dstate)])
+    for name, value, same in zip(("x", "delta", "a", "b", "c"), got, auto):
+        close("gradient of " + name, value[None] if token and name != "a" else value, want[name], N * min(T, 64) + D // G + T * n)
+        assert torch.equal(value, same), name
+
+
 def test_scan_steps_equal_the_sequence(mem):
     src = Source(21, torch.bfloat16)
     T, n, D, N, G = 40, 9, 136, 16, 2
