@@ -7,6 +7,7 @@
 #include <ATen/ATen.h>
 #include <ATen/hip/impl/HIPGuardImplMasqueradingAsCUDA.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -170,6 +171,18 @@ Tensor shared_like(const Tensor& t)
 Tensor like_or_none(const Tensor* t) { return t ? like(*t) : Tensor(); }
 void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
+// A state that the caller gave to be written.  Autograd hears of it as of PyTorch's own operations in place: what kept the state
+// for a backward pass refuses to run it, and a state with a history that the write would cut off is not taken.
+void check_writable(const Tensor& t)
+{
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        refuse("a state that requires gradients cannot be written in place: give out_state, detach the state, or call under torch.no_grad()");
+}
+void written(const Tensor& t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 Tensor bytes(size_t size, const Common& c) { return size ? at::empty({(int64_t)size}, c.options(at::kByte)) : Tensor(); }
 
 PyObject* wrap(const Tensor& t)
@@ -227,6 +240,7 @@ PyObject* causal_conv(PyObject* const* v)
     Tensor out;
     if (const Tensor* given = maybe(v[7], "out_state")) {
         a.state_out = dense<void>(given, "out_state", {c.n, a.taps - 1, c.channels}, c.type, c);
+        check_writable(*given);
         out = *given;
     } else {
         out = at::empty({c.n, a.taps < 1 ? 0 : a.taps - 1, c.channels}, c.options(c.type));
@@ -234,6 +248,7 @@ PyObject* causal_conv(PyObject* const* v)
     }
     a.y = place(y, c);
     call(g_lib.conv, a, c);
+    if (v[7] != Py_None) written(out);
     return tuple({y, out});
 }
 
@@ -295,6 +310,7 @@ PyObject* selective_scan(PyObject* const* v)
     const Tensor y = like(x);
     if (const Tensor* given = maybe(v[13], "out_state")) {
         a.state_out = dense<float>(given, "out_state", {c.n, c.channels, a.states}, at::kFloat, c);
+        check_writable(*given);
         out = *given;
     } else {
         out = at::empty({c.n, c.channels, a.states}, c.options(at::kFloat));
@@ -309,6 +325,7 @@ PyObject* selective_scan(PyObject* const* v)
     a.workspace = address(work);
     a.workspace_bytes = work.defined() ? (size_t)work.numel() : 0;
     call(g_lib.scan, a, c);
+    if (v[13] != Py_None) written(out);
     return tuple({y, out, saved});
 }
 

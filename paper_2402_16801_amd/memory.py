@@ -12,8 +12,10 @@ Sequences are [steps][n][channels], the order of rollouts; a batch-first tensor 
 side).  `first` (uint8 or bool [steps][n]) marks steps at which an episode begins, as the simulator's
 `done` does for the observation that came with it; `lengths` (int32 [n]) says how many steps of each
 environment count.  The `*_step` forms take one token, [n][channels], and update the state in place
-unless `out_state` is given.  Activations are float32, bfloat16 or float16, parameters and the states
-of the scan float32; a convolution's state has the type of its input.
+unless `out_state` is given; as with PyTorch's operations in place, a state that requires gradients is
+refused there, and a backward pass that needs the state as it was raises.  Activations are float32,
+bfloat16 or float16, parameters and the states of the scan float32; a convolution's state has the type
+of its input.
 
 Argument marshalling only (in csrc/marshal.cpp): outputs and workspaces are allocated, the work runs
 in the HIP kernels, on the current stream of the tensors' device.  `conv`, `scan` and `norm` are the
@@ -170,16 +172,18 @@ class _Scan(torch.autograd.Function):
     def forward(ctx, x, delta, a, b, c, d, z, delta_bias, state, first, lengths, softplus):
         y, out, saved = selective_scan(x, delta, a, b, c, d=d, z=z, delta_bias=delta_bias, softplus=softplus, state=state, first=first,
                                        lengths=lengths, save=True)
-        ctx.save_for_backward(saved, x, delta, a, b, c, d, z, delta_bias, state, first, lengths)
+        ctx.save_for_backward(saved, x, delta, a, b, c, d, z, delta_bias, first, lengths)
+        # not among the saved tensors: its values are in `saved`, so that it may be written before the backward pass
+        ctx.state = None if state is None else state.detach()
         ctx.softplus = softplus
         return y, out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, dstate):
-        saved, x, delta, a, b, c, d, z, delta_bias, state, first, lengths = ctx.saved_tensors
+        saved, x, delta, a, b, c, d, z, delta_bias, first, lengths = ctx.saved_tensors
         g = selective_scan_backward(_side_by_side(dy, x), saved, x, delta, a, b, c, d=d, z=z, delta_bias=delta_bias, softplus=ctx.softplus,
-                                    state=state, first=first, lengths=lengths, dstate=dstate.contiguous())
+                                    state=ctx.state, first=first, lengths=lengths, dstate=dstate.contiguous())
         return g.x, g.delta, g.a, g.b, g.c, g.d, g.z, g.delta_bias, g.state, None, None, None
 
 

@@ -599,6 +599,74 @@ def test_differentiable_functions(mem):
         close("gradient of " + name, got[name], want[name], 9 * (N * T + T * n + D))
 
 
+def _rollout_and_step(mem, operator):
+    """(a rollout from a state as a differentiable call, a step that takes a state and out_state, a fresh state, its leaves)"""
+    src = Source(91, torch.float32)
+    T, n, D, N = 6, 3, 40, 16
+    t = scan_inputs(src, T, n, D, N, 1, False, True)
+    g = scan_gpu(src, t)
+    if operator == "conv":
+        weight = plain(src.normal(D, 4)).requires_grad_(True)
+        return (lambda s: mem.conv(g["x"], weight, state=s)[0], lambda s, out=None: mem.causal_conv_step(g["x"][0], weight, None, s, out_state=out)[1],
+                plain(src.normal(n, 3, D)), weight)
+    x = g["x"].requires_grad_(True)
+    return (lambda s: mem.scan(x, g["delta"], g["a"], g["b"], g["c"], state=s)[0],
+            lambda s, out=None: mem.selective_scan_step(g["x"][0], g["delta"][0], g["a"], g["b"][0], g["c"][0], s, out_state=out)[1], g["state"], x)
+
+
+@pytest.mark.parametrize("operator", ["conv", "scan"])
+def test_a_step_between_forward_and_backward(mem, operator):
+    """A state that a rollout began with is stepped on before the backward pass.  The convolution's gradients need it as it was, so
+    that they raise as behind PyTorch's own operations in place; the scan's do not, and are what they are without the step."""
+    rollout, step, state, leaf = _rollout_and_step(mem, operator)
+    (want,) = torch.autograd.grad(rollout(state).sum(), leaf)
+    y = rollout(state)
+    step(state.clone())
+    step(state, torch.empty_like(state))
+    (same,) = torch.autograd.grad(y.sum(), leaf, retain_graph=True)
+    assert torch.equal(same, want)
+    before = state.clone()
+    assert step(state) is state and not torch.equal(state, before)
+    if operator == "conv":
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    else:
+        (same,) = torch.autograd.grad(y.sum(), leaf)
+        assert torch.equal(same, want)
+    # written as another state's place, too
+    y, other = rollout(state), state.clone()
+    step(other, state)
+    if operator == "conv":
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+
+
+@pytest.mark.parametrize("operator", ["conv", "scan"])
+def test_states_written_in_place_as_autograd_sees_them(mem, operator):
+    from paper_2402_16801_amd import binding
+    _, step, state, _ = _rollout_and_step(mem, operator)
+    version = state._version
+    step(state)
+    assert state._version == version + 1
+    step(state, torch.empty_like(state))
+    with pytest.raises(binding.CraftaxError):
+        step(state[:, :-1])
+    assert state._version == version + 1
+    for grown in (state.clone().requires_grad_(True), state.clone().requires_grad_(True) * 2):
+        kept = grown.detach().clone()
+        for where in ((grown,), (state, grown)):
+            with pytest.raises(binding.CraftaxError, match="requires gradients"):
+                step(*where)
+        torch.cuda.synchronize()
+        assert torch.equal(grown, kept) and step(grown, torch.empty_like(state)) is not grown
+        with torch.no_grad():
+            assert step(grown) is grown and not torch.equal(grown, kept)
+    with torch.inference_mode():
+        plain_state = state.clone()
+        assert step(plain_state) is plain_state
+    assert step(plain_state) is plain_state
+
+
 # ---- refusals ---------------------------------------------------------------------------------------------
 
 def test_refusals(mem):
