@@ -98,6 +98,13 @@ template <int CHUNKS, int V, Fit FIT> struct RowPlace {
     {
         return FIT == WHOLE || (j >= old[c] && (FIT == TAIL || j < channels));
     }
+    // s with value j's product added where it counts in this lane.  A selection, not a product with 0: the values that do not count may
+    // be infinite.  Of several chunks the first half is filled in every row (see with_row) and needs none.
+    __device__ __forceinline__ float add(int c, int j, float a, float b, float s) const
+    {
+        const float sum = __builtin_fmaf(a, b, s);
+        return c < CHUNKS / 2 || mine(c, j) ? sum : s;
+    }
 };
 
 template <typename P, int CHUNKS, int V, Fit FIT>
@@ -171,8 +178,12 @@ template <typename P, int CHUNKS, int V> __device__ __forceinline__ void pin(Pac
     __builtin_memcpy(q, words, sizeof(q));
 }
 
+// Wavefronts per SIMD at most: rows of 16 values per lane that do not fill the lanes are faster with two than with the three that
+// their registers leave room for (131,072 rows of 1,000 bfloat16 264 us, 270 with three; 40,000 of 3,001 float16 285 and 290).
+template <typename E, int CHUNKS, Fit FIT> constexpr int norm_waves() { return FIT == TAIL && CHUNKS * 16 / sizeof(E) > 8 ? 2 : 8; }
+
 template <typename E, typename R, int W, int CHUNKS, Fit FIT>
-__global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<E, R> p)
+__global__ __launch_bounds__(RowBlock<W>::THREADS) __attribute__((amdgpu_waves_per_eu(2, norm_waves<E, CHUNKS, FIT>()))) void k_norm(const NormParams<E, R> p)
 {
     constexpr int V = 16 / sizeof(E), ROWS = RowBlock<W>::ROWS;
     __shared__ float slots[2][ROWS][W];
@@ -193,11 +204,6 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
     load_weight(w, p.post_weight, w1);
     load_weight(w, p.scale, scale);
     load_weight(w, p.pre_weight, w2);
-    float share[CHUNKS][V];                    // 1 where a value counts in this lane, else 0
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-        for (int j = 0; j < V; ++j) share[c][j] = w.mine(c, j) ? 1.0f : 0.0f;
     const float mean = 1.0f / (float)p.channels;
     for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += stride) {
         const uint32_t row = base + which;
@@ -212,7 +218,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = __builtin_fmaf(FIT == WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s);
             root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         float s = 0.0f;
@@ -222,7 +228,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm(const NormParams<
             for (int j = 0; j < V; ++j) {
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * root * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = __builtin_fmaf(FIT == WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
+                s = w.add(c, j, r[c][j], r[c][j], s);
             }
         root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
         // the next row's values, waited for in front of the stores: behind them the wait would be for those too
@@ -283,11 +289,6 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
     load_weight(w, p.post_weight, w1);
     load_weight(w, p.scale, scale);
     load_weight(w, p.pre_weight, w2);
-    float share[CHUNKS][V];                    // 1 where a value counts in this lane, else 0
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-        for (int j = 0; j < V; ++j) share[c][j] = w.mine(c, j) ? 1.0f : 0.0f;
     float d1[CHUNKS][V] = {}, ds[CHUNKS][V] = {}, d2[CHUNKS][V] = {};
     const float mean = 1.0f / (float)p.channels;
     auto one = [&](uint32_t base, Raw& mine, Raw& next) {
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = __builtin_fmaf(FIT == WHOLE ? y[c][j] : y[c][j] * share[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s);
             root_y = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         // out again, its root, and the sum over the row of (du w2) (out root)
@@ -319,7 +320,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 y[c][j] *= root_y;                                   // from here on without its scale
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = __builtin_fmaf(FIT == WHOLE ? r[c][j] : r[c][j] * share[c][j], r[c][j], s);
+                s = w.add(c, j, r[c][j], r[c][j], s);
             }
         const float root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
 #pragma unroll
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 r[c][j] *= root;
                 d2[c][j] = __builtin_fmaf(du[c][j] * on, r[c][j], d2[c][j]);
                 du[c][j] *= w2[c][j];
-                m = __builtin_fmaf(FIT == WHOLE ? du[c][j] : du[c][j] * share[c][j], r[c][j], m);
+                m = w.add(c, j, du[c][j], r[c][j], m);
             }
         m = row_sum<W>(m, slots[2][which]) * mean;
         float q = 0.0f;
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
                 d1[c][j] = __builtin_fmaf(dv * on, y[c][j], d1[c][j]);
                 du[c][j] = dv * w1[c][j];
-                q = __builtin_fmaf(FIT == WHOLE ? du[c][j] : du[c][j] * share[c][j], y[c][j], q);
+                q = w.add(c, j, du[c][j], y[c][j], q);
             }
         if (p.post_weight) {
             q = row_sum<W>(q, slots[3][which]) * mean;
@@ -491,6 +492,7 @@ template <bool BACKWARD, typename F> static void with_row(const craftax_norm_arg
                 else if (a->channels >= V) f(e, r, wc, count, std::integral_constant<Fit, TAIL>{});
                 else if constexpr (W == 1 && C == 1) f(e, r, wc, count, std::integral_constant<Fit, SHORT>{});
             };
+            // More than one chunk only where half as many would not hold the row: the first half is filled.
             constexpr int EIGHT = 8 / V;          // chunks of eight values
             if (V < 8 && a->channels <= W * WAVE * V) whole(std::integral_constant<int, 1>{});
             else if ((BACKWARD && W < 8) || a->channels <= W * WAVE * 8) whole(std::integral_constant<int, EIGHT>{});

@@ -498,6 +498,49 @@ def test_norm_of_rows_of_zeros_and_of_two_dimensions(mem):
         close("gradient of " + name, getattr(got, name), want[name], 16)
 
 
+def alike(what, got, want, terms):
+    """close(), where the definition is finite; where it is infinite or no number, the same."""
+    got64 = got.detach().cpu().double()
+    assert torch.equal(torch.isnan(got64), torch.isnan(want)), f"{what}: {int(torch.isnan(got64).sum())} values are no numbers, by its definition {int(torch.isnan(want).sum())}"
+    ends = torch.isinf(want)
+    assert torch.equal(torch.isinf(got64), ends) and torch.equal(got64[ends], want[ends]), f"{what}: infinities differ"
+    finite = torch.isfinite(want)
+    close(what, torch.where(finite, got.detach().cpu(), 0.0), torch.where(finite, want, 0.0), terms)
+
+
+# lengths that fill the lanes of a row (512), that do not in one of one, two and four chunks a lane, that leave lanes without a value, and short ones
+@pytest.mark.parametrize("D", [3, 7, 20, 200, 300, 512, 513, 1000, 1345, 2050, 4097, 8191])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_of_rows_with_an_infinity(mem, dtype, D):
+    """An infinity makes the root of its row 0: the row's other values are the residual's, or 0, wherever it lies.  One in the
+    gradient of u is in that of every value of its row and of no other row."""
+    src = Source(D, TYPES[dtype])
+    places = sorted({0, 1, D // 2, max(0, D - 9), D - 2, D - 1})
+    n = len(places) + 1                                   # the last row is finite
+    t = {"y": src.seq(1, n, D), "residual": src.seq(1, n, D), "gate": src.seq(1, n, D), "pre_weight": 1 + src.normal(D, spread=0.1),
+         "post_weight": 1 + src.normal(D, spread=0.1)}
+    t = {k: v.float().double() for k, v in t.items()}
+    du = src.seq(1, n, D)
+
+    def put(v):
+        v = v.clone()
+        for row, place in enumerate(places):
+            v[0, row, place] = float("inf") if row % 2 else -float("inf")
+        return v
+
+    for where, post in (("y", True), ("y", False), ("residual", True)):
+        bad = {k: put(v) if k == where else v for k, v in t.items() if post or k != "post_weight"}
+        out, u = ref.norm(**bad)
+        got_out, got_u = mem.residual_norm(**{k: plain(v) if "weight" in k else src.gpu(v) for k, v in bad.items()})
+        alike(f"out, infinity in {where}", got_out, out, 4)
+        alike(f"u, infinity in {where}", got_u, u, 4)
+    t.pop("post_weight")
+    _, want = ref.gradients(ref.norm, t, (None, put(du)))
+    got = mem.residual_norm_backward(None, src.gpu(put(du)), src.gpu(t["y"]), src.gpu(t["residual"]), gate=src.gpu(t["gate"]), pre_weight=plain(t["pre_weight"]))
+    for name in ("y", "residual", "gate"):
+        alike("gradient of " + name, getattr(got, name), want[name], 16)
+
+
 def test_norm_gradients_against_differences(mem):
     """As for the scan: central differences of step 2^-7 along a random direction, good to 1 percent."""
     src = Source(19, torch.float32)
