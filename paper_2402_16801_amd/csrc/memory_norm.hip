@@ -293,7 +293,12 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
     const float mean = 1.0f / (float)p.channels;
     auto one = [&](uint32_t base, Raw& mine, Raw& next) {
         const uint32_t row = base + which;
-        const float on = row < p.rows ? 1.0f : 0.0f;       // a row that is none adds nothing to the weights' gradients
+        // a wavefront without a row goes along with the last one: that adds nothing to the weights' gradients, be it infinite
+        const bool on = ROWS == 1 || row < p.rows;
+        auto add = [&](float a, float b, float& sum) {
+            const float with = __builtin_fmaf(a, b, sum);
+            sum = on ? with : sum;
+        };
         if (AHEAD == 0) load(mine, base);
         float y[CHUNKS][V], r[CHUNKS][V], g[CHUNKS][V] = {}, du[CHUNKS][V], dr[CHUNKS][V] = {};
         expand(mine.y, y);
@@ -328,7 +333,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 r[c][j] *= root;
-                d2[c][j] = __builtin_fmaf(du[c][j] * on, r[c][j], d2[c][j]);
+                add(du[c][j], r[c][j], d2[c][j]);
                 du[c][j] *= w2[c][j];
                 m = w.add(c, j, du[c][j], r[c][j], m);
             }
@@ -342,9 +347,9 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 dr[c][j] = d;
                 const float value = gate_value(g[c][j], p.gate_act), act = gated ? value : 1.0f;
                 const float v = y[c][j] * w1[c][j], dv = d * scale[c][j] * act;
-                ds[c][j] = __builtin_fmaf(d * v * on, act, ds[c][j]);
+                add(d * v, act, ds[c][j]);
                 g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
-                d1[c][j] = __builtin_fmaf(dv * on, y[c][j], d1[c][j]);
+                add(dv, y[c][j], d1[c][j]);
                 du[c][j] = dv * w1[c][j];
                 q = w.add(c, j, du[c][j], y[c][j], q);
             }

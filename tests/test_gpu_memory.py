@@ -541,6 +541,20 @@ def test_norm_of_rows_with_an_infinity(mem, dtype, D):
         alike("gradient of " + name, getattr(got, name), want[name], 16)
 
 
+@pytest.mark.parametrize("rows", [1, 2, 3, 5])
+@pytest.mark.parametrize("D", [6, 512, 700, 1345])
+def test_norm_gradients_of_weights_with_an_infinity_in_the_last_row(mem, D, rows):
+    """Rows that a block has no place filled with add nothing: an infinite gradient in the last row is in the weights' gradients once."""
+    src = Source(100 * D + rows, torch.float32)
+    t = {"y": src.seq(1, rows, D), "residual": src.seq(1, rows, D), "scale": src.normal(D), "pre_weight": (1 + src.normal(D, spread=0.1)).float().double()}
+    du = src.seq(1, rows, D)
+    du[0, -1, D // 2] = float("inf")
+    _, want = ref.gradients(ref.norm, t, (None, du))
+    got = mem.residual_norm_backward(None, plain(du), plain(t["y"]), plain(t["residual"]), scale=plain(t["scale"]), pre_weight=plain(t["pre_weight"]))
+    for name in ("scale", "pre_weight"):
+        alike("gradient of " + name, getattr(got, name), want[name], rows + 16)
+
+
 def test_norm_gradients_against_differences(mem):
     """As for the scan: central differences of step 2^-7 along a random direction, good to 1 percent."""
     src = Source(19, torch.float32)
