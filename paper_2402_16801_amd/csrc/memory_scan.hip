@@ -285,7 +285,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
     __shared__ float4 shared_lds[SCAN_WAVES][BLOCK * N / 2];
     __shared__ float2 step_lds[SCAN_WAVES][BLOCK * CHANNELS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + wave;
+    const int64_t item = spread_block() * SCAN_WAVES + wave;
     if (item >= (int64_t)p.n * p.tiles) return;
     const int i = (int)(item / p.tiles);
     const Tile w = tile_of<N>(p, (int)(item % p.tiles));
@@ -703,7 +703,6 @@ static ScanSpace scan_space(const craftax_scan_args* a, bool backward)
 size_t scan_workspace_bytes(const craftax_scan_args* a, bool backward)
 {
     if (!scan_shape_ok(a)) return 0;
-    if (!backward && a->steps == 1 && !a->saved) return 0;
     return scan_space(a, backward).bytes;
 }
 
@@ -740,45 +739,53 @@ static int check_workspace(const void* workspace, size_t given, size_t need, con
     return CRAFTAX_OK;
 }
 
+// whether the kernel for one token takes the call
+static bool scan_token(const craftax_scan_args* a) { return a->steps == 1 && !a->saved && token_fits(a->channels, a->states); }
+
 int scan(const craftax_scan_args* a, void* stream, const char** why)
 {
     if (int rc = scan_check(a, false, why)) return rc;
     if (int rc = check_workspace(a->workspace, a->workspace_bytes, scan_workspace_bytes(a, false), why)) return rc;
     const hipStream_t st = (hipStream_t)stream;
+    int rc = CRAFTAX_OK;
     with_type(a->dtype, [&](auto e) {
         using E = decltype(e);
         ScanParams<E> p = scan_params<E>(a);
         with_states(a->states, [&](auto states) {
             constexpr int N = decltype(states)::value;
-            if (a->steps == 1 && !a->saved) {
+            if (scan_token(a)) {
                 // environments side by side: as many threads as the chip holds, each with several of them in turn, or all
                 const int64_t per_env = (int64_t)a->channels * (N / 4), side = ceil_div(TOKEN_FILL * WAVE, per_env);
                 p.part = (int)(side < a->n ? side : a->n);
                 const dim3 grid((unsigned)ceil_div(p.part * per_env, SCAN_THREADS));
                 if (a->n * per_env * (int64_t)sizeof(float4) > TOKEN_STREAMED) hipLaunchKernelGGL((k_scan_token<E, N, true>), grid, dim3(SCAN_THREADS), 0, st, p);
                 else hipLaunchKernelGGL((k_scan_token<E, N, false>), grid, dim3(SCAN_THREADS), 0, st, p);
+                rc = launched(why);
                 return;
             }
             const ScanSpace s = scan_space(a, false);
             char* base = static_cast<char*>(a->workspace);
             p.part = s.parts.part; p.parts = s.parts.parts;
-            const unsigned blocks = (unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES);
-            const dim3 grid(blocks, (unsigned)p.parts);
+            const Spread blocks = spread(ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES), SCAN_THREADS);
+            const dim3 grid(blocks.x, (unsigned)p.parts, blocks.z);
             if (p.parts > 1) {
                 p.starts = reinterpret_cast<float4*>(base + s.starts);
                 p.decays = reinterpret_cast<float2*>(base + s.decays);
-                hipLaunchKernelGGL((k_scan<E, N, PART_ONLY, false>), dim3(blocks, (unsigned)p.parts - 1), dim3(SCAN_THREADS), 0, st, p);
+                hipLaunchKernelGGL((k_scan<E, N, PART_ONLY, false>), dim3(blocks.x, (unsigned)p.parts - 1, blocks.z), dim3(SCAN_THREADS), 0, st, p);
+                if ((rc = launched(why))) return;
                 // a state that is written in place is not there any more when the last parts ask for it
                 p.own_starts = p.parts <= OWN_STARTS && !(p.state_in && p.state_in == p.state_out);
                 if (!p.own_starts) hipLaunchKernelGGL((k_scan_carry<E, N, false>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
+                if ((rc = launched(why))) return;
             }
             if (p.saved && p.z.data) hipLaunchKernelGGL((k_scan<E, N, SAVE, true>), grid, dim3(SCAN_THREADS), 0, st, p);
             else if (p.saved) hipLaunchKernelGGL((k_scan<E, N, SAVE, false>), grid, dim3(SCAN_THREADS), 0, st, p);
             else if (p.z.data) hipLaunchKernelGGL((k_scan<E, N, RUN, true>), grid, dim3(SCAN_THREADS), 0, st, p);
             else hipLaunchKernelGGL((k_scan<E, N, RUN, false>), grid, dim3(SCAN_THREADS), 0, st, p);
+            rc = launched(why);
         });
     });
-    return launched(why);
+    return rc;
 }
 
 int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
@@ -787,6 +794,7 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
     if (int rc = check_workspace(a->workspace, a->workspace_bytes, scan_workspace_bytes(a, true), why)) return rc;
     const hipStream_t st = (hipStream_t)stream;
     const ScanSpace s = scan_space(a, true);
+    int rc = CRAFTAX_OK;
     with_type(a->dtype, [&](auto e) {
         using E = decltype(e);
         ScanParams<E> p = scan_params<E>(a);
@@ -799,21 +807,26 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
         with_states(a->states, [&](auto states) {
             constexpr int N = decltype(states)::value;
             if (p.parts > 1) {
-                const unsigned blocks = (unsigned)ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES);
-                hipLaunchKernelGGL((k_scan_back_part<E, N>), dim3(blocks, (unsigned)p.parts - 1), dim3(SCAN_THREADS), 0, st, p);
+                const Spread blocks = spread(ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES), SCAN_THREADS);
+                hipLaunchKernelGGL((k_scan_back_part<E, N>), dim3(blocks.x, (unsigned)p.parts - 1, blocks.z), dim3(SCAN_THREADS), 0, st, p);
+                if ((rc = launched(why))) return;
                 p.own_starts = p.parts <= OWN_STARTS;
                 if (!p.own_starts) hipLaunchKernelGGL((k_scan_carry<E, N, true>), dim3((unsigned)(a->n * p.tiles)), dim3(carry_threads(p.parts)), 0, st, p);
+                if ((rc = launched(why))) return;
             }
-            const dim3 grid((unsigned)((int64_t)(s.rows / p.parts) * a->groups * s.group_blocks), (unsigned)p.parts);
+            const Spread blocks = spread((int64_t)(s.rows / p.parts) * a->groups * s.group_blocks, s.waves * WAVE);
+            const dim3 grid(blocks.x, (unsigned)p.parts, blocks.z);
             if (p.z.data) hipLaunchKernelGGL((k_scan_back<E, N, true>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
             else hipLaunchKernelGGL((k_scan_back<E, N, false>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
-            const int64_t values = (int64_t)a->steps * a->n * a->groups * 2 * N;
-            hipLaunchKernelGGL((k_scan_shared<E, N>), dim3((unsigned)ceil_div(values, SCAN_THREADS)), dim3(SCAN_THREADS), 0, st, p,
-                               seq<E>(a->db), seq<E>(a->dc));
+            if ((rc = launched(why))) return;
+            const Spread sums = spread(ceil_div((int64_t)a->steps * a->n * a->groups * 2 * N, SCAN_THREADS), SCAN_THREADS);
+            hipLaunchKernelGGL((k_scan_shared<E, N>), dim3(sums.x, 1, sums.z), dim3(SCAN_THREADS), 0, st, p, seq<E>(a->db), seq<E>(a->dc));
+            if ((rc = launched(why))) return;
             sum_rows(p.weight_part, s.rows, (int64_t)a->channels * (N + 2), PutScan<N>{a->da, a->dd, a->ddelta_bias}, st);
+            rc = launched(why);
         });
     });
-    return launched(why);
+    return rc;
 }
 
 }  // namespace host

@@ -111,8 +111,10 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
     float4* step_lds = lds + waves * (BLOCK * N / 2) + wave * (BLOCK * CHANNELS);        // [step][channel]: D, D x, dy, x
     float* sum_lds = reinterpret_cast<float*>(lds + waves * (BLOCK * N / 2 + BLOCK * CHANNELS));   // [turn][wave][step][2 N]
     const int blocks = given.groups * given.group_blocks;
-    const int group_block = (int)(blockIdx.x % (unsigned)blocks);
-    const int env_row = (int)(blockIdx.x / (unsigned)blocks), env_rows = given.rows / given.parts;
+    const unsigned block = (unsigned)spread_block();
+    const int group_block = (int)(block % (unsigned)blocks);
+    const int env_row = (int)(block / (unsigned)blocks), env_rows = given.rows / given.parts;
+    if (env_row >= env_rows) return;
     const int group = group_block / given.group_blocks, in_group = (group_block % given.group_blocks) * waves + wave;
     const bool works = in_group < given.group_tiles;          // the other wavefronts only keep the barriers
     const Tile w = tile_of<N>(given, group * given.group_tiles + (works ? in_group : given.group_tiles - 1));
@@ -371,7 +373,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
     __shared__ float4 shared_lds[SCAN_WAVES][BLOCK * N / 2];
     __shared__ float2 step_lds[SCAN_WAVES][BLOCK * CHANNELS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + wave;
+    const int64_t item = spread_block() * SCAN_WAVES + wave;
     if (item >= (int64_t)p.n * p.tiles) return;
     const int i = (int)(item / p.tiles);
     const Tile w = tile_of<N>(p, (int)(item % p.tiles));
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
 template <typename E, int N>
 __global__ __launch_bounds__(SCAN_THREADS) void k_scan_shared(const ScanParams<E> p, Seq<E> db, Seq<E> dc)
 {
-    const int64_t at = (int64_t)blockIdx.x * SCAN_THREADS + threadIdx.x;
+    const int64_t at = spread_block() * SCAN_THREADS + threadIdx.x;
     const int value = (int)(at % (2 * N));
     const int64_t row = at / (2 * N);                  // (step, environment, group)
     if (row >= (int64_t)p.steps * p.n * p.groups) return;

@@ -309,6 +309,59 @@ def test_scan_state_beyond_four_gigabytes(mem):
     assert bool((state[:-3] == 0).all()) and bool((y[:-3] == 0).all())
 
 
+def test_scan_sums_of_groups_beyond_two_to_the_32_threads(mem):
+    """64 steps of 4,096 environments of 512 groups of one channel: 2^32 sums for the gradients of b and c.  The environments are
+    four, again and again, and come out as the four alone."""
+    T, few, many, D, N = 64, 4, 4096, 512, 16
+    src = Source(43, torch.bfloat16)
+    t = scan_inputs(src, T, few, D, 16, 1, False, False)
+    row = src.seq(T, 1, D, N)
+    g = {k: src.gpu(t[k]) for k in ("x", "delta")}
+    g.update({k: plain(t[k]) for k in ("a", "d", "delta_bias")})
+    b, dy = src.gpu(row), src.gpu(src.seq(T, few, D))
+    c = src.gpu(src.seq(T, 1, D, N))
+
+    def gradients(n):
+        x, delta, seed = (v.repeat(1, n // few, 1) for v in (g["x"], g["delta"], dy))
+        args = (x, delta, g["a"], b.expand(T, n, D, N), c.expand(T, n, D, N))
+        how = {"d": g["d"], "delta_bias": g["delta_bias"]}
+        _, _, saved = mem.selective_scan(*args, save=True, **how)
+        return mem.selective_scan_backward(seed, saved, *args, **how)
+
+    small = gradients(few)
+    big = gradients(many)
+    for name in ("b", "c"):
+        want, got = getattr(small, name), getattr(big, name)
+        assert all(torch.equal(v, want) for v in got.split(few, 1)), name
+    close("gradient of a", big.a, small.a.cpu().double() * (many // few), T * many)
+    torch.cuda.empty_cache()
+
+
+def test_scan_of_more_wavefronts_than_one_dimension_takes(mem):
+    """2^26 + 2^16 groups of one channel, a wavefront each: forward and backward come out as 2^16 of them alone, again and again."""
+    T, P, R, N = 2, 1 << 16, (1 << 10) + 1, 8
+    src = Source(47, torch.bfloat16)
+    t = scan_inputs(src, T, 1, P, N, 1, False, True)
+    t["b"], t["c"] = src.seq(T, 1, P, N), src.seq(T, 1, P, N)
+    g, dy = scan_gpu(src, t), src.gpu(src.seq(T, 1, P))
+
+    def run(times):
+        args = [g[k].repeat(1, 1, times, *[1] * (g[k].dim() - 3)) if k != "a" else g[k].repeat(times, 1) for k in ("x", "delta", "a", "b", "c")]
+        how = {"state": g["state"].repeat(1, times, 1), "d": g["d"].repeat(times), "delta_bias": g["delta_bias"].repeat(times)}
+        y, h, saved = mem.selective_scan(*args, save=True, **how)
+        grads = mem.selective_scan_backward(dy.repeat(1, 1, times), saved, *args, **how)
+        return {"y": y, "h": h, **{k: v for k, v in grads._asdict().items() if v is not None}}
+
+    small = run(1)
+    torch.cuda.empty_cache()
+    for name, got in run(R).items():
+        want = small[name]
+        axis = {"y": 2, "h": 1, "x": 2, "delta": 2, "b": 2, "c": 2, "state": 1}.get(name, 0)
+        assert all(torch.equal(v, want) for v in got.split(P, axis)), name
+    del got
+    torch.cuda.empty_cache()
+
+
 # ---- convolution ------------------------------------------------------------------------------------------
 
 CONV_CASES = [

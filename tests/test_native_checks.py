@@ -43,6 +43,14 @@ def test_every_wavefront_of_a_launch_sees_its_number(tmp_path):
     assert "launch_order_test: ok" in _run([exe])
 
 
+def test_launches_of_the_policy_operators_can_be_made(tmp_path):
+    """How they are cut where one dimension does not take all their threads (csrc/memory_grid.hpp)."""
+    exe = str(tmp_path / "memory_grid_test")
+    _run(["g++", "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-o", exe,
+          os.path.join(NATIVE, "memory_grid_test.cpp")])
+    assert "memory_grid_test: ok" in _run([exe])
+
+
 def test_carry_masks_of_the_generators_come_from_a_scalar_instruction(tmp_path):
     """The generators' inline assembly, as compiled: an addition whose carry is a mask in scalar registers has
     it from a scalar instruction of the same statement.  What a vector instruction has just written there is not ready for the
