@@ -416,7 +416,7 @@ typedef struct craftax_view { void *data; int64_t step, env; } craftax_view;
 typedef struct craftax_conv_args {
     uint32_t dtype;             /* of x, y, the states and their gradients */
     uint32_t silu;
-    int32_t steps, n, channels; /* all positive (one token: steps 1), n * channels below 2^31 - 4095 */
+    int32_t steps, n, channels; /* all positive (one token: steps 1), steps and n * channels below 2^31 - 4095 */
     int32_t taps;               /* 2..4 */
     const float *weight;        /* [channels][taps], the newest input last */
     const float *bias;          /* [channels] or NULL */

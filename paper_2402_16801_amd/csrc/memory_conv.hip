@@ -259,7 +259,7 @@ template <typename E, int K, int V>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E> p)
 {
     const uint32_t at = blockIdx.x * CONV_THREADS + threadIdx.x;
-    int i = (int)(at / (uint32_t)p.vectors);
+    const int i = (int)(at / (uint32_t)p.vectors);
     if (i >= p.stretch) return;                 // here: environments that are taken side by side
     const Span w = Span::of<V>((int)(at % (uint32_t)p.vectors), p.channels);
     Taps<K, V> taps;
@@ -276,7 +276,8 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E>
         if (p.lengths) length = p.lengths[e];
     };
     load(i);
-    for (; i < p.n; i += p.stretch) {
+    // unsigned: the environment behind a thread's last one may be beyond 2^31
+    for (uint32_t at_env = (uint32_t)i, side = (uint32_t)p.stretch, n = (uint32_t)p.n; at_env < n; at_env += side) {
         float win[K - 1][V], x[V], y[V];
         const bool live = length > 0, empty = !p.state_in || (flag && live);
 #pragma unroll
@@ -296,8 +297,8 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E>
             const float v = taps.sum(win, x[j], j), g = sigmoid(v);
             y[j] = live ? v * (p.silu ? g : 1.0f) : 0.0f;
         }
-        const int e = i;
-        if (i + p.stretch < p.n) load(i + p.stretch);
+        const int e = (int)at_env;
+        if (at_env + side < n) load((int)(at_env + side));
         put<E, V>(p.y.at(0, e) + w.c, w, shrink<E, V>(y));
         if (p.state_out) {
 #pragma unroll
@@ -321,7 +322,7 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams
     __shared__ float sums[CONV_THREADS * COLS];
     const int lanes = 1 << p.lanes_log2, side = threadIdx.x >> p.lanes_log2, rows = CONV_THREADS >> p.lanes_log2;
     const int vec = (int)blockIdx.x * lanes + (threadIdx.x & (lanes - 1));
-    const int stretches = (p.steps + p.stretch - 1) / p.stretch;
+    const int stretches = (p.steps - 1) / p.stretch + 1;
     float dw[K][V], db[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -501,7 +502,8 @@ static int conv_check(const craftax_conv_args* a, bool backward, const char** wh
     if (a->dtype > CRAFTAX_F16) return refuse(CRAFTAX_E_CONFIG, "unknown dtype", why);
     if (a->taps < 2 || a->taps > 4) return refuse(CRAFTAX_E_CONFIG, "taps must be 2..4", why);
     if (a->steps < 1 || a->n < 1 || a->channels < 1) return refuse(CRAFTAX_E_COUNT, "steps, n and channels must be positive", why);
-    if ((int64_t)a->n * a->channels > ((int64_t)1 << 31) - 4096) return refuse(CRAFTAX_E_COUNT, "n * channels must be below 2^31", why);
+    if (a->steps > MOST_COUNT) return refuse(CRAFTAX_E_COUNT, "steps must be below 2^31 - 4095", why);
+    if ((int64_t)a->n * a->channels > MOST_COUNT) return refuse(CRAFTAX_E_COUNT, "n * channels must be below 2^31 - 4095", why);
     if (!a->weight || !a->x.data) return refuse(CRAFTAX_E_NULL, "weight or x is NULL", why);
     const size_t e = elem_bytes(a->dtype);
     if (!aligned(a->weight, 4) || !aligned(a->bias, 4) || !aligned(a->lengths, 4) || !aligned(a->x.data, e) || !aligned(a->state_in, e))

@@ -6,6 +6,9 @@
 
 namespace mem {
 
+// Kernels count steps in signed 32 bits and look some of them ahead, by less than 4,096.
+constexpr int64_t MOST_COUNT = ((int64_t)1 << 31) - 4096;
+
 // `blocks` blocks of `threads` threads: a dimension of a launch takes fewer than 2^32 threads, so that more blocks than that lie
 // over x and z.  Some of the last ones in z may be too many.
 struct Spread { unsigned x, z; };

@@ -517,7 +517,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_token(const ScanParams<E>
         if (p.lengths) length = p.lengths[e];
     };
     load(i);
-    for (; i < p.n; i += p.part) {
+    // unsigned: the environment behind a thread's last one may be beyond 2^31
+    for (uint32_t at_env = (uint32_t)i, side = (uint32_t)p.part, n = (uint32_t)p.n; at_env < n; at_env += side) {
         const bool alive = length > 0, begin = flag != 0;
         float size = Elem<E>::up(delta) + bias;
         if (p.softplus) size = softplus(size);
@@ -530,8 +531,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_token(const ScanParams<E>
             h[m] = alive ? next : old[m];
             out = __builtin_fmaf(next, Elem<E>::up(c.v[m]), out);
         }
-        const int e = i;
-        if (i + p.part < p.n) load(i + p.part);
+        const int e = (int)at_env;
+        if (at_env + side < n) load((int)(at_env + side));
         out += dpp<DPP_XOR1>(out);
         if constexpr (QUADS >= 4) out += dpp<DPP_XOR2>(out);
         if constexpr (QUADS >= 8) out += dpp<DPP_HALF_MIRROR>(out);
@@ -561,7 +562,8 @@ static int scan_check(const craftax_scan_args* a, bool backward, const char** wh
     if (a->states != 8 && a->states != 16 && a->states != 32) return refuse(CRAFTAX_E_CONFIG, "states must be 8, 16 or 32", why);
     if (a->steps < 1 || a->n < 1 || a->channels < 1) return refuse(CRAFTAX_E_COUNT, "steps, n and channels must be positive", why);
     if (a->groups < 1 || a->channels % a->groups != 0) return refuse(CRAFTAX_E_COUNT, "groups must divide channels", why);
-    if ((int64_t)a->n * a->channels > ((int64_t)1 << 31) - 4096) return refuse(CRAFTAX_E_COUNT, "n * channels must be below 2^31", why);
+    if (a->steps > MOST_COUNT) return refuse(CRAFTAX_E_COUNT, "steps must be below 2^31 - 4095", why);
+    if ((int64_t)a->n * a->channels > MOST_COUNT) return refuse(CRAFTAX_E_COUNT, "n * channels must be below 2^31 - 4095", why);
     const craftax_view* need[] = {&a->x, &a->delta, &a->b, &a->c};
     for (const craftax_view* v : need)
         if (!v->data) return refuse(CRAFTAX_E_NULL, "x, delta, b or c is NULL", why);

@@ -487,6 +487,22 @@ def test_conv_beyond_two_to_the_31_elements(mem):
     assert int((y[:, :-2] != 0).sum(dtype=torch.int64)) == 0
 
 
+def test_conv_step_of_the_most_environments(mem):
+    """2^31 - 4096 environments of one channel, a state in place: 4,096 of them, again and again."""
+    few, times = 4096, 2 ** 19 - 1
+    src = Source(23, torch.bfloat16)
+    x, state, weight = (src.normal(few, 1, dtype=torch.bfloat16).cuda().bfloat16(), src.normal(few, 1, 1, dtype=torch.bfloat16).cuda().bfloat16(),
+                        plain(src.normal(1, 2)))
+    want, after = mem.causal_conv_step(x, weight, None, state, out_state=torch.empty_like(state))
+    held = state.repeat(times, 1, 1)
+    y, same = mem.causal_conv_step(x.repeat(times, 1), weight, None, held)
+    assert same is held
+    for got, one in ((y, want), (held, after)):
+        assert all(torch.equal(v, one.view(1, few).expand_as(v)) for v in got.view(times, few).split(1 << 14))
+    del y, held, same, got
+    torch.cuda.empty_cache()
+
+
 # ---- norm -------------------------------------------------------------------------------------------------
 
 NORM_CASES = [

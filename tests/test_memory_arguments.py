@@ -34,6 +34,20 @@ def test_an_unknown_gate_is_refused(mem):
         mem.residual_norm(torch.zeros(1, 1, 8), torch.zeros(1, 1, 8), gate_act="tanh")
 
 
+def test_counts_that_32_bits_do_not_hold_with_what_is_read_ahead_are_refused():
+    """At the C entry, before anything is looked at on a device: the addresses are none."""
+    lib, at, most = binding.load(), 1 << 20, 2 ** 31 - 4096
+    conv = dict(dtype=1, n=1, channels=1, taps=2, weight=at, x=at, y=at, dy=at, dx=at)
+    scan = dict(dtype=1, n=1, channels=1, states=8, groups=1, a=at, x=at, delta=at, b=at, c=at, y=at, dy=at, dx=at, ddelta=at, db=at, dc=at, da=at, saved=at)
+    for args, calls in ((binding.ConvArgs(steps=most + 1, **conv), ("causal_conv", "causal_conv_backward")),
+                        (binding.ScanArgs(steps=most + 1, **scan), ("selective_scan", "selective_scan_backward"))):
+        for call in calls:
+            assert getattr(lib, "craftax_" + call)(args, None) == -3 and b"steps" in lib.craftax_last_error(), call
+        args.steps, args.n = 1, most + 1
+        for call in calls:
+            assert getattr(lib, "craftax_" + call)(args, None) == -3 and b"n * channels" in lib.craftax_last_error(), call
+
+
 def test_structures_match_the_header(tmp_path):
     pairs = [("craftax_conv_args", binding.ConvArgs), ("craftax_scan_args", binding.ScanArgs),
              ("craftax_norm_args", binding.NormArgs)]
