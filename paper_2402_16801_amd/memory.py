@@ -169,9 +169,9 @@ class _Conv(torch.autograd.Function):
 
 class _Scan(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, delta, a, b, c, d, z, delta_bias, state, first, lengths, softplus):
+    def forward(ctx, x, delta, a, b, c, d, z, delta_bias, state, first, lengths, softplus, save):
         y, out, saved = selective_scan(x, delta, a, b, c, d=d, z=z, delta_bias=delta_bias, softplus=softplus, state=state, first=first,
-                                       lengths=lengths, save=True)
+                                       lengths=lengths, save=save)
         ctx.save_for_backward(saved, x, delta, a, b, c, d, z, delta_bias, first, lengths)
         # not among the saved tensors: its values are in `saved`, so that it may be written before the backward pass
         ctx.state = None if state is None else state.detach()
@@ -184,7 +184,7 @@ class _Scan(torch.autograd.Function):
         saved, x, delta, a, b, c, d, z, delta_bias, first, lengths = ctx.saved_tensors
         g = selective_scan_backward(_side_by_side(dy, x), saved, x, delta, a, b, c, d=d, z=z, delta_bias=delta_bias, softplus=ctx.softplus,
                                     state=ctx.state, first=first, lengths=lengths, dstate=dstate.contiguous())
-        return g.x, g.delta, g.a, g.b, g.c, g.d, g.z, g.delta_bias, g.state, None, None, None
+        return g.x, g.delta, g.a, g.b, g.c, g.d, g.z, g.delta_bias, g.state, None, None, None, None
 
 
 class _Norm(torch.autograd.Function):
@@ -210,7 +210,9 @@ def conv(x, weight, bias=None, *, state=None, first=None, lengths=None, silu=Tru
 
 def scan(x, delta, a, b, c, *, d=None, z=None, delta_bias=None, softplus=True, state=None, first=None, lengths=None):
     """selective_scan, differentiable in every tensor but first and lengths: (y, state after the last step)."""
-    return _Scan.apply(x, delta, a, b, c, d, z, delta_bias, state, first, lengths, softplus)
+    # what a backward pass needs is kept only where one can follow
+    save = torch.is_grad_enabled() and any(isinstance(v, Tensor) and v.requires_grad for v in (x, delta, a, b, c, d, z, delta_bias, state))
+    return _Scan.apply(x, delta, a, b, c, d, z, delta_bias, state, first, lengths, softplus, save)
 
 
 def norm(y, residual, *, gate=None, post_weight=None, scale=None, pre_weight=None, gate_act="sigmoid", eps=1e-6):

@@ -725,6 +725,29 @@ def test_differentiable_functions(mem):
         close("gradient of " + name, got[name], want[name], 9 * (N * T + T * n + D))
 
 
+@pytest.mark.parametrize("grad", [True, False], ids=["grad", "no_grad"])
+def test_scan_keeps_nothing_where_no_backward_pass_can_follow(mem, grad):
+    """Under no_grad, and where nothing requires gradients, no states are saved: 16 floats for every 8 steps, twice the outputs."""
+    src = Source(95, torch.float32)
+    T, n, D = 256, 16, 512
+    g = scan_gpu(src, scan_inputs(src, T, n, D, 16, 1, True, True))
+    args, how = [g[k] for k in ("x", "delta", "a", "b", "c")], {k: g[k] for k in ("d", "z", "delta_bias", "state")}
+    want_y, want_h = mem.scan(*[v.clone().requires_grad_(True) for v in args], **how)
+    assert want_y.requires_grad and want_h.requires_grad
+    want_y, want_h = want_y.detach(), want_h.detach()
+    if not grad:
+        args[0].requires_grad_(True)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    held = torch.cuda.memory_allocated()
+    with torch.set_grad_enabled(grad):
+        y, h = mem.scan(*args, **how)
+    saved = T // 8 * n * D * 16 * 4
+    taken = torch.cuda.max_memory_allocated() - held
+    assert taken < saved / 2 + y.numel() * 4 + h.numel() * 4, (taken, saved)
+    assert not y.requires_grad and torch.equal(y, want_y) and torch.equal(h, want_h)
+
+
 def _rollout_and_step(mem, operator):
     """(a rollout from a state as a differentiable call, a step that takes a state and out_state, a fresh state, its leaves)"""
     src = Source(91, torch.float32)
