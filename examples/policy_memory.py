@@ -102,7 +102,8 @@ class Policy(torch.nn.Module):
 
 @torch.no_grad()
 def act(policy, sim, states, first, steps):
-    """Plays `steps` steps: what was seen, done and earned, [steps][n] each.  states and first are carried on in place."""
+    """Plays `steps` steps: what was seen, done and earned, [steps][n] each, and `ahead`, the value of what is seen behind the last
+    step, [n].  states and first are carried on in place."""
     n, seen = sim.n, {k: [] for k in ("obs", "first", "logits", "actions", "reward", "done")}
     for _ in range(steps):
         obs = sim.obs.view(torch.float32)
@@ -114,14 +115,17 @@ def act(policy, sim, states, first, steps):
         seen["reward"].append(reward.clone())
         seen["done"].append(done.clone())
         first.copy_(done)
-    return {k: torch.stack(v) for k, v in seen.items()}
+    seen = {k: torch.stack(v) for k, v in seen.items()}
+    _, seen["ahead"], _ = policy(sim.obs.view(torch.float32), [[v.clone() for v in state] for state in states], first)
+    return seen
 
 
 def loss_of(policy, seen, states, discount=0.99):
-    """(actor-critic loss over a rollout that began with `states`, logits)"""
+    """(actor-critic loss over a rollout that began with `states`, logits).  The return of the last step goes on with the value of what
+    followed it, as acting saw it."""
     logits, values, _ = policy(seen["obs"], states, seen["first"])
     with torch.no_grad():
-        returns, ahead = torch.empty_like(values), values[-1]
+        returns, ahead = torch.empty_like(values), seen["ahead"].to(values.dtype)
         for t in range(len(values) - 1, -1, -1):
             ahead = returns[t] = seen["reward"][t] + discount * ahead * (1 - seen["done"][t].float())
         advantage = returns - values

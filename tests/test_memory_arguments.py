@@ -1,5 +1,6 @@
 """The policy memory operators refuse what is not on a GPU, and their structures match the C header's (no GPU needed)."""
 import ctypes
+import importlib.util
 import os
 import subprocess
 
@@ -66,3 +67,21 @@ def test_structures_match_the_header(tmp_path):
     subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), "-o", str(tmp_path / "sizes"), str(source)], check=True)
     got = subprocess.run([str(tmp_path / "sizes")], check=True, capture_output=True, text=True).stdout.split()
     assert [int(v) for v in got] == want
+
+
+def test_the_returns_of_the_example_go_on_behind_the_rollout():
+    """The return of the last step: its reward and the discounted value of what followed it, nothing where the episode ended."""
+    spec = importlib.util.spec_from_file_location("policy_memory", os.path.join(ROOT, "examples", "policy_memory.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    reward = torch.tensor([[1.0, 0.0, 2.0], [0.5, 1.0, 0.0], [0.25, 2.0, 1.0]], dtype=torch.float64)
+    done = torch.tensor([[0, 1, 0], [0, 0, 0], [0, 0, 1]], dtype=torch.uint8)
+    values = torch.tensor([[0.5, 1.5, -1.0], [2.0, 0.0, 1.0], [3.0, -2.0, 4.0]], dtype=torch.float64)
+    logits = torch.zeros(3, 3, example.ACTIONS, dtype=torch.float64)
+    seen = {"obs": None, "first": None, "reward": reward, "done": done, "actions": torch.zeros(3, 3, dtype=torch.int32),
+            "ahead": torch.tensor([8.0, -16.0, 32.0], dtype=torch.float64)}
+    loss, _ = example.loss_of(lambda obs, states, first: (logits, values, None), seen, None, discount=0.5)
+    returns = torch.tensor([[1 + 0.25 + 0.0625 + 1.0, 0.0, 2 + 0.0 + 0.25], [0.5 + 0.125 + 2.0, 1 + 1.0 - 4.0, 0.5], [0.25 + 4.0, 2.0 - 8.0, 1.0]], dtype=torch.float64)
+    chance = torch.tensor(1.0 / example.ACTIONS, dtype=torch.float64)
+    want = -(chance.log() * (returns - values)).mean() + 0.5 * (returns - values).square().mean() + 0.01 * chance.log()
+    assert abs(float(loss - want)) <= 1e-12
