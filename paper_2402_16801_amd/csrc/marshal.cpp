@@ -8,6 +8,7 @@
 #include <ATen/hip/impl/HIPGuardImplMasqueradingAsCUDA.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <c10/core/GradMode.h>
+#include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -27,6 +28,7 @@ struct Refusal : std::runtime_error {
 };
 
 PyObject* g_error = nullptr;      // CraftaxError
+PyObject* g_no_memory = nullptr;  // torch.OutOfMemoryError
 
 // The entry points of the loaded library (the release or the debug one), set by bind().
 struct Library {
@@ -431,23 +433,25 @@ PyObject* entry(PyObject*, PyObject* const* v, Py_ssize_t count)
         return F(v);
     } catch (const Refusal& e) {
         if (!PyErr_Occurred()) PyErr_SetString(g_error ? g_error : PyExc_RuntimeError, e.what());
+    } catch (const c10::OutOfMemoryError& e) {
+        PyErr_SetString(g_no_memory ? g_no_memory : PyExc_RuntimeError, e.what_without_backtrace());
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
     return nullptr;
 }
 
-// bind(error class, addresses of the entry points in the order of Library)
+// bind(error class, class of errors for want of memory, addresses of the entry points in the order of Library)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t count)
 {
     constexpr Py_ssize_t ENTRIES = sizeof(Library) / sizeof(void*);
-    if (count != 1 + ENTRIES) {
-        PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", 1 + ENTRIES, count);
+    if (count != 2 + ENTRIES) {
+        PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", 2 + ENTRIES, count);
         return nullptr;
     }
     void* at[ENTRIES];
     for (Py_ssize_t k = 0; k < ENTRIES; ++k) {
-        at[k] = PyLong_AsVoidPtr(v[1 + k]);
+        at[k] = PyLong_AsVoidPtr(v[2 + k]);
         if (PyErr_Occurred()) return nullptr;
     }
     static_assert(sizeof(at) == sizeof(Library), "one address per entry point");
@@ -455,6 +459,9 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t count)
     Py_INCREF(v[0]);
     Py_XDECREF(g_error);
     g_error = v[0];
+    Py_INCREF(v[1]);
+    Py_XDECREF(g_no_memory);
+    g_no_memory = v[1];
     Py_RETURN_NONE;
 }
 

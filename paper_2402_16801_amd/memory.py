@@ -51,7 +51,7 @@ def _ready():
     global _bound
     if _bound is None or _bound is not binding._lib:
         lib = binding.load()
-        _marshal.bind(CraftaxError, *(ctypes.cast(getattr(lib, "craftax_" + name), ctypes.c_void_p).value for name in _ENTRIES))
+        _marshal.bind(CraftaxError, torch.OutOfMemoryError, *(ctypes.cast(getattr(lib, "craftax_" + name), ctypes.c_void_p).value for name in _ENTRIES))
         _bound = lib
     return _marshal
 

@@ -855,6 +855,15 @@ def test_refusals(mem):
     refused("channels must be 1..8192", mem.residual_norm, wide, wide)
 
 
+def test_want_of_memory_is_the_error_that_torch_has_for_it(mem):
+    """Outputs of 550 GB, of an input that is one row: what a caller who tries again with less looks for."""
+    x, weight = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda").expand(1 << 26, 64, 64), torch.zeros(64, 4, device="cuda")
+    with pytest.raises(torch.OutOfMemoryError):
+        mem.causal_conv(x, weight)
+    y, _ = mem.causal_conv(x[:4], weight)
+    assert bool((y == 0).all())
+
+
 def test_refusals_at_the_c_entry(mem):
     """Codes and texts of the calls themselves; nothing is launched."""
     import ctypes
