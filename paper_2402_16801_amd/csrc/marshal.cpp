@@ -66,6 +66,14 @@ const Tensor& need(PyObject* o, const char* name)
     return *t;
 }
 
+// an option that is on or off; what has no truth value leaves its own error
+bool truth(PyObject* o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Refusal("");
+    return v != 0;
+}
+
 uint32_t type_code(at::ScalarType t)
 {
     switch (t) {
@@ -221,7 +229,7 @@ craftax_conv_args conv_args(const Common& c, const Tensor& x, PyObject* const* v
     const int64_t taps = weight.size(1);
     craftax_conv_args a = {};
     a.dtype = type_code(c.type);
-    a.silu = PyObject_IsTrue(v[6]);
+    a.silu = truth(v[6]);
     a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.channels = (int32_t)c.channels; a.taps = (int32_t)taps;
     a.weight = dense<const float>(&weight, "weight", {c.channels, taps}, at::kFloat, c);
     a.bias = dense<const float>(maybe(v[2], "bias"), "bias", {c.channels}, at::kFloat, c);
@@ -285,7 +293,7 @@ craftax_scan_args scan_args(const Common& c, const Tensor& x, PyObject* const* v
     const int64_t states = rates.size(1), groups = b.size(-2);
     craftax_scan_args a = {};
     a.dtype = type_code(c.type);
-    a.softplus = PyObject_IsTrue(v[8]);
+    a.softplus = truth(v[8]);
     a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.channels = (int32_t)c.channels;
     a.states = (int32_t)states; a.groups = (int32_t)groups;
     a.a = dense<const float>(&rates, "a", {c.channels, states}, at::kFloat, c);
@@ -319,7 +327,7 @@ PyObject* selective_scan(PyObject* const* v)
         a.state_out = out.data_ptr<float>();
     }
     a.y = place(y, c);
-    if (PyObject_IsTrue(v[12])) {
+    if (truth(v[12])) {
         saved = bytes(g_lib.scan_saved ? g_lib.scan_saved(&a) : 0, c);
         a.saved = address(saved);
     }

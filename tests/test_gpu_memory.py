@@ -855,6 +855,16 @@ def test_refusals(mem):
     refused("channels must be 1..8192", mem.residual_norm, wide, wide)
 
 
+def test_options_without_a_truth_value_are_refused(mem):
+    src = Source(83, torch.float32)
+    g, w = scan_gpu(src, scan_inputs(src, 4, 3, 32, 16, 2, True, True)), plain(src.normal(32, 4))
+    args, neither = [g[k] for k in ("x", "delta", "a", "b", "c")], torch.zeros(2)
+    for call in (lambda: mem.causal_conv(g["x"], w, silu=neither), lambda: mem.selective_scan(*args, softplus=neither),
+                 lambda: mem.selective_scan(*args, save=neither)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            call()
+
+
 def test_want_of_memory_is_the_error_that_torch_has_for_it(mem):
     """Outputs of 550 GB, of an input that is one row: what a caller who tries again with less looks for."""
     x, weight = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda").expand(1 << 26, 64, 64), torch.zeros(64, 4, device="cuda")
