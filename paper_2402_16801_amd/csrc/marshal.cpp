@@ -66,6 +66,13 @@ const Tensor& need(PyObject* o, const char* name)
     return *t;
 }
 
+// a dimension, as the C ABI has it
+int32_t count(int64_t v, const char* name)
+{
+    if (v > INT32_MAX) refuse(name, " is beyond 2^31 - 1");
+    return (int32_t)v;
+}
+
 // an option that is on or off; what has no truth value leaves its own error
 bool truth(PyObject* o)
 {
@@ -230,7 +237,7 @@ craftax_conv_args conv_args(const Common& c, const Tensor& x, PyObject* const* v
     craftax_conv_args a = {};
     a.dtype = type_code(c.type);
     a.silu = truth(v[6]);
-    a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.channels = (int32_t)c.channels; a.taps = (int32_t)taps;
+    a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.channels = (int32_t)c.channels; a.taps = count(taps, "taps");
     a.weight = dense<const float>(&weight, "weight", {c.channels, taps}, at::kFloat, c);
     a.bias = dense<const float>(maybe(v[2], "bias"), "bias", {c.channels}, at::kFloat, c);
     a.first = flags(maybe(v[4], "first"), c);
@@ -295,7 +302,7 @@ craftax_scan_args scan_args(const Common& c, const Tensor& x, PyObject* const* v
     a.dtype = type_code(c.type);
     a.softplus = truth(v[8]);
     a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.channels = (int32_t)c.channels;
-    a.states = (int32_t)states; a.groups = (int32_t)groups;
+    a.states = count(states, "states"); a.groups = count(groups, "groups");
     a.a = dense<const float>(&rates, "a", {c.channels, states}, at::kFloat, c);
     a.d = dense<const float>(maybe(v[5], "d"), "d", {c.channels}, at::kFloat, c);
     a.delta_bias = dense<const float>(maybe(v[7], "delta_bias"), "delta_bias", {c.channels}, at::kFloat, c);

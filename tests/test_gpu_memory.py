@@ -865,6 +865,19 @@ def test_options_without_a_truth_value_are_refused(mem):
             call()
 
 
+def test_counts_that_32_bits_do_not_hold_are_refused(mem):
+    """2^32 + 3 taps are not three, nor 2^32 + 16 states sixteen."""
+    from paper_2402_16801_amd import binding
+    x, wide = torch.zeros(1, 1, 1, device="cuda"), torch.empty(1, 2 ** 32 + 16, device="cuda")
+    with pytest.raises(binding.CraftaxError, match="taps is beyond"):
+        mem.causal_conv(x, wide[:, :2 ** 32 + 3])
+    short = wide.view(1, 1, 1, -1)
+    with pytest.raises(binding.CraftaxError, match="states is beyond"):
+        mem.selective_scan(x, x, wide, short, short)
+    del wide, short
+    torch.cuda.empty_cache()
+
+
 def test_want_of_memory_is_the_error_that_torch_has_for_it(mem):
     """Outputs of 550 GB, of an input that is one row: what a caller who tries again with less looks for."""
     x, weight = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda").expand(1 << 26, 64, 64), torch.zeros(64, 4, device="cuda")
