@@ -126,12 +126,16 @@ __device__ __forceinline__ void load4(const void* p, float (&h)[4])
 __device__ __forceinline__ void store4(void* p, const float (&h)[4]) { *static_cast<float4*>(p) = make_float4(h[0], h[1], h[2], h[3]); }
 __device__ __forceinline__ void zero(float (&h)[4]) { h[0] = h[1] = h[2] = h[3] = 0.0f; }
 
-// The decay's exponent is taken to base 2: a is scaled once.
+// The decay's exponent is taken to base 2: a is scaled once.  It stays finite, since steps that do not count have the size 0,
+// and 0 times an infinity is no number; a step that counts decays to 0 by either.
 template <int N> __device__ __forceinline__ void load_rates(const float* a, const Tile& w, float (&a2)[4])
 {
     load4(a + (int64_t)w.channel * N + w.quad * 4, a2);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) a2[m] *= LOG2E;
+    for (int m = 0; m < 4; ++m) {
+        a2[m] *= LOG2E;
+        if (__builtin_fabsf(a2[m]) > __FLT_MAX__) a2[m] = __builtin_copysignf(__FLT_MAX__, a2[m]);
+    }
 }
 
 // Where a lane reads or writes one sequence: its channel at its own first step of the current block of steps.

@@ -235,6 +235,28 @@ def test_scan_gradients_where_the_groups_are_the_outer_dimension(mem, token, odd
         assert torch.equal(value, same), name
 
 
+@pytest.mark.parametrize("T", [5, 40, 300])
+def test_scan_with_rates_of_minus_infinity(mem, T):
+    """A state that nothing is left of after a step.  Steps behind the end, and places without a channel, leave it finite all the same."""
+    src = Source(13, torch.float32)
+    n, D, N = 3, 37, 16
+    t = scan_inputs(src, T, n, D, N, 1, True, True)
+    t["a"][-1, 3] = t["a"][5, :] = -float("inf")
+    lengths = torch.tensor([T, T - 3, 1], dtype=torch.int32)
+    dy, dstate = src.seq(T, n, D), src.normal(n, D, N)
+    (y, h), want = ref.gradients(ref.scan, t, (dy, dstate), lengths=lengths)
+    g = scan_gpu(src, t)
+    how = {k: g[k] for k in ("d", "z", "delta_bias", "state")}
+    how["lengths"] = lengths.cuda()
+    args = [g[k] for k in ("x", "delta", "a", "b", "c")]
+    got_y, got_h, saved = mem.selective_scan(*args, save=True, **how)
+    close("y", got_y, y, N * 64)
+    close("state", got_h, h, N * 64)
+    got = mem.selective_scan_backward(plain(dy), saved, *args, dstate=plain(dstate), **how)
+    for name in ("x", "b", "c", "d", "z", "state"):
+        close("gradient of " + name, getattr(got, name), want[name], N * 64 + D + T * n)
+
+
 def test_scan_steps_equal_the_sequence(mem):
     src = Source(21, torch.bfloat16)
     T, n, D, N, G = 40, 9, 136, 16, 2
