@@ -48,6 +48,14 @@ __device__ __forceinline__ float row_sum(float v, float* slots)
     return v;
 }
 
+// 1 / sqrt(v), also of a subnormal number, as with a tiny eps: the instruction alone takes one for 0
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const bool tiny = v < 0x1p-126f;
+    const float root = __builtin_amdgcn_rsqf(tiny ? v * 0x1p24f : v);
+    return tiny ? root * 0x1p12f : root;
+}
+
 // act(gate) and its derivative; written as selections, so that no branch stands between the elements of a row
 __device__ __forceinline__ float gate_value(float g, int act)
 {
@@ -219,7 +227,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) __attribute__((amdgpu_waves_p
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
                 for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s);
-            root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
+            root = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         float s = 0.0f;
 #pragma unroll
@@ -230,7 +238,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) __attribute__((amdgpu_waves_p
                 r[c][j] = __builtin_fmaf(y[c][j] * root * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
                 s = w.add(c, j, r[c][j], r[c][j], s);
             }
-        root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
+        root = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
         // the next row's values, waited for in front of the stores: behind them the wait would be for those too
         pin(raw_y);
         pin(raw_r);
@@ -314,7 +322,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
                 for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s);
-            root_y = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
+            root_y = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         // out again, its root, and the sum over the row of (du w2) (out root)
         float s = 0.0f, m = 0.0f;
@@ -327,7 +335,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 r[c][j] = __builtin_fmaf(y[c][j] * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
                 s = w.add(c, j, r[c][j], r[c][j], s);
             }
-        const float root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
+        const float root = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll

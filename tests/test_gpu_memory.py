@@ -589,6 +589,27 @@ def test_norm_of_rows_of_zeros_and_of_two_dimensions(mem):
         close("gradient of " + name, getattr(got, name), want[name], 16)
 
 
+@pytest.mark.parametrize("D", [1, 200, 512, 1345])
+@pytest.mark.parametrize("power", [-149, -132, -126])
+def test_norm_with_a_subnormal_eps(mem, D, power):
+    """Rows of zeros, rows whose squares are subnormal (and exact in 32 bits), and ordinary ones."""
+    src = Source(D - power, torch.float32)
+    y, r, w = src.normal(3, D), src.normal(3, D), (1 + src.normal(D, spread=0.1)).float().double()
+    y[0] = r[0] = r[1] = 0.0
+    y[1] = 2.0 ** -66
+    how = {"post_weight": w, "pre_weight": w}
+    out, u = ref.norm(y, r, eps=2.0 ** power, **how)
+    got_out, got_u = mem.residual_norm(plain(y), plain(r), eps=2.0 ** power, **{k: plain(v) for k, v in how.items()})
+    close("out", got_out, out, 4)
+    close("u", got_u, u, 4)
+    assert bool((got_out[0] == 0).all()) and bool((got_u[0] == 0).all())
+    y, r, du = y[2:], r[2:], src.normal(1, D)
+    _, want = ref.gradients(ref.norm, {"y": y, "residual": r, **how}, (None, du), eps=2.0 ** power)
+    got = mem.residual_norm_backward(None, plain(du), plain(y), plain(r), eps=2.0 ** power, **{k: plain(v) for k, v in how.items()})
+    for name in ("y", "residual", "post_weight", "pre_weight"):
+        close("gradient of " + name, getattr(got, name), want[name], 16)
+
+
 def alike(what, got, want, terms):
     """close(), where the definition is finite; where it is infinite or no number, the same."""
     got64 = got.detach().cpu().double()
