@@ -301,8 +301,9 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
     const float mean = 1.0f / (float)p.channels;
     auto one = [&](uint32_t base, Raw& mine, Raw& next) {
         const uint32_t row = base + which;
-        // a wavefront without a row goes along with the last one: that adds nothing to the weights' gradients, be it infinite
-        const bool on = ROWS == 1 || row < p.rows;
+        // Without a row of its own, one of two wavefronts of a row goes along with the last one, for the barriers: that adds nothing to
+        // the weights' gradients, be it infinite.
+        const bool on = W != 2 || row < p.rows;
         auto add = [&](float a, float b, float& sum) {
             const float with = __builtin_fmaf(a, b, sum);
             sum = on ? with : sum;
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
     for (uint32_t base = blockIdx.x * ROWS; base < p.rows; base += SLOTS * stride) {
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k)
-            if (base + k * stride < p.rows) one(base + k * stride, raw[k], raw[(k + 1) % SLOTS]);
+            if (base + k * stride + (W == 1 ? which : 0) < p.rows) one(base + k * stride, raw[k], raw[(k + 1) % SLOTS]);
     }
     if (p.part == nullptr) return;
     // one partial row per block and weight; the rows that a block works on at once are added up in LDS
