@@ -87,9 +87,10 @@ template <int W> struct RowBlock {
 
 // How rows fit the lanes' chunks of V values.  WHOLE: exactly.  TAIL: a chunk that passes the end of the row is moved back to
 // end with it: its first `old` values are another lane's too (those of a lane with nothing left: all V).  They are computed
-// and stored like the other lane's, bit for bit, and only left out of the sums.  SHORT: rows of fewer than V values are
-// read and written value by value, by one lane.
-enum Fit { WHOLE, TAIL, SHORT };
+// and stored like the other lane's, bit for bit, and only left out of the sums.  EVEN: the same where V divides the row, so that
+// `old` is 0 or V and a chunk is left out by one selection instead of V (backward of 131,072 rows of 400 bfloat16 213 us, 220 as TAIL, of
+// 1,000 487 and 504).  SHORT: rows of fewer than V values are read and written value by value, by one lane.
+enum Fit { WHOLE, EVEN, TAIL, SHORT };
 template <int CHUNKS, int V, Fit FIT> struct RowPlace {
     int at[CHUNKS], old[CHUNKS], channels;
     __device__ __forceinline__ RowPlace(int n, int side, int width) : channels(n)
@@ -104,14 +105,19 @@ template <int CHUNKS, int V, Fit FIT> struct RowPlace {
     }
     __device__ __forceinline__ bool mine(int c, int j) const
     {
-        return FIT == WHOLE || (j >= old[c] && (FIT == TAIL || j < channels));
+        if (FIT == WHOLE || FIT == EVEN) return FIT == WHOLE || old[c] == 0;
+        return j >= old[c] && (FIT == TAIL || j < channels);
     }
-    // s with value j's product added where it counts in this lane.  A selection, not a product with 0: the values that do not count may
-    // be infinite.  Of several chunks the first half is filled in every row (see with_row) and needs none.
-    __device__ __forceinline__ float add(int c, int j, float a, float b, float s) const
+    // s with value j's product added where it counts in this lane; values are added in order, and `before` is the sum in front of a chunk.
+    // A selection, not a product with 0: the values that do not count may be infinite.  Of several chunks the first half is filled
+    // in every row (see with_row) and needs none.
+    __device__ __forceinline__ float add(int c, int j, float a, float b, float s, float& before) const
     {
         const float sum = __builtin_fmaf(a, b, s);
-        return c < CHUNKS / 2 || mine(c, j) ? sum : s;
+        if (FIT == WHOLE || c < CHUNKS / 2) return sum;
+        if (FIT != EVEN) return mine(c, j) ? sum : s;
+        if (j == 0) before = s;
+        return j < V - 1 || old[c] == 0 ? sum : before;
     }
 };
 
@@ -188,7 +194,7 @@ template <typename P, int CHUNKS, int V> __device__ __forceinline__ void pin(Pac
 
 // Wavefronts per SIMD at most: rows of 16 values per lane that do not fill the lanes are faster with two than with the three that
 // their registers leave room for (131,072 rows of 1,000 bfloat16 264 us, 270 with three; 40,000 of 3,001 float16 285 and 290).
-template <typename E, int CHUNKS, Fit FIT> constexpr int norm_waves() { return FIT == TAIL && CHUNKS * 16 / sizeof(E) > 8 ? 2 : 8; }
+template <typename E, int CHUNKS, Fit FIT> constexpr int norm_waves() { return FIT != WHOLE && CHUNKS * 16 / sizeof(E) > 8 ? 2 : 8; }
 
 template <typename E, typename R, int W, int CHUNKS, Fit FIT>
 __global__ __launch_bounds__(RowBlock<W>::THREADS) __attribute__((amdgpu_waves_per_eu(2, norm_waves<E, CHUNKS, FIT>()))) void k_norm(const NormParams<E, R> p)
@@ -222,21 +228,21 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) __attribute__((amdgpu_waves_p
         if (base + stride < p.rows) load(row + stride < last ? row + stride : last);
         float root = 1.0f;
         if (p.post_weight) {
-            float s = 0.0f;
+            float s = 0.0f, before;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s, before);
             root = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
-        float s = 0.0f;
+        float s = 0.0f, before;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * root * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = w.add(c, j, r[c][j], r[c][j], s);
+                s = w.add(c, j, r[c][j], r[c][j], s, before);
             }
         root = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
         // the next row's values, waited for in front of the stores: behind them the wait would be for those too
@@ -318,15 +324,15 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
         if (AHEAD > 0 && base + AHEAD * stride < p.rows) load(mine, base + AHEAD * stride);
         float root_y = 1.0f;
         if (p.post_weight) {
-            float s = 0.0f;
+            float s = 0.0f, before;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s);
+                for (int j = 0; j < V; ++j) s = w.add(c, j, y[c][j], y[c][j], s, before);
             root_y = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[0][which]), mean, p.eps));
         }
         // out again, its root, and the sum over the row of (du w2) (out root)
-        float s = 0.0f, m = 0.0f;
+        float s = 0.0f, m = 0.0f, before;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -334,7 +340,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 y[c][j] *= root_y;                                   // from here on without its scale
                 const float act = gate_value(g[c][j], p.gate_act);
                 r[c][j] = __builtin_fmaf(y[c][j] * w1[c][j] * scale[c][j], gated ? act : 1.0f, r[c][j]);
-                s = w.add(c, j, r[c][j], r[c][j], s);
+                s = w.add(c, j, r[c][j], r[c][j], s, before);
             }
         const float root = inverse_root(__builtin_fmaf(row_sum<W>(s, slots[1][which]), mean, p.eps));
 #pragma unroll
@@ -344,7 +350,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 r[c][j] *= root;
                 add(du[c][j], r[c][j], d2[c][j]);
                 du[c][j] *= w2[c][j];
-                m = w.add(c, j, du[c][j], r[c][j], m);
+                m = w.add(c, j, du[c][j], r[c][j], m, before);
             }
         m = row_sum<W>(m, slots[2][which]) * mean;
         float q = 0.0f;
@@ -360,7 +366,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
                 add(dv, y[c][j], d1[c][j]);
                 du[c][j] = dv * w1[c][j];
-                q = w.add(c, j, du[c][j], y[c][j], q);
+                q = w.add(c, j, du[c][j], y[c][j], q, before);
             }
         if (p.post_weight) {
             q = row_sum<W>(q, slots[3][which]) * mean;
@@ -503,14 +509,21 @@ template <bool BACKWARD, typename F> static void with_row(const craftax_norm_arg
             auto whole = [&](auto count) {
                 constexpr int C = decltype(count)::value;
                 if (a->channels == W * WAVE * V * C) f(e, r, wc, count, std::integral_constant<Fit, WHOLE>{});
+                else if (a->channels % V == 0) f(e, r, wc, count, std::integral_constant<Fit, EVEN>{});
                 else if (a->channels >= V) f(e, r, wc, count, std::integral_constant<Fit, TAIL>{});
                 else if constexpr (W == 1 && C == 1) f(e, r, wc, count, std::integral_constant<Fit, SHORT>{});
             };
             // More than one chunk only where half as many would not hold the row: the first half is filled.
             constexpr int EIGHT = 8 / V;          // chunks of eight values
-            if (V < 8 && a->channels <= W * WAVE * V) whole(std::integral_constant<int, 1>{});
-            else if ((BACKWARD && W < 8) || a->channels <= W * WAVE * 8) whole(std::integral_constant<int, EIGHT>{});
-            else if constexpr (!BACKWARD || W == 8) whole(std::integral_constant<int, 2 * EIGHT>{});
+            // one wavefront takes a row of any length that fits it; more of them are taken for no fewer values per lane than half of
+            // what they hold (see row_waves)
+            if constexpr (W == 1) {
+                if (V < 8 && a->channels <= WAVE * V) return whole(std::integral_constant<int, 1>{});
+            }
+            if constexpr (W == 1 || BACKWARD) {
+                if (a->channels <= W * WAVE * 8) return whole(std::integral_constant<int, EIGHT>{});
+            }
+            if constexpr (!BACKWARD || W == 8) whole(std::integral_constant<int, 2 * EIGHT>{});
         };
         auto waves = [&](auto r) {
             if (w == 1) chunks(r, std::integral_constant<int, 1>{});
