@@ -621,7 +621,7 @@ def alike(what, got, want, terms):
 
 
 # lengths that fill the lanes of a row (512), that do not in one of one, two and four chunks a lane, that leave lanes without a value, and short ones
-@pytest.mark.parametrize("D", [3, 7, 20, 200, 300, 512, 513, 1000, 1345, 2050, 4097, 8191])
+@pytest.mark.parametrize("D", [3, 7, 20, 200, 300, 512, 513, 600, 1000, 1345, 1544, 2050, 3000, 4097, 6000, 8191])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_norm_of_rows_with_an_infinity(mem, dtype, D):
     """An infinity makes the root of its row 0: the row's other values are the residual's, or 0, wherever it lies.  One in the
@@ -665,6 +665,31 @@ def test_norm_gradients_of_weights_with_an_infinity_in_the_last_row(mem, D, rows
     got = mem.residual_norm_backward(None, plain(du), plain(t["y"]), plain(t["residual"]), scale=plain(t["scale"]), pre_weight=plain(t["pre_weight"]))
     for name in ("scale", "pre_weight"):
         alike("gradient of " + name, getattr(got, name), want[name], rows + 16)
+
+
+def _norm_tensors(src, T, n, D, gate=True):
+    t = {"y": src.seq(T, n, D), "residual": src.seq(T, n, D), "gate": src.seq(T, n, D) if gate else None, "scale": src.normal(D),
+         "post_weight": (1 + src.normal(D, spread=0.1)).float().double(), "pre_weight": (1 + src.normal(D, spread=0.1)).float().double()}
+    return {k: v for k, v in t.items() if v is not None}
+
+
+# rows of one, two, four and eight wavefronts, forward and backward, whole, in vectors and ragged; more of them than the chip holds at
+# once, and no multiple of that
+@pytest.mark.parametrize("dtype,rows,D", [("f32", 27001, 9), ("bf16", 26003, 512), ("f32", 13001, 333), ("bf16", 9007, 1000), ("f32", 7001, 1345), ("f16", 5003, 1536),
+                                          ("bf16", 3301, 2050), ("f32", 2003, 3000), ("bf16", 1999, 4097), ("f32", 1801, 6000)])
+def test_norm_of_many_rows(mem, dtype, rows, D):
+    """Blocks go on to further rows: what they read ahead, and the sums in LDS that several wavefronts share, row after row."""
+    src = Source(rows + D, TYPES[dtype])
+    t = _norm_tensors(src, 1, rows, D)
+    dout, du = src.seq(1, rows, D), src.seq(1, rows, D)
+    (out, u), want = ref.gradients(ref.norm, t, (dout, du))
+    g = {k: plain(v) if k in ("scale", "post_weight", "pre_weight") else src.gpu(v) for k, v in t.items()}
+    got_out, got_u = mem.residual_norm(**g)
+    close("out", got_out, out, 4)
+    close("u", got_u, u, 4)
+    got = mem.residual_norm_backward(src.gpu(dout), src.gpu(du), **g)
+    for name, value in got._asdict().items():
+        close("gradient of " + name, value, want[name], rows if name in ("post_weight", "scale", "pre_weight") else 16)
 
 
 def test_norm_gradients_against_differences(mem):
