@@ -287,6 +287,43 @@ def test_scan_steps_equal_the_sequence(mem):
     close("its state", end, h, N * 64)
 
 
+@pytest.mark.parametrize("dtype,n,D,N,G", [("bf16", 3001, 136, 16, 2), ("f32", 9001, 60, 8, 3), ("f16", 2003, 130, 32, 1)])
+def test_scan_step_of_many_environments(mem, dtype, n, D, N, G):
+    """A thread takes environments in turn, the next one's state under way while one is written in place."""
+    src = Source(n + D, TYPES[dtype])
+    t = scan_inputs(src, 1, n, D, N, G, True, True)
+    g = scan_gpu(src, t)
+    for flags in (src.flags(1, n, 0.3), None):
+        y, h = ref.scan(**t, first=flags)
+        held = g["state"].clone()
+        got, same = mem.selective_scan_step(g["x"][0], g["delta"][0], g["a"], g["b"][0], g["c"][0], held, d=g["d"], z=g["z"][0], delta_bias=g["delta_bias"],
+                                            first=None if flags is None else flags[0].cuda())
+        assert same is held
+        close("y", got, y[0], N * 64)
+        close("state", held, h, N * 64)
+
+
+@pytest.mark.parametrize("dtype,T,n,D,N,G", [("f32", 13, 2500, 130, 16, 2), ("bf16", 20, 3001, 40, 32, 1)])
+def test_scan_of_many_environments(mem, dtype, T, n, D, N, G):
+    """Blocks of the backward pass go on to further environments, of unequal lengths, with the gradients of a, d and delta_bias kept over them."""
+    src = Source(n + D, TYPES[dtype])
+    t = scan_inputs(src, T, n, D, N, G, True, True)
+    first, lengths = src.flags(T, n, 0.1), torch.randint(0, T + 1, (n,), generator=src.gen, dtype=torch.int32)
+    dy, dstate = src.seq(T, n, D), src.normal(n, D, N)
+    (y, h), want = ref.gradients(ref.scan, t, (dy, dstate), first=first, lengths=lengths)
+    g = scan_gpu(src, t)
+    how = {k: g[k] for k in ("d", "z", "delta_bias", "state")}
+    how.update(first=first.cuda(), lengths=lengths.cuda())
+    args = [g[k] for k in ("x", "delta", "a", "b", "c")]
+    got_y, got_h, saved = mem.selective_scan(*args, save=True, **how)
+    close("y", got_y, y, N * T)
+    close("state", got_h, h, N * T)
+    got = mem.selective_scan_backward(src.gpu(dy), saved, *args, dstate=plain(dstate), **how)
+    terms = {"b": N * T + D // G, "c": N * T + D // G, "a": N * T + T * n, "d": T * n, "delta_bias": N * T + T * n}
+    for name, value in got._asdict().items():
+        close("gradient of " + name, value, want[name], terms.get(name, N * T))
+
+
 def test_scan_gradients_against_differences(mem):
     """Along a random direction of all inputs: central differences of step 2^-7 of the kernel's own forward pass.  Their
     error: the third derivative, some units times 2^-14 / 6, and the roundings of some 5,000 outputs of size 1
@@ -472,6 +509,39 @@ def test_conv_forgets_infinities_and_ignores_dead_steps(mem):
     close("gradient of x", got.x, want["x"], 2 * K)
     close("gradient of the state", got.state, want["state"], 2 * K)
     close("gradient of bias", got.bias, want["bias"], T * n)
+
+
+@pytest.mark.parametrize("dtype,T,n,D,K", [("bf16", 9, 5003, 260, 4), ("f32", 40, 2501, 67, 3), ("f16", 3, 30011, 30, 2)])
+def test_conv_of_many_environments(mem, dtype, T, n, D, K):
+    """Threads of the backward pass go on to further environments, with the gradients of weight and bias kept over them."""
+    src = Source(n + D, TYPES[dtype])
+    t = {"x": src.seq(T, n, D), "weight": src.normal(D, K, spread=0.5), "bias": src.normal(D), "state": src.normal(n, K - 1, D, dtype=TYPES[dtype])}
+    first, lengths = src.flags(T, n, 0.15), torch.randint(0, T + 1, (n,), generator=src.gen, dtype=torch.int32)
+    dy, dstate = src.seq(T, n, D), src.normal(n, K - 1, D, dtype=TYPES[dtype])
+    for flags in (first, None):
+        (y, tail), want = ref.gradients(ref.conv, t, (dy, dstate), first=flags, lengths=lengths)
+        how = {"state": t["state"].to("cuda", TYPES[dtype]), "first": None if flags is None else flags.cuda(), "lengths": lengths.cuda()}
+        args = (src.gpu(t["x"]), plain(t["weight"]), plain(t["bias"]))
+        got_y, got_tail = mem.causal_conv(*args, **how)
+        close("y", got_y, y, K + 1)
+        assert torch.equal(got_tail.cpu().double(), tail)
+        got = mem.causal_conv_backward(src.gpu(dy), *args, dstate=dstate.to("cuda", TYPES[dtype]), **how)
+        for name, value in got._asdict().items():
+            close("gradient of " + name, value, want[name], T * n if name in ("weight", "bias") else 2 * K)
+
+
+@pytest.mark.parametrize("dtype,n,D,K", [("bf16", 2000, 1027, 4), ("f32", 5001, 516, 3), ("f16", 60001, 13, 2)])
+def test_conv_step_of_many_environments(mem, dtype, n, D, K):
+    """A thread takes environments in turn, the next one's state under way while one is written in place."""
+    src = Source(n + D, TYPES[dtype])
+    x, weight, bias, state = src.seq(1, n, D), src.normal(D, K, spread=0.5), src.normal(D), src.normal(n, K - 1, D, dtype=TYPES[dtype])
+    for flags in (src.flags(1, n, 0.3), None):
+        y, tail = ref.conv(x, weight, bias, state, flags)
+        held = state.to("cuda", TYPES[dtype])
+        got, same = mem.causal_conv_step(src.gpu(x)[0], plain(weight), plain(bias), held, first=None if flags is None else flags[0].cuda())
+        assert same is held
+        close("y", got, y[0], K + 1)
+        assert torch.equal(held.cpu().double(), tail)
 
 
 def test_conv_gradients_against_differences(mem):
