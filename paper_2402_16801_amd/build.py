@@ -16,6 +16,7 @@ HIPCC_FLAGS = [
 
 
 DEBUG_OUT = os.path.join(_PKG, "libcraftax_hip_debug.so")
+HEADER = os.path.join(os.path.dirname(_PKG), "include", "craftax.h")
 
 
 def build_library(verbose: bool = False, only_changed: bool = False, debug_bounds: bool = False) -> str:
@@ -28,7 +29,7 @@ def build_library(verbose: bool = False, only_changed: bool = False, debug_bound
     objdir = os.path.join(_PKG, "_build_debug" if debug_bounds else "_build")
     os.makedirs(objdir, exist_ok=True)
     csrc = os.path.join(_PKG, "csrc")
-    deps = [os.path.join(csrc, f) for f in os.listdir(csrc)] + [os.path.join(os.path.dirname(_PKG), "include", "craftax.h")]
+    deps = [os.path.join(csrc, f) for f in os.listdir(csrc) if not f.endswith(".cpp")] + [HEADER]
     newest = max(os.path.getmtime(d) for d in deps)
     flags = [f for f in HIPCC_FLAGS if f != "-shared"] + (["-DCRAFTAX_DEBUG_BOUNDS"] if debug_bounds else [])
     out = DEBUG_OUT if debug_bounds else OUT
@@ -60,8 +61,10 @@ MARSHAL_SRC = os.path.join(_PKG, "csrc", "marshal.cpp")
 MARSHAL_OUT = os.path.join(_PKG, "_marshal.so")
 
 
-def build_marshal() -> str:
-    """The Python extension that hands tensors to the C ABI (see memory.py)."""
+def build_marshal(only_changed: bool = False) -> str:
+    """The Python extension that hands tensors to the C ABI (see memory.py); only_changed as for the library."""
+    if only_changed and os.path.exists(MARSHAL_OUT) and os.path.getmtime(MARSHAL_OUT) >= max(map(os.path.getmtime, (MARSHAL_SRC, HEADER))):
+        return MARSHAL_OUT
     import sysconfig
 
     from torch.utils.cpp_extension import include_paths, library_paths
@@ -84,7 +87,7 @@ def build_all(only_changed: bool = False):
     with ThreadPoolExecutor(max_workers=3) as ex:
         a = ex.submit(build_library, False, only_changed, False)
         b = ex.submit(build_library, False, only_changed, True)
-        c = ex.submit(build_marshal)
+        c = ex.submit(build_marshal, only_changed)
         c.result()
         return a.result(), b.result()
 

@@ -85,3 +85,24 @@ def test_the_returns_of_the_example_go_on_behind_the_rollout():
     chance = torch.tensor(1.0 / example.ACTIONS, dtype=torch.float64)
     want = -(chance.log() * (returns - values)).mean() + 0.5 * (returns - values).square().mean() + 0.01 * chance.log()
     assert abs(float(loss - want)) <= 1e-12
+
+
+def test_quick_builds_compile_what_has_changed(monkeypatch):
+    """only_changed: neither the extension nor, behind a change of the extension's source, the kernels are compiled again."""
+    from paper_2402_16801_amd import build
+    ran = []
+
+    class Done:
+        returncode, stderr = 0, ""
+
+    monkeypatch.setattr(build.subprocess, "run", lambda cmd, **how: ran.append(cmd) or Done())
+    monkeypatch.setattr(build.os, "makedirs", lambda *a, **k: None)
+    monkeypatch.setattr(build.os.path, "exists", lambda p: True)
+    age = {".cpp": 3, ".o": 2, ".so": 4}                       # everything else: 1
+    monkeypatch.setattr(build.os.path, "getmtime", lambda p: age.get(os.path.splitext(p)[1], 1))
+    build.build_all(only_changed=True)
+    assert len(ran) == 2 and all("-c" not in cmd for cmd in ran)           # the two libraries are linked
+    del ran[:]
+    age[".so"] = 2
+    build.build_all(only_changed=True)
+    assert len(ran) == 3 and sum(build.MARSHAL_SRC in cmd for cmd in ran) == 1
