@@ -166,7 +166,7 @@ template <typename E, int N> struct WalkShared {
     {
         const int lane = (int)(threadIdx.x & (WAVE - 1)), piece = lane % 8;
         step = piece < 4 ? p.b.step : p.c.step;
-        at = (piece < 4 ? p.b.at(t, i) : p.c.at(t, i)) + w.group * N + (piece & 3) * Lay<N>::LANES + lane / 8 * step;
+        at = (piece < 4 ? p.b.at(t, i) : p.c.at(t, i)) + (int64_t)w.group * N + (piece & 3) * Lay<N>::LANES + lane / 8 * step;
     }
     __device__ __forceinline__ void move(int blocks) { at += blocks * BLOCK * step; }
     __device__ __forceinline__ void load(int count)
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_token(const ScanParams<E>
     if (!on) i = p.part - 1;
     const uint32_t rest = at % per_env;
     const int channel = (int)(rest / QUADS), quad = (int)(rest % QUADS);
-    const int shared = channel / p.group_channels * N + quad * 4;
+    const int64_t shared = (int64_t)(channel / p.group_channels) * N + quad * 4;
     float a4[4];
     load4(p.a + (int64_t)rest * 4, a4);
 #pragma unroll

@@ -448,7 +448,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_shared(const ScanParams<E
     const int value = (int)(at % (2 * N));
     const int64_t row = at / (2 * N);                  // (step, environment, group)
     if (row >= (int64_t)p.steps * p.n * p.groups) return;
-    const int group = (int)(row % p.groups);
+    const int64_t group = row % p.groups;
     const int64_t token = row / p.groups;
     const float* q = p.shared_part + row * p.group_blocks * (2 * N) + value;
     float s = 0.0f;

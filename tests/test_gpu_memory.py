@@ -421,6 +421,33 @@ def test_scan_of_more_wavefronts_than_one_dimension_takes(mem):
     torch.cuda.empty_cache()
 
 
+def test_scan_of_groups_and_states_beyond_two_to_the_31(mem):
+    """2^26 + 2^16 groups of one channel of 32 states: b and c of one step have more values than 31 bits count.  As 2^16 of them alone."""
+    P, R, N = 1 << 16, (1 << 10) + 1, 32
+    src = Source(53, torch.bfloat16)
+    t = scan_inputs(src, 1, 1, P, N, 1, False, True)
+    t["b"], t["c"] = src.seq(1, 1, P, N), src.seq(1, 1, P, N)
+    g, dy = scan_gpu(src, t), src.gpu(src.seq(1, 1, P))
+
+    def run(times):
+        args = [g[k].repeat(1, 1, times, *[1] * (g[k].dim() - 3)) if k != "a" else g[k].repeat(times, 1) for k in ("x", "delta", "a", "b", "c")]
+        how = {"d": g["d"].repeat(times), "delta_bias": g["delta_bias"].repeat(times)}
+        state = g["state"].repeat(1, times, 1)
+        out = {}
+        out["y of a token"], out["state of a token"] = mem.selective_scan_step(args[0][0], args[1][0], args[2], args[3][0], args[4][0], state.clone(), **how)
+        y, _, saved = mem.selective_scan(*args, state=state, save=True, **how)
+        grads = mem.selective_scan_backward(dy.repeat(1, 1, times), saved, *args, state=state, **how)
+        return {"y": y, **out, "x": grads.x, "delta": grads.delta, "b": grads.b, "c": grads.c, "a": grads.a, "state": grads.state}
+
+    torch.cuda.empty_cache()
+    small = run(1)
+    for name, got in run(R).items():
+        axis = {"y of a token": 1, "state of a token": 1, "a": 0, "state": 1}.get(name, 2)
+        assert all(torch.equal(v, small[name]) for v in got.split(P, axis)), name
+    del got
+    torch.cuda.empty_cache()
+
+
 # ---- convolution ------------------------------------------------------------------------------------------
 
 CONV_CASES = [
