@@ -121,19 +121,20 @@ __device__ __forceinline__ float wave_sum(float v)
     return p.a + p.b;
 }
 
-// the block's number in a launch that lies over x and z (see spread)
-__device__ __forceinline__ int64_t spread_block() { return (int64_t)blockIdx.z * gridDim.x + blockIdx.x; }
+// the block's number in a launch that lies over x and z (see spread), `wide` blocks in x: an argument, since the grid's own size arrives
+// later than those
+__device__ __forceinline__ int64_t spread_block(unsigned wide) { return (int64_t)((uint64_t)blockIdx.z * wide + blockIdx.x); }
 
 // ---- sums of partial results -----------------------------------------------------------------------
 // put(c, sum over rows of part[row][c]) for every column: a block takes 16 columns, 16 threads each add
 // every 16th row, in a fixed order.
 constexpr int SUM_COLUMNS = 16, SUM_ROWS = 16;
 template <typename Put>
-static __global__ __launch_bounds__(SUM_COLUMNS* SUM_ROWS) void k_sum_rows(const float* part, int rows, int64_t columns, Put put)
+static __global__ __launch_bounds__(SUM_COLUMNS* SUM_ROWS) void k_sum_rows(const float* part, int rows, int64_t columns, unsigned wide, Put put)
 {
     __shared__ float sums[SUM_ROWS][SUM_COLUMNS];
     const int x = threadIdx.x % SUM_COLUMNS, y = threadIdx.x / SUM_COLUMNS;
-    const int64_t c = spread_block() * SUM_COLUMNS + x;
+    const int64_t c = spread_block(wide) * SUM_COLUMNS + x;
     constexpr int GO = 8;
     float s = 0.0f;
     if (c < columns) {
@@ -177,7 +178,7 @@ inline int launched(const char** why)
 template <typename Put> inline void sum_rows(const float* part, int rows, int64_t columns, Put put, hipStream_t st)
 {
     const Spread grid = spread(ceil_div(columns, SUM_COLUMNS), SUM_COLUMNS * SUM_ROWS);
-    hipLaunchKernelGGL(k_sum_rows<Put>, dim3(grid.x, 1, grid.z), dim3(SUM_COLUMNS * SUM_ROWS), 0, st, part, rows, columns, put);
+    hipLaunchKernelGGL(k_sum_rows<Put>, dim3(grid.x, 1, grid.z), dim3(SUM_COLUMNS * SUM_ROWS), 0, st, part, rows, columns, grid.x, put);
 }
 
 template <typename E> Seq<E> seq(const craftax_view& v) { return {static_cast<E*>(v.data), v.step, v.env}; }

@@ -259,7 +259,7 @@ template <typename E, int K, int V>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E> p)
 {
     const uint32_t at = blockIdx.x * CONV_THREADS + threadIdx.x;
-    const int i = (int)(at / (uint32_t)p.vectors);
+    int i = (int)(at / (uint32_t)p.vectors);
     if (i >= p.stretch) return;                 // here: environments that are taken side by side
     const Span w = Span::of<V>((int)(at % (uint32_t)p.vectors), p.channels);
     Taps<K, V> taps;
@@ -276,8 +276,7 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E>
         if (p.lengths) length = p.lengths[e];
     };
     load(i);
-    // unsigned: the environment behind a thread's last one may be beyond 2^31
-    for (uint32_t at_env = (uint32_t)i, side = (uint32_t)p.stretch, n = (uint32_t)p.n; at_env < n; at_env += side) {
+    for (; i < p.n; i += p.stretch) {
         float win[K - 1][V], x[V], y[V];
         const bool live = length > 0, empty = !p.state_in || (flag && live);
 #pragma unroll
@@ -297,8 +296,8 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E>
             const float v = taps.sum(win, x[j], j), g = sigmoid(v);
             y[j] = live ? v * (p.silu ? g : 1.0f) : 0.0f;
         }
-        const int e = (int)at_env;
-        if (at_env + side < n) load((int)(at_env + side));
+        const int e = i;
+        if (i + p.stretch < p.n) load(i + p.stretch);
         put<E, V>(p.y.at(0, e) + w.c, w, shrink<E, V>(y));
         if (p.state_out) {
 #pragma unroll
@@ -571,8 +570,7 @@ int conv(const craftax_conv_args* a, void* stream, const char** why)
             const int64_t threads = (int64_t)a->n * p.vectors;
             if (a->steps == 1) {
                 // environments side by side: two wavefronts per SIMD, each with several environments in turn, or all of them
-                const int64_t side = ceil_div(CONV_FILL / 2, p.vectors);
-                p.stretch = (int)(side < a->n ? side : a->n);
+                p.stretch = side_by_side(ceil_div(CONV_FILL / 2, p.vectors), a->n);
                 const dim3 grid((unsigned)ceil_div((int64_t)p.stretch * p.vectors, CONV_THREADS));
                 hipLaunchKernelGGL((k_conv_token<E, K, V>), grid, dim3(CONV_THREADS), 0, st, p);
                 return;

@@ -19,6 +19,14 @@ inline Spread spread(int64_t blocks, int threads)
     return {(unsigned)x, (unsigned)z};
 }
 
+// Environments that are taken side by side by kernels whose threads go on by that many: `want` or all of them, and so few that what is
+// behind the last one still has a number.
+inline int side_by_side(int64_t want, int n)
+{
+    const int64_t room = ((int64_t)1 << 31) - n, side = want < n ? want : n;
+    return (int)(side < room ? side : room);
+}
+
 // Whether the scan's kernel for one token can number its threads in 32 bits (states / 4 of them to a channel, and a chip full of them
 // more); the kernel for sequences takes what it cannot.
 inline bool token_fits(int64_t channels, int states) { return channels * (states / 4) <= (int64_t)1 << 31; }

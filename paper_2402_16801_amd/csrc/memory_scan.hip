@@ -50,6 +50,7 @@ template <typename E> struct ScanParams {
     float* weight_part;    // backward: [rows][channels][N + 2] sums for da, dd and ddelta_bias
     int steps, n, channels, groups, group_channels, group_tiles, tiles, softplus;
     int part, parts;       // steps per part (whole blocks), number of parts
+    unsigned wide;         // blocks in x (see spread)
     int own_starts;        // wavefronts find the starts of their parts themselves (see part_start)
     int rows, group_blocks;          // backward: rows of weight_part, blocks per group
 };
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5)
     __shared__ float4 shared_lds[SCAN_WAVES][BLOCK * N / 2];
     __shared__ float2 step_lds[SCAN_WAVES][BLOCK * CHANNELS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int64_t item = spread_block() * SCAN_WAVES + wave;
+    const int64_t item = spread_block(p.wide) * SCAN_WAVES + wave;
     if (item >= (int64_t)p.n * p.tiles) return;
     const int i = (int)(item / p.tiles);
     const Tile w = tile_of<N>(p, (int)(item % p.tiles));
@@ -521,8 +522,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_token(const ScanParams<E>
         if (p.lengths) length = p.lengths[e];
     };
     load(i);
-    // unsigned: the environment behind a thread's last one may be beyond 2^31
-    for (uint32_t at_env = (uint32_t)i, side = (uint32_t)p.part, n = (uint32_t)p.n; at_env < n; at_env += side) {
+    for (; i < p.n; i += p.part) {
         const bool alive = length > 0, begin = flag != 0;
         float size = Elem<E>::up(delta) + bias;
         if (p.softplus) size = softplus(size);
@@ -535,8 +535,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_token(const ScanParams<E>
             h[m] = alive ? next : old[m];
             out = __builtin_fmaf(next, Elem<E>::up(c.v[m]), out);
         }
-        const int e = (int)at_env;
-        if (at_env + side < n) load((int)(at_env + side));
+        const int e = i;
+        if (i + p.part < p.n) load(i + p.part);
         out += dpp<DPP_XOR1>(out);
         if constexpr (QUADS >= 4) out += dpp<DPP_XOR2>(out);
         if constexpr (QUADS >= 8) out += dpp<DPP_HALF_MIRROR>(out);
@@ -761,8 +761,8 @@ int scan(const craftax_scan_args* a, void* stream, const char** why)
             constexpr int N = decltype(states)::value;
             if (scan_token(a)) {
                 // environments side by side: as many threads as the chip holds, each with several of them in turn, or all
-                const int64_t per_env = (int64_t)a->channels * (N / 4), side = ceil_div(TOKEN_FILL * WAVE, per_env);
-                p.part = (int)(side < a->n ? side : a->n);
+                const int64_t per_env = (int64_t)a->channels * (N / 4);
+                p.part = side_by_side(ceil_div(TOKEN_FILL * WAVE, per_env), a->n);
                 const dim3 grid((unsigned)ceil_div(p.part * per_env, SCAN_THREADS));
                 if (a->n * per_env * (int64_t)sizeof(float4) > TOKEN_STREAMED) hipLaunchKernelGGL((k_scan_token<E, N, true>), grid, dim3(SCAN_THREADS), 0, st, p);
                 else hipLaunchKernelGGL((k_scan_token<E, N, false>), grid, dim3(SCAN_THREADS), 0, st, p);
@@ -774,6 +774,7 @@ int scan(const craftax_scan_args* a, void* stream, const char** why)
             p.part = s.parts.part; p.parts = s.parts.parts;
             const Spread blocks = spread(ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES), SCAN_THREADS);
             const dim3 grid(blocks.x, (unsigned)p.parts, blocks.z);
+            p.wide = blocks.x;
             if (p.parts > 1) {
                 p.starts = reinterpret_cast<float4*>(base + s.starts);
                 p.decays = reinterpret_cast<float2*>(base + s.decays);
@@ -814,6 +815,7 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
             constexpr int N = decltype(states)::value;
             if (p.parts > 1) {
                 const Spread blocks = spread(ceil_div((int64_t)a->n * p.tiles, SCAN_WAVES), SCAN_THREADS);
+                p.wide = blocks.x;
                 hipLaunchKernelGGL((k_scan_back_part<E, N>), dim3(blocks.x, (unsigned)p.parts - 1, blocks.z), dim3(SCAN_THREADS), 0, st, p);
                 if ((rc = launched(why))) return;
                 p.own_starts = p.parts <= OWN_STARTS;
@@ -822,10 +824,12 @@ int scan_backward(const craftax_scan_args* a, void* stream, const char** why)
             }
             const Spread blocks = spread((int64_t)(s.rows / p.parts) * a->groups * s.group_blocks, s.waves * WAVE);
             const dim3 grid(blocks.x, (unsigned)p.parts, blocks.z);
+            p.wide = blocks.x;
             if (p.z.data) hipLaunchKernelGGL((k_scan_back<E, N, true>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
             else hipLaunchKernelGGL((k_scan_back<E, N, false>), grid, dim3(s.waves * WAVE), s.waves * scan_back_lds<N>(), st, p);
             if ((rc = launched(why))) return;
             const Spread sums = spread(ceil_div((int64_t)a->steps * a->n * a->groups * 2 * N, SCAN_THREADS), SCAN_THREADS);
+            p.wide = sums.x;
             hipLaunchKernelGGL((k_scan_shared<E, N>), dim3(sums.x, 1, sums.z), dim3(SCAN_THREADS), 0, st, p, seq<E>(a->db), seq<E>(a->dc));
             if ((rc = launched(why))) return;
             sum_rows(p.weight_part, s.rows, (int64_t)a->channels * (N + 2), PutScan<N>{a->da, a->dd, a->ddelta_bias}, st);

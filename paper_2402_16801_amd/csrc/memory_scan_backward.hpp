@@ -111,7 +111,7 @@ __global__ __launch_bounds__(SCAN_BACK_WAVES* WAVE) __attribute__((amdgpu_waves_
     float4* step_lds = lds + waves * (BLOCK * N / 2) + wave * (BLOCK * CHANNELS);        // [step][channel]: D, D x, dy, x
     float* sum_lds = reinterpret_cast<float*>(lds + waves * (BLOCK * N / 2 + BLOCK * CHANNELS));   // [turn][wave][step][2 N]
     const int blocks = given.groups * given.group_blocks;
-    const unsigned block = (unsigned)spread_block();
+    const unsigned block = (unsigned)spread_block(given.wide);
     const int group_block = (int)(block % (unsigned)blocks);
     const int env_row = (int)(block / (unsigned)blocks), env_rows = given.rows / given.parts;
     if (env_row >= env_rows) return;
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
     __shared__ float4 shared_lds[SCAN_WAVES][BLOCK * N / 2];
     __shared__ float2 step_lds[SCAN_WAVES][BLOCK * CHANNELS];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int64_t item = spread_block() * SCAN_WAVES + wave;
+    const int64_t item = spread_block(p.wide) * SCAN_WAVES + wave;
     if (item >= (int64_t)p.n * p.tiles) return;
     const int i = (int)(item / p.tiles);
     const Tile w = tile_of<N>(p, (int)(item % p.tiles));
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_scan_back_part(const ScanParam
 template <typename E, int N>
 __global__ __launch_bounds__(SCAN_THREADS) void k_scan_shared(const ScanParams<E> p, Seq<E> db, Seq<E> dc)
 {
-    const int64_t at = spread_block() * SCAN_THREADS + threadIdx.x;
+    const int64_t at = spread_block(p.wide) * SCAN_THREADS + threadIdx.x;
     const int value = (int)(at % (2 * N));
     const int64_t row = at / (2 * N);                  // (step, environment, group)
     if (row >= (int64_t)p.steps * p.n * p.groups) return;

@@ -31,6 +31,13 @@ int main()
             if (token_fits(channels, states)) expect(per_env + 2 * 524288 + 512 < (int64_t)1 << 32, "threads of a token", channels, states);
             else expect(per_env > (int64_t)1 << 31, "a token that would fit", channels, states);
         }
+    // environments side by side: at least one, no more than there are or are wanted, and the one behind the last is a number
+    for (int64_t want : {(int64_t)1, (int64_t)512, (int64_t)131072, (int64_t)1 << 31, (int64_t)1 << 34})
+        for (int n : {1, 2, 511, 4096, 131073, 2147483647 - 524288, (int)MOST_COUNT - 1, (int)MOST_COUNT}) {
+            const int side = side_by_side(want, n);
+            expect(side >= 1 && side <= n && side <= want && (int64_t)n - 1 + side <= 2147483647, "environments side by side", want, n);
+            if (n <= 2147483647 - 524288 && want <= 524288) expect(side == (want < n ? want : n), "all that are wanted", want, n);
+        }
     std::printf(failures ? "memory_grid_test: %d failures\n" : "memory_grid_test: ok\n", failures);
     return failures ? 1 : 0;
 }
