@@ -481,7 +481,7 @@ int craftax_selective_scan_backward(const craftax_scan_args *args, void *stream)
  *   out    = residual + branch * scale * act(gate)
  *   u      = out * r(out) * pre_weight          (norm before the next block)
  * u is computed from out before out is rounded.  out and residual are of `residual_dtype`, the other
- * activations of `dtype`. */
+ * activations of `dtype`.  An infinity makes its row's r 0, wherever it lies and however long the row is. */
 enum { CRAFTAX_GATE_SIGMOID = 0, CRAFTAX_GATE_SILU = 1, CRAFTAX_GATE_LINEAR = 2 };
 typedef struct craftax_norm_args {
     uint32_t dtype;

@@ -188,7 +188,8 @@ template <int AHEAD> struct Begins {
 };
 
 // CUTS: begins of episodes are given.  64 steps of 4,096 environments of 512 channels in bfloat16: 150 us, 3.6 TB/s; 2,048
-// environments in float32 117 us, 4.6 TB/s.
+// environments in float32 117 us, 4.6 TB/s.  Registers leave room for five wavefronts per SIMD (seven of 16-bit types without
+// begins) where a rollout of that size launches eight.
 template <typename E, int K, int V, bool CUTS>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv(const ConvParams<E> p)
 {
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(CONV_THREADS) void k_conv_token(const ConvParams<E>
 // for the weight.  A block sums its weight gradients in LDS and writes one partial row; rows are added in a
 // fixed order by a second kernel.  Two wavefronts per SIMD is what the registers leave room for (weights, their gradients,
 // both windows and what is read ahead); vector issue is at about two thirds of the time.  64 steps of 4,096 environments of 512 channels in
-// bfloat16: 196 us, 4.1 TB/s, with begins 238.
+// bfloat16: 196 us, 4.1 TB/s, with begins 236 (their flags are loaded and tested by every thread for itself, step by step).
 template <typename E, int K, int V, bool CUTS>
 __global__ __launch_bounds__(CONV_THREADS) void k_conv_backward(const ConvParams<E> p)
 {

@@ -12,7 +12,8 @@
 // values per lane (backward 8); with one wavefront every sum stays inside it, with more the sums meet in LDS.
 // Blocks go on to further rows with the weights, and in the backward pass their gradients, in registers.
 // 262,144 rows of 512 values in bfloat16 with a gate: forward 250 us, 5.3 TB/s; backward 500 us, 4.3 TB/s, with vector issue
-// at about half beside it (131,072 rows in float32: 259 us, 5.2 TB/s, and 418, 5.1).
+// at about half beside it (131,072 rows in float32: 258 us, 5.2 TB/s, and 418, 5.1).  Beyond 4,096 values the backward pass has no room for a
+// row's eight arrays: 112 to 276 bytes of scratch a lane (16,384 rows of 8,192 bfloat16: 640 us, 3.4 TB/s).
 #include "memory_api.hpp"
 #include "memory_common.hpp"
 
@@ -435,7 +436,9 @@ struct PutNorm {
 namespace host {
 
 constexpr int NORM_CHANNELS = 8192;
-constexpr int NORM_WAVES = 6, NORM_BACK_WAVES = 2;       // wavefronts per SIMD that are launched at most: those that are there at once
+// Wavefronts per SIMD that are launched at most.  Backward all are there at once.  Forward a SIMD holds five to eight of the kernels with up to
+// eight values per lane, and two or three of those with sixteen, so that these blocks follow one another.
+constexpr int NORM_WAVES = 6, NORM_BACK_WAVES = 2;
 
 static int norm_check(const craftax_norm_args* a, bool backward, const char** why)
 {

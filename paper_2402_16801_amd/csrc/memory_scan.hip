@@ -279,8 +279,10 @@ __device__ __forceinline__ void part_start(const ScanParams<E>& p, int part, int
 // state.  SAVE: the states before every block are kept for a backward pass (streamed: they are read long after).  The
 // activations of the next block are under way while a block is computed.  Eight wavefronts to a block of threads put the
 // rows of 128 channels side by side in time.  64 steps of 4,096 environments of 512 channels in 16 bits, with a gate:
-// 750 us, with saved states 875 (998 with four wavefronts and cached stores); vector instructions issue 3/4 of the time.  Where
-// wavefronts are fewer than two per SIMD, a step takes one 175 ns, its own rate of issue.
+// 750 us, with saved states 860 (998 with four wavefronts and cached stores); vector instructions issue 3/4 of the time.  That is 105 ns
+// of its SIMD for a step of a wavefront.  A block is eight wavefronts, two to a SIMD, whatever the launch: two on a SIMD take 172 ns
+// a step together, one alone 135 (measured in one block of one to four live wavefronts), so that few environments with long
+// sequences run at 172 ns a step on the compute units that have a block, and the others idle.
 enum ScanMode { RUN, SAVE, PART_ONLY };
 template <typename E, int N, ScanMode MODE, bool GATE>
 __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(5))) void k_scan(const ScanParams<E> p)
@@ -632,9 +634,11 @@ static unsigned carry_threads(int parts) { return (unsigned)(parts < CARRY_WAVES
 // streamed 106 us, through the caches 117, 2.1 GB 924 and 998; below it a token finds the state of the one before
 // (33 MB through the caches 12.6 us, streamed 14.8).
 constexpr int64_t TOKEN_STREAMED = (int64_t)192 << 20;
-constexpr int64_t SCAN_FILL = (int64_t)CHIP_SIMDS * 5;           // wavefronts that the chip holds of k_scan,
-constexpr int64_t SCAN_BACK_FILL = (int64_t)CHIP_SIMDS * 2;      // of k_scan_back,
-constexpr int64_t TOKEN_FILL = (int64_t)CHIP_SIMDS * 8;          // of k_scan_token
+// Wavefronts that a launch is to have for a full chip.  Registers leave room for five per SIMD of k_scan, but a block is eight or none, so
+// that four are there at once and the last parts of a split sequence follow behind the others.
+constexpr int64_t SCAN_FILL = (int64_t)CHIP_SIMDS * 5;
+constexpr int64_t SCAN_BACK_FILL = (int64_t)CHIP_SIMDS * 2;      // k_scan_back: what is there at once,
+constexpr int64_t TOKEN_FILL = (int64_t)CHIP_SIMDS * 8;          // k_scan_token: too
 
 static bool scan_shape_ok(const craftax_scan_args* a)
 {
@@ -684,8 +688,10 @@ static ScanSpace scan_space(const craftax_scan_args* a, bool backward)
         const int64_t side = each < room ? room / each : 1, turns = ceil_div(a->n, side);
         s.rows = (int)ceil_div(a->n, turns) * s.parts.parts;
     } else {
-        // Split steps cost the recurrence of the states twice, 1.7 times the work: a quarter of the chip is filled better without
-        // (100 steps of 64 environments of 512 channels: 24 us, in two parts 46).
+        // Split steps cost the recurrence of the states twice, 1.7 times the work: sequences that fill a quarter of the chip are not split
+        // (100 steps of 64 environments of 512 channels: 24 us, in two parts 46; 1,000 steps of them 162, in parts for two or four times
+        // the wavefronts 198).  The line is between sizes, not at the best of each: 1,000 steps of 37 ragged environments of 648 channels
+        // are not split, 173 us, and take 152 in such parts.
         const int64_t want = SCAN_FILL / ((int64_t)a->n * t.tiles);
         s.parts = scan_parts(a, want < 4 ? 1 : want);
     }
