@@ -505,6 +505,85 @@ size_t craftax_residual_norm_workspace_bytes(const craftax_norm_args *args);
 int craftax_residual_norm(const craftax_norm_args *args, void *stream);
 int craftax_residual_norm_backward(const craftax_norm_args *args, void *stream);
 
+/* Gated linear recurrence of every channel, one state each:
+ *   a = exp(rate * sigmoid(decay)),  h = a * h + sqrt(1 - a * a) * sigmoid(intake) * x,  y = h * z * sigmoid(z)
+ * (the last factors only with a gate z).  rate is at most 0; above it the root counts as 0.  Where a is 1 the root has no derivative and
+ * none is counted for it.  The state h is float[n][channels].
+ * For a backward pass the forward call leaves the states at regular steps in `saved` (DEVICE, 256-byte aligned,
+ * craftax_gated_recurrence_saved_bytes() long); the backward call gets it with the same inputs, except that state_in is not read. */
+typedef struct craftax_recurrence_args {
+    uint32_t dtype;             /* of x, decay, intake, z, y and their gradients */
+    int32_t steps, n, channels; /* all positive, steps and n * channels below 2^31 - 4095 */
+    const float *rate;          /* [channels] */
+    craftax_view first;         /* uint8, or absent */
+    const int32_t *lengths;     /* or NULL */
+    craftax_view x, decay, intake, z, y;   /* z may be absent */
+    const float *state_in;      /* or NULL: 0 */
+    float *state_out;           /* or NULL; may be state_in */
+    void *saved;                /* or NULL: no backward pass follows */
+    /* craftax_gated_recurrence_backward only: y and state_out are neither read nor written */
+    craftax_view dy, dx, ddecay, dintake, dz;
+    const float *dstate_out;    /* gradient of state_out, or NULL: 0 */
+    float *dstate_in;           /* gradient of state_in, or NULL */
+    float *drate;               /* [channels], or NULL if not wanted */
+    void *workspace;
+    size_t workspace_bytes;
+} craftax_recurrence_args;
+size_t craftax_gated_recurrence_saved_bytes(const craftax_recurrence_args *args);
+/* backward: 0 for craftax_gated_recurrence, 1 for craftax_gated_recurrence_backward */
+size_t craftax_gated_recurrence_workspace_bytes(const craftax_recurrence_args *args, int backward);
+int craftax_gated_recurrence(const craftax_recurrence_args *args, void *stream);
+int craftax_gated_recurrence_backward(const craftax_recurrence_args *args, void *stream);
+
+/* Matrix product of every token with an epilogue:
+ *   pre = x * weight^T + bias,  out = residual + act(pre)
+ * act: nothing, max(v, 0), v * sigmoid(v), or v * sigmoid(2 sqrt(2 / pi) (v + 0.044715 v^3)), the GELU with a hyperbolic tangent.  x is
+ * [inputs] values per step and environment, out [outputs].  Element (o, i) of weight lies at weight[o * weight_row + i * weight_column],
+ * and one of the two strides is 1.  pre, rounded to dtype, is what the backward call needs unless act is CRAFTAX_ACT_NONE.
+ * Backward: dp = dout * act'(pre), dx = dp * weight, dweight = dp^T * x, dbias = the sum of dp (the gradient of residual is dout).  The
+ * products take dp rounded to dtype, the sum of dbias does not.  Sums are in 32 bits. */
+enum { CRAFTAX_ACT_NONE = 0, CRAFTAX_ACT_RELU = 1, CRAFTAX_ACT_SILU = 2, CRAFTAX_ACT_GELU_TANH = 3 };
+typedef struct craftax_projection_args {
+    uint32_t dtype;             /* of x, weight, pre and dx */
+    uint32_t out_dtype;         /* of out, residual and dout: dtype or CRAFTAX_F32 */
+    uint32_t act;               /* CRAFTAX_ACT_* */
+    int32_t steps, n;           /* steps * n rows, below 2^31 */
+    int32_t inputs, outputs;    /* positive, below 2^31 - 4095; no matrix of more than 2^42 values */
+    const void *weight;
+    int64_t weight_row, weight_column;
+    const float *bias;          /* [outputs] or NULL */
+    craftax_view x, residual, out;     /* residual may be absent: 0 */
+    craftax_view pre;           /* may be absent */
+    /* craftax_projection_backward only: residual, bias and out are neither read nor written */
+    craftax_view dout, dx;      /* dx may be absent */
+    void *dweight;              /* [outputs][inputs] of dweight_dtype, or NULL if not wanted */
+    float *dbias;               /* [outputs], or NULL if not wanted */
+    uint32_t dweight_dtype;     /* dtype or CRAFTAX_F32 */
+    void *workspace;
+    size_t workspace_bytes;
+} craftax_projection_args;
+/* backward: 0 for craftax_projection, 1 for craftax_projection_backward */
+size_t craftax_projection_workspace_bytes(const craftax_projection_args *args, int backward);
+int craftax_projection(const craftax_projection_args *args, void *stream);
+int craftax_projection_backward(const craftax_projection_args *args, void *stream);
+
+/* Dropout onto a residual: out = residual + x * 2^16 / (2^16 - t) where the mask keeps x and residual where it does not, whatever x is
+ * there; t = p * 2^16, rounded.  The mask is never stored: number c % 8 (16 bits, the lower half of a word first) of Philox4x32-10 with
+ * the counter (c / 8, env + e, step + s) and the key `seed` is at least t where channel c of environment e is kept at step s.  So a call for
+ * one token and a call for a rollout that contains it have the same mask, and the gradient of x is this call on the
+ * gradient of out, without residual.  step_at (DEVICE) is read when the kernel runs: a captured call finds other masks at every replay. */
+typedef struct craftax_dropout_args {
+    uint32_t dtype;             /* of x */
+    uint32_t out_dtype;         /* of out and residual: dtype or CRAFTAX_F32; without a residual any, if dtype is CRAFTAX_F32 */
+    int32_t steps, n, channels; /* all positive, steps * n below 2^31, channels below 2^31 - 4095 */
+    double p;                   /* 0..1 */
+    uint64_t seed;
+    int64_t step, env;          /* numbers of the first step and environment: step + steps below 2^63, env + n at most 2^32 */
+    const int64_t *step_at;     /* one number that is added to step, or NULL */
+    craftax_view x, residual, out;     /* residual may be absent: 0; out may be x or residual */
+} craftax_dropout_args;
+int craftax_residual_dropout(const craftax_dropout_args *args, void *stream);
+
 /* Debug build with bounds checks (a build of the same sources with -DCRAFTAX_DEBUG_BOUNDS, shipped
  * as libcraftax_hip_debug.so): every index the kernels form into a map, an LDS window or a staging
  * area is checked on the device; an index outside its range is counted (and replaced by 0, so that

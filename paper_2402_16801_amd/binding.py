@@ -29,6 +29,8 @@ EXPORTS = [
     "craftax_causal_conv", "craftax_causal_conv_backward", "craftax_causal_conv_workspace_bytes",
     "craftax_selective_scan", "craftax_selective_scan_backward", "craftax_selective_scan_saved_bytes", "craftax_selective_scan_workspace_bytes",
     "craftax_residual_norm", "craftax_residual_norm_backward", "craftax_residual_norm_workspace_bytes",
+    "craftax_gated_recurrence", "craftax_gated_recurrence_backward", "craftax_gated_recurrence_saved_bytes", "craftax_gated_recurrence_workspace_bytes",
+    "craftax_projection", "craftax_projection_backward", "craftax_projection_workspace_bytes", "craftax_residual_dropout",
 ]
 
 
@@ -77,6 +79,7 @@ assert STATS_DTYPE.itemsize == 408 + 8 * STATS_ACHIEVEMENTS
 
 F32, BF16, F16 = 0, 1, 2
 GATE_SIGMOID, GATE_SILU, GATE_LINEAR = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU_TANH = 0, 1, 2, 3
 
 
 def _view(name):
@@ -113,6 +116,23 @@ class NormArgs(ctypes.Structure):
                 _pointers("post_weight", "scale", "pre_weight") + _view("y") + _view("residual") + _view("gate") + _view("out") + _view("u") +
                 _view("dout") + _view("du") + _view("dy") + _view("dresidual") + _view("dgate") +
                 _pointers("dpost_weight", "dscale", "dpre_weight") + _WORKSPACE)
+
+
+class RecurrenceArgs(ctypes.Structure):
+    _fields_ = (_ints("dtype", "steps", "n", "channels") + _pointers("rate") + _view("first") + _pointers("lengths") + _view("x") + _view("decay") +
+                _view("intake") + _view("z") + _view("y") + _pointers("state_in", "state_out", "saved") + _view("dy") + _view("dx") + _view("ddecay") +
+                _view("dintake") + _view("dz") + _pointers("dstate_out", "dstate_in", "drate") + _WORKSPACE)
+
+
+class ProjectionArgs(ctypes.Structure):
+    _fields_ = (_ints("dtype", "out_dtype", "act", "steps", "n", "inputs", "outputs") + _pointers("weight") +
+                [("weight_row", ctypes.c_int64), ("weight_column", ctypes.c_int64)] + _pointers("bias") + _view("x") + _view("residual") + _view("out") +
+                _view("pre") + _view("dout") + _view("dx") + _pointers("dweight", "dbias") + _ints("dweight_dtype") + _WORKSPACE)
+
+
+class DropoutArgs(ctypes.Structure):
+    _fields_ = (_ints("dtype", "out_dtype", "steps", "n", "channels") + [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("step", ctypes.c_int64),
+                ("env", ctypes.c_int64)] + _pointers("step_at") + _view("x") + _view("residual") + _view("out"))
 
 
 class CraftaxError(RuntimeError):
@@ -182,14 +202,18 @@ def load() -> ctypes.CDLL:
     L.craftax_stats_static.argtypes = [vp, vp, i32, vp]
     L.craftax_debug_bounds.argtypes = [ctypes.POINTER(ctypes.c_uint32 * 4)]
     L.craftax_debug_bounds_selftest.argtypes = []
-    for name, args in (("causal_conv", ConvArgs), ("selective_scan", ScanArgs), ("residual_norm", NormArgs)):
+    for name, args in (("causal_conv", ConvArgs), ("selective_scan", ScanArgs), ("residual_norm", NormArgs),
+                       ("gated_recurrence", RecurrenceArgs), ("projection", ProjectionArgs)):
         for call in (name, name + "_backward"):
             getattr(L, "craftax_" + call).argtypes = [ctypes.POINTER(args), vp]
         size = getattr(L, f"craftax_{name}_workspace_bytes")
-        size.argtypes = [ctypes.POINTER(args)] + ([i32] if name == "selective_scan" else [])
+        size.argtypes = [ctypes.POINTER(args)] + ([i32] if name in ("selective_scan", "gated_recurrence", "projection") else [])
         size.restype = ctypes.c_size_t
-    L.craftax_selective_scan_saved_bytes.argtypes = [ctypes.POINTER(ScanArgs)]
-    L.craftax_selective_scan_saved_bytes.restype = ctypes.c_size_t
+    for name, args in (("selective_scan", ScanArgs), ("gated_recurrence", RecurrenceArgs)):
+        size = getattr(L, f"craftax_{name}_saved_bytes")
+        size.argtypes = [ctypes.POINTER(args)]
+        size.restype = ctypes.c_size_t
+    L.craftax_residual_dropout.argtypes = [ctypes.POINTER(DropoutArgs), vp]
     L.craftax_last_error.argtypes = []
     L.craftax_last_error.restype = ctypes.c_char_p
     _lib = L

@@ -1745,6 +1745,40 @@ int craftax_residual_norm_backward(const craftax_norm_args* args, void* stream)
     return memory_call(rc, why);
 }
 
+size_t craftax_gated_recurrence_saved_bytes(const craftax_recurrence_args* args) { return mem::host::recurrence_saved_bytes(args); }
+size_t craftax_gated_recurrence_workspace_bytes(const craftax_recurrence_args* args, int backward) { return mem::host::recurrence_workspace_bytes(args, backward != 0); }
+int craftax_gated_recurrence(const craftax_recurrence_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::recurrence(args, stream, &why);
+    return memory_call(rc, why);
+}
+int craftax_gated_recurrence_backward(const craftax_recurrence_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::recurrence_backward(args, stream, &why);
+    return memory_call(rc, why);
+}
+size_t craftax_projection_workspace_bytes(const craftax_projection_args* args, int backward) { return mem::host::projection_workspace_bytes(args, backward != 0); }
+int craftax_projection(const craftax_projection_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::projection(args, stream, &why);
+    return memory_call(rc, why);
+}
+int craftax_projection_backward(const craftax_projection_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::projection_backward(args, stream, &why);
+    return memory_call(rc, why);
+}
+int craftax_residual_dropout(const craftax_dropout_args* args, void* stream)
+{
+    const char* why = "";
+    const int rc = mem::host::dropout(args, stream, &why);
+    return memory_call(rc, why);
+}
+
 int craftax_debug_bounds(uint32_t report[4])
 {
     if (!report) return fail(CRAFTAX_E_NULL, "report is NULL");

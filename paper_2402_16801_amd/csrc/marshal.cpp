@@ -42,6 +42,14 @@ struct Library {
     int (*norm)(const craftax_norm_args*, void*);
     int (*norm_backward)(const craftax_norm_args*, void*);
     size_t (*norm_workspace)(const craftax_norm_args*);
+    int (*recurrence)(const craftax_recurrence_args*, void*);
+    int (*recurrence_backward)(const craftax_recurrence_args*, void*);
+    size_t (*recurrence_saved)(const craftax_recurrence_args*);
+    size_t (*recurrence_workspace)(const craftax_recurrence_args*, int);
+    int (*projection)(const craftax_projection_args*, void*);
+    int (*projection_backward)(const craftax_projection_args*, void*);
+    size_t (*projection_workspace)(const craftax_projection_args*, int);
+    int (*dropout)(const craftax_dropout_args*, void*);
     const char* (*last_error)();
 } g_lib = {};
 
@@ -132,14 +140,16 @@ craftax_view place(const Tensor& t, const Common& c)
     return {t.data_ptr(), c.token ? 0 : t.stride(0), t.stride(c.token ? 0 : 1)};
 }
 
-craftax_view sequence(const Tensor* t, const char* name, const Common& c, at::ScalarType type)
+// of `channels` values a token
+craftax_view sequence_of(const Tensor* t, const char* name, const Common& c, at::ScalarType type, int64_t channels)
 {
     if (!t) return {nullptr, 0, 0};
     check_kind(*t, name, type, c.device);
-    check_sequence(*t, name, c, c.channels);
-    if (c.channels != 1 && t->stride(-1) != 1) refuse("the channels of ", name, " must lie side by side");
+    check_sequence(*t, name, c, channels);
+    if (channels != 1 && t->stride(-1) != 1) refuse("the channels of ", name, " must lie side by side");
     return place(*t, c);
 }
+craftax_view sequence(const Tensor* t, const char* name, const Common& c, at::ScalarType type) { return sequence_of(t, name, c, type, c.channels); }
 
 // b or c, [..][groups][states]; rows that do not lie side by side are copied first (they are short).
 craftax_view shared(Tensor& t, const char* name, const Common& c, int64_t groups, int64_t states)
@@ -184,6 +194,13 @@ Tensor shared_like(const Tensor& t)
     Tensor out = like(t);
     if (out.stride(-2) != out.size(-1)) out = at::empty(t.sizes(), t.options());
     return out;
+}
+// Of `type` and `channels` values a token, steps and environments in the order in which they lie in t.
+Tensor like_of(const Tensor& t, const Common& c, at::ScalarType type, int64_t channels)
+{
+    if (c.token) return at::empty({c.n, channels}, c.options(type));
+    if (t.stride(0) < t.stride(1)) return at::empty({c.n, c.steps, channels}, c.options(type)).transpose(0, 1);
+    return at::empty({c.steps, c.n, channels}, c.options(type));
 }
 Tensor like_or_none(const Tensor* t) { return t ? like(*t) : Tensor(); }
 void* address(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
@@ -436,6 +453,206 @@ PyObject* residual_norm_backward(PyObject* const* v)
     return tuple({dy, dresidual, dgate, dpost, dscale, dpre});
 }
 
+// x, decay, intake, rate, z, state, first, lengths
+craftax_recurrence_args recurrence_args(const Common& c, const Tensor& x, PyObject* const* v)
+{
+    craftax_recurrence_args a = {};
+    a.dtype = type_code(c.type);
+    a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.channels = (int32_t)c.channels;
+    a.rate = dense<const float>(&need(v[3], "rate"), "rate", {c.channels}, at::kFloat, c);
+    a.first = flags(maybe(v[6], "first"), c);
+    a.lengths = dense<const int32_t>(maybe(v[7], "lengths"), "lengths", {c.n}, at::kInt, c);
+    a.x = sequence(&x, "x", c, c.type);
+    a.decay = sequence(&need(v[1], "decay"), "decay", c, c.type);
+    a.intake = sequence(&need(v[2], "intake"), "intake", c, c.type);
+    a.z = sequence(maybe(v[4], "z"), "z", c, c.type);
+    a.state_in = dense<const float>(maybe(v[5], "state"), "state", {c.n, c.channels}, at::kFloat, c);
+    return a;
+}
+
+// .., save, out_state (None: a new one)
+PyObject* gated_recurrence(PyObject* const* v)
+{
+    const Tensor& x = need(v[0], "x");
+    const Common c(x, "x");
+    craftax_recurrence_args a = recurrence_args(c, x, v);
+    const Tensor y = like(x);
+    Tensor out, saved;
+    if (const Tensor* given = maybe(v[9], "out_state")) {
+        a.state_out = dense<float>(given, "out_state", {c.n, c.channels}, at::kFloat, c);
+        check_writable(*given);
+        out = *given;
+    } else {
+        out = at::empty({c.n, c.channels}, c.options(at::kFloat));
+        a.state_out = out.data_ptr<float>();
+    }
+    a.y = place(y, c);
+    if (truth(v[8])) {
+        saved = bytes(g_lib.recurrence_saved ? g_lib.recurrence_saved(&a) : 0, c);
+        a.saved = address(saved);
+    }
+    const Tensor work = bytes(g_lib.recurrence_workspace ? g_lib.recurrence_workspace(&a, 0) : 0, c);
+    a.workspace = address(work);
+    a.workspace_bytes = work.defined() ? (size_t)work.numel() : 0;
+    call(g_lib.recurrence, a, c);
+    if (v[9] != Py_None) written(out);
+    return tuple({y, out, saved});
+}
+
+// .., saved, dy, dstate
+PyObject* gated_recurrence_backward(PyObject* const* v)
+{
+    const Tensor &x = need(v[0], "x"), &decay = need(v[1], "decay"), &intake = need(v[2], "intake"), &rate = need(v[3], "rate");
+    const Tensor *z = maybe(v[4], "z"), *state = maybe(v[5], "state"), *saved = maybe(v[8], "saved");
+    const Common c(x, "x");
+    craftax_recurrence_args a = recurrence_args(c, x, v);
+    if (!saved || saved->scalar_type() != at::kByte || saved->device() != c.device || !saved->is_contiguous() || !g_lib.recurrence_saved ||
+        (size_t)saved->numel() < g_lib.recurrence_saved(&a))
+        refuse("saved is not what gated_recurrence(..., save=True) returned for these inputs");
+    a.saved = saved->data_ptr();
+    const Tensor dx = like(x), ddecay = like(decay), dintake = like(intake), drate = like(rate), dz = like_or_none(z), dstate = like_or_none(state);
+    a.dy = sequence(&need(v[9], "dy"), "dy", c, c.type);
+    a.dx = place(dx, c);
+    a.ddecay = place(ddecay, c);
+    a.dintake = place(dintake, c);
+    if (dz.defined()) a.dz = place(dz, c);
+    a.dstate_out = dense<const float>(maybe(v[10], "dstate"), "dstate", {c.n, c.channels}, at::kFloat, c);
+    a.dstate_in = static_cast<float*>(address(dstate));
+    a.drate = static_cast<float*>(address(drate));
+    const Tensor work = bytes(g_lib.recurrence_workspace(&a, 1), c);
+    a.workspace = address(work);
+    a.workspace_bytes = work.defined() ? (size_t)work.numel() : 0;
+    call(g_lib.recurrence_backward, a, c);
+    return tuple({dx, ddecay, dintake, drate, dz, dstate});
+}
+
+// x, weight, bias, act
+craftax_projection_args projection_args(const Common& c, const Tensor& x, PyObject* const* v)
+{
+    const Tensor& weight = need(v[1], "weight");
+    if (weight.dim() != 2) refuse("weight must be [outputs][inputs]");
+    check_kind(weight, "weight", c.type, c.device);
+    check_shape(weight, "weight", {weight.size(0), c.channels});
+    craftax_projection_args a = {};
+    a.dtype = type_code(c.type);
+    a.act = (uint32_t)PyLong_AsLong(v[3]);
+    if (PyErr_Occurred()) throw Refusal("");
+    a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.inputs = (int32_t)c.channels; a.outputs = count(weight.size(0), "outputs");
+    a.weight = weight.data_ptr();
+    a.weight_row = weight.stride(0); a.weight_column = weight.stride(1);
+    if (a.weight_row != 1 && a.weight_column != 1 && a.inputs > 1 && a.outputs > 1) refuse("the inputs or the outputs of weight must lie side by side");
+    a.bias = dense<const float>(maybe(v[2], "bias"), "bias", {a.outputs}, at::kFloat, c);
+    a.x = sequence(&x, "x", c, c.type);
+    return a;
+}
+
+// the type of a tensor of outputs, which is the activations' or float32
+at::ScalarType wide_type(const Tensor& t, const char* name, const Common& c)
+{
+    if (t.scalar_type() != c.type && t.scalar_type() != at::kFloat) refuse(name, " must be ", c.type, " or float32, not ", t.scalar_type());
+    return t.scalar_type();
+}
+
+// .., residual, save
+PyObject* projection(PyObject* const* v)
+{
+    const Tensor& x = need(v[0], "x");
+    const Tensor* residual = maybe(v[4], "residual");
+    const Common c(x, "x");
+    craftax_projection_args a = projection_args(c, x, v);
+    const at::ScalarType type = residual ? wide_type(*residual, "residual", c) : c.type;
+    a.out_dtype = type_code(type);
+    a.residual = sequence_of(residual, "residual", c, type, a.outputs);
+    const Tensor out = like_of(x, c, type, a.outputs);
+    Tensor pre;
+    a.out = place(out, c);
+    if (truth(v[5])) {
+        pre = like_of(x, c, c.type, a.outputs);
+        a.pre = place(pre, c);
+    }
+    const Tensor work = bytes(g_lib.projection_workspace ? g_lib.projection_workspace(&a, 0) : 0, c);
+    a.workspace = address(work);
+    a.workspace_bytes = work.defined() ? (size_t)work.numel() : 0;
+    call(g_lib.projection, a, c);
+    return tuple({out, pre});
+}
+
+// .., pre, dout, whether the gradients of x and of weight are wanted, and whether the latter is float32
+PyObject* projection_backward(PyObject* const* v)
+{
+    const Tensor& x = need(v[0], "x");
+    const Tensor *bias = maybe(v[2], "bias"), *pre = maybe(v[4], "pre");
+    const Tensor& dout = need(v[5], "dout");
+    const Common c(x, "x");
+    craftax_projection_args a = projection_args(c, x, v);
+    const at::ScalarType type = wide_type(dout, "dout", c);
+    a.out_dtype = type_code(type);
+    a.dout = sequence_of(&dout, "dout", c, type, a.outputs);
+    a.pre = sequence_of(pre, "pre", c, c.type, a.outputs);
+    Tensor dx, dweight, dbias = like_or_none(bias);
+    if (truth(v[6])) {
+        dx = like(x);
+        a.dx = place(dx, c);
+    }
+    a.dweight_dtype = a.dtype;
+    if (truth(v[7])) {
+        const at::ScalarType kept = truth(v[8]) ? at::kFloat : c.type;
+        dweight = at::empty({a.outputs, c.channels}, c.options(kept));
+        a.dweight = dweight.data_ptr();
+        a.dweight_dtype = type_code(kept);
+    }
+    a.dbias = static_cast<float*>(address(dbias));
+    const Tensor work = bytes(g_lib.projection_workspace ? g_lib.projection_workspace(&a, 1) : 0, c);
+    a.workspace = address(work);
+    a.workspace_bytes = work.defined() ? (size_t)work.numel() : 0;
+    call(g_lib.projection_backward, a, c);
+    return tuple({dx, dweight, dbias});
+}
+
+int64_t whole(PyObject* o, const char* name)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse(name, " must be a whole number below 2^63");
+    }
+    return v;
+}
+
+// x, residual, p, seed, step, step_at, env, type of the output (a code; below 0: as residual or x)
+PyObject* residual_dropout(PyObject* const* v)
+{
+    const Tensor& x = need(v[0], "x");
+    const Tensor *residual = maybe(v[1], "residual"), *step_at = maybe(v[5], "step");
+    const Common c(x, "x");
+    craftax_dropout_args a = {};
+    a.dtype = type_code(c.type);
+    a.steps = (int32_t)c.steps; a.n = (int32_t)c.n; a.channels = (int32_t)c.channels;
+    a.p = PyFloat_AsDouble(v[2]);
+    if (PyErr_Occurred()) throw Refusal("");
+    a.seed = PyLong_AsUnsignedLongLong(v[3]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse("seed must be a whole number of 0..2^64 - 1");
+    }
+    a.step = whole(v[4], "step"); a.env = whole(v[6], "env");
+    if (step_at) {
+        check_kind(*step_at, "step", at::kLong, c.device);
+        if (step_at->numel() != 1) refuse("step must be one number");
+        a.step_at = step_at->data_ptr<int64_t>();
+    }
+    const int64_t code = whole(v[7], "dtype");
+    at::ScalarType type = residual ? wide_type(*residual, "residual", c) : c.type;
+    if (code >= 0) type = code == CRAFTAX_F32 ? at::kFloat : code == CRAFTAX_BF16 ? at::kBFloat16 : at::kHalf;
+    a.out_dtype = type_code(type);
+    a.x = sequence(&x, "x", c, c.type);
+    a.residual = sequence(residual, "residual", c, type);
+    const Tensor out = type == c.type ? like(x) : like_of(x, c, type, c.channels);
+    a.out = place(out, c);
+    call(g_lib.dropout, a, c);
+    return wrap(out);
+}
+
 // ---- module -----------------------------------------------------------------------------------------------
 template <PyObject* (*F)(PyObject* const*), int COUNT>
 PyObject* entry(PyObject*, PyObject* const* v, Py_ssize_t count)
@@ -489,6 +706,11 @@ PyMethodDef g_methods[] = {
     {"selective_scan_backward", CRAFTAX_FAST((&entry<selective_scan_backward, 15>)), METH_FASTCALL, nullptr},
     {"residual_norm", CRAFTAX_FAST((&entry<residual_norm, 8>)), METH_FASTCALL, nullptr},
     {"residual_norm_backward", CRAFTAX_FAST((&entry<residual_norm_backward, 10>)), METH_FASTCALL, nullptr},
+    {"gated_recurrence", CRAFTAX_FAST((&entry<gated_recurrence, 10>)), METH_FASTCALL, nullptr},
+    {"gated_recurrence_backward", CRAFTAX_FAST((&entry<gated_recurrence_backward, 11>)), METH_FASTCALL, nullptr},
+    {"projection", CRAFTAX_FAST((&entry<projection, 6>)), METH_FASTCALL, nullptr},
+    {"projection_backward", CRAFTAX_FAST((&entry<projection_backward, 9>)), METH_FASTCALL, nullptr},
+    {"residual_dropout", CRAFTAX_FAST((&entry<residual_dropout, 8>)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -21,6 +21,14 @@ size_t scan_workspace_bytes(const craftax_scan_args* args, bool backward);
 int norm(const craftax_norm_args* args, void* stream, const char** why);
 int norm_backward(const craftax_norm_args* args, void* stream, const char** why);
 size_t norm_workspace_bytes(const craftax_norm_args* args);
+int recurrence(const craftax_recurrence_args* args, void* stream, const char** why);
+int recurrence_backward(const craftax_recurrence_args* args, void* stream, const char** why);
+size_t recurrence_saved_bytes(const craftax_recurrence_args* args);
+size_t recurrence_workspace_bytes(const craftax_recurrence_args* args, bool backward);
+int projection(const craftax_projection_args* args, void* stream, const char** why);
+int projection_backward(const craftax_projection_args* args, void* stream, const char** why);
+size_t projection_workspace_bytes(const craftax_projection_args* args, bool backward);
+int dropout(const craftax_dropout_args* args, void* stream, const char** why);
 
 }  // namespace host
 }  // namespace mem
