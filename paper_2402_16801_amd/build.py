@@ -6,7 +6,7 @@ import subprocess
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 SRCS = [os.path.join(_PKG, "csrc", f) for f in ("craftax.hip", "full.hip", "memory_conv.hip", "memory_scan.hip", "memory_norm.hip",
-                                              "memory_recurrence.hip", "memory_product.hip", "memory_dropout.hip")]
+                                              "memory_recurrence.hip", "memory_product.hip", "memory_product_direct.hip", "memory_dropout.hip")]
 OUT = os.path.join(_PKG, "libcraftax_hip.so")
 
 HIPCC_FLAGS = [

@@ -12,42 +12,13 @@
 
 namespace mem {
 
-constexpr int TILE_BYTES = 128;        // along k, of a tile that lies with k inside
-template <typename E> constexpr int tile_k() { return TILE_BYTES / (int)sizeof(E); }
-
-// A matrix operand: rows of k (INSIDE) or rows of the other index, one behind the other along k.
-template <typename E> struct Operand {
-    const E* data;
-    Rows rows;
-};
-
-template <typename E, typename R> struct ProductParams {
-    Operand<E> p, q;
-    int64_t k;               // length of the sums
-    uint32_t m;              // rows of the result
-    int n;                   // columns of it
-    uint32_t m_tiles, n_tiles;
-    int64_t k_part;          // of a part of the sums, a multiple of the tile
-    float* part;             // [parts][m][n], or nullptr: one part, finished here
-    unsigned wide;
-    Finish<E, R> finish;
-};
-
-// The place of a 16-byte chunk in a tile: exchanged within the row by a number of the row, so that the chunks that are read at once lie in
-// different banks.
-template <int FP, bool IS_P> __device__ __forceinline__ int inside_key(int row) { return IS_P ? (row & 3) | ((row / (4 * FP)) & 1) << 2 : row & 7; }
-template <typename E, int TILE> __device__ __forceinline__ int across_key(int k)
-{
-    return (sizeof(E) == 2 ? ((k & 3) << 1) | ((k >> 3) & 1) << 3 : ((k >> 2) & 3) << 2) & (TILE * (int)sizeof(E) / 16 - 1);
-}
-
 // One operand's tile of TILE rows on its way from memory to LDS.
 template <typename E, int TILE, int THREADS, bool INSIDE, int FP, bool IS_P> struct Stage {
     static constexpr int V = 16 / sizeof(E), CHUNKS = TILE * 8 / THREADS, ROW_CHUNKS = INSIDE ? 8 : TILE / V;
-    const E* from[INSIDE ? CHUNKS : 1];
+    const E* from[INSIDE ? CHUNKS : 1];      // rows
     U4v raw[CHUNKS];
-    int side;                // chunks inside a row: values before this thread's
-    int left;                // across: values of a row from its chunk on
+    int side;                // values of a row before this thread's chunk
+    int columns;             // across: of a row, from the tile's first on
     Operand<E> op;
     __device__ __forceinline__ static int row_of(int c) { return ((int)threadIdx.x + c * THREADS) / ROW_CHUNKS; }
     __device__ __forceinline__ static int chunk_of(int c) { return ((int)threadIdx.x + c * THREADS) % ROW_CHUNKS; }
@@ -55,7 +26,7 @@ template <typename E, int TILE, int THREADS, bool INSIDE, int FP, bool IS_P> str
     {
         static_assert(THREADS % ROW_CHUNKS == 0, "a thread's chunks lie below one another");
         side = chunk_of(0) * V;
-        left = (int)(rows - first) - side;
+        columns = (int)(rows - first);
         if (INSIDE) {
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
@@ -69,14 +40,19 @@ template <typename E, int TILE, int THREADS, bool INSIDE, int FP, bool IS_P> str
     // values k .. k + tile of the sums; those at or behind `end` are 0
     __device__ __forceinline__ void load(int64_t k, int64_t end)
     {
+        const bool whole = INSIDE ? k + tile_k<E>() <= end : columns >= TILE && k + tile_k<E>() <= end;
+        auto row = [&](int c) {
+            const int64_t r = k + row_of(c);
+            return from[0] + op.rows.at((uint32_t)(r < end ? r : end - 1));
+        };
+        if (whole) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            if (INSIDE) {
-                const int64_t rest = end - (k + side);
-                raw[c] = load_some<E>(from[c] + k + side, rest > V ? V : (int)rest);
-            } else {
-                const int64_t row = k + row_of(c);
-                raw[c] = load_some<E>(from[0] + op.rows.at((uint32_t)(row < end ? row : end - 1)) + side, row < end ? left : 0);
+            for (int c = 0; c < CHUNKS; ++c) raw[c] = load_chunk<false>(INSIDE ? from[c] + k + side : row(c) + side);
+        } else {
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                if (INSIDE) raw[c] = load_some<E>(from[c], k + side, end);
+                else raw[c] = load_some<E>(row(c), side, k + row_of(c) < end ? columns : 0);
             }
         }
     }
@@ -97,18 +73,7 @@ template <typename E, int TILE, int THREADS, bool INSIDE, int FP, bool IS_P> str
             const int r = row + (IS_P ? i / 4 * (4 * FP) + i % 4 : i);
             return *reinterpret_cast<const U4v*>(lds + (r * 8 + ((half * 4 + g) ^ inside_key<FP, IS_P>(r))) * 16);
         } else if constexpr (sizeof(E) == 2) {
-            // a group of 16 lanes reads four rows of 16 values and gets them column by column
-            U4v out;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = half * 32 + g * 8 + h * 4 + i / 4, col = row + i % 4 * 4;
-                const char* at = lds + (k * ROW_CHUNKS + ((col / 8) ^ across_key<E, TILE>(k))) * 16 + col % 8 * 2;
-                const S4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4*)(at));
-                const uint64_t bits = __builtin_bit_cast(uint64_t, v);
-                out[2 * h] = (uint32_t)bits;
-                out[2 * h + 1] = (uint32_t)(bits >> 32);
-            }
-            return out;
+            return across_frag<E, TILE>(lds, row, half);
         } else {
             U4v out;
 #pragma unroll
@@ -121,24 +86,6 @@ template <typename E, int TILE, int THREADS, bool INSIDE, int FP, bool IS_P> str
     }
 };
 
-// Which tile a block computes.  Consecutive blocks go to the eight dies in turn: the tiles of a row of tiles, which read the same rows of Q,
-// follow one another on one die.
-struct TilePlace {
-    uint32_t m, n, part;
-    bool on;
-    template <typename P> __device__ __forceinline__ explicit TilePlace(const P& p)
-    {
-        constexpr uint32_t DIES = 8;
-        const uint64_t block = (uint64_t)spread_block(p.wide);
-        const uint32_t per_part = (p.m_tiles + DIES - 1) / DIES * DIES * p.n_tiles;
-        part = (uint32_t)(block / per_part);
-        const uint32_t at = (uint32_t)(block % per_part), turn = at / DIES;
-        n = turn % p.n_tiles;
-        m = turn / p.n_tiles * DIES + at % DIES;
-        on = m < p.m_tiles && (int64_t)part * p.k_part < p.k;
-    }
-};
-
 // A block of WP x WQ wavefronts computes 16 FP WP columns by 16 FQ WQ rows.
 template <typename E, typename R, bool INSIDE, int FP, int FQ, int WP, int WQ>
 __global__ __launch_bounds__(64 * WP * WQ) void k_product(const ProductParams<E, R> p)
@@ -147,7 +94,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(const ProductParams<E,
     using StageP = Stage<E, TP, THREADS, INSIDE, FP, true>;
     using StageQ = Stage<E, TQ, THREADS, INSIDE, FP, false>;
     __shared__ __attribute__((aligned(16))) char lds[2][(TP + TQ) * TILE_BYTES];
-    const TilePlace at(p);
+    const TilePlace at(p, (uint32_t)spread_block(p.wide));
     if (!at.on) return;
     const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE, wp = wave % WP * 16 * FP, wq = wave / WP * 16 * FQ;
     const uint32_t m0 = at.m * TQ;
@@ -220,8 +167,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(const ProductParams<E,
 }
 
 // Few rows: a block is one fragment of 16 by 16, its wavefronts share the sums, and operands go from memory to registers.
-constexpr int ROW_WAVES = 8;
-template <typename E, typename R>
+template <typename E, typename R, bool ODD, int ROW_WAVES>
 __global__ __launch_bounds__(64 * ROW_WAVES) void k_product_rows(const ProductParams<E, R> p)
 {
     constexpr int V = 16 / sizeof(E), STEP = 4 * V, AHEAD = 4;
@@ -230,25 +176,23 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void k_product_rows(const ProductPa
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), i = lane & 15, g = lane >> 4;
     const uint32_t m = mt * 16 + i;
     const int n = (int)nt * 16 + i;
-    const E* q = p.q.data + p.q.rows.at(m < p.m ? m : p.m - 1) + g * V;
-    const E* w = p.p.data + p.p.rows.at((uint32_t)(n < p.n ? n : p.n - 1)) + g * V;
+    const E* q = p.q.data + p.q.rows.at(m < p.m ? m : p.m - 1);
+    const E* w = p.p.data + p.p.rows.at((uint32_t)(n < p.n ? n : p.n - 1));
     F4 acc = {};
-    int64_t k = (int64_t)wave * STEP;
-    for (; k + ((AHEAD - 1) * ROW_WAVES + 1) * STEP <= p.k; k += AHEAD * ROW_WAVES * STEP) {
-        U4v a[AHEAD], b[AHEAD];
+    const int64_t full = p.k / STEP;            // steps without an end of the sums in them
+    for (int64_t s = wave; s < full; s += AHEAD * ROW_WAVES) {
+        U4v a[AHEAD] = {}, b[AHEAD] = {};
 #pragma unroll
-        for (int s = 0; s < AHEAD; ++s) {
-            a[s] = load_some<E>(w + k + s * ROW_WAVES * STEP, V);
-            b[s] = load_some<E>(q + k + s * ROW_WAVES * STEP, V);
-        }
+        for (int j = 0; j < AHEAD; ++j)
+            if (s + j * ROW_WAVES < full) {
+                a[j] = load_chunk<ODD>(w + (s + j * ROW_WAVES) * STEP + g * V);
+                b[j] = load_chunk<ODD>(q + (s + j * ROW_WAVES) * STEP + g * V);
+            }
 #pragma unroll
-        for (int s = 0; s < AHEAD; ++s) acc = Frag<E>::times(a[s], b[s], acc);
+        for (int j = 0; j < AHEAD; ++j) acc = Frag<E>::times(a[j], b[j], acc);
     }
-    for (; k < p.k; k += ROW_WAVES * STEP) {
-        const int64_t rest = p.k - (k + g * V);
-        const int count = rest > V ? V : (int)rest;
-        acc = Frag<E>::times(load_some<E>(w + k, count), load_some<E>(q + k, count), acc);
-    }
+    if (full * STEP < p.k && wave == ROW_WAVES - 1)
+        acc = Frag<E>::times(load_some<E>(w, full * STEP + g * V, p.k), load_some<E>(q, full * STEP + g * V, p.k), acc);
     sums[wave][lane] = acc;
     __syncthreads();
     if (wave != 0) return;
@@ -273,25 +217,45 @@ __global__ __launch_bounds__(256) void k_product_sum(const float* part, int part
     finish(row, c, v);
 }
 
-// out[c][r] = in[r][c]
+// out[c][r] = in[r][c], in tiles of 32 by 32; rows of out are filled with 0 up to `out_row`, less than a tile
 template <typename E>
 __global__ __launch_bounds__(256) void k_turn(const E* in, int64_t in_row, E* out, int64_t out_row, int rows, int columns, unsigned x_tiles, unsigned wide)
 {
-    __shared__ E tile[64][64 + 4 / sizeof(E)];
+    __shared__ E tile[32][32 + 4 / sizeof(E)];
     const uint32_t block = (uint32_t)spread_block(wide);
-    const int x = threadIdx.x % 64, y = threadIdx.x / 64;
-    const int64_t r0 = (int64_t)(block / x_tiles) * 64, c0 = (int64_t)(block % x_tiles) * 64;
+    const int x = threadIdx.x % 32, y = threadIdx.x / 32;
+    const int64_t r0 = (int64_t)(block / x_tiles) * 32, c0 = (int64_t)(block % x_tiles) * 32;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int64_t r = r0 + y + 4 * k, c = c0 + x;
-        if (r < rows && c < columns) tile[y + 4 * k][x] = in[r * in_row + c];
+    for (int k = 0; k < 32; k += 8) {
+        const int64_t r = r0 + y + k, c = c0 + x;
+        tile[y + k][x] = r < rows && c < columns ? in[r * in_row + c] : (E)0.0f;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int64_t c = c0 + y + 4 * k, r = r0 + x;
-        if (r < rows && c < columns) out[c * out_row + r] = tile[x][y + 4 * k];
+    for (int k = 0; k < 32; k += 8) {
+        const int64_t c = c0 + y + k, r = r0 + x;
+        if (r < out_row && c < columns) out[c * out_row + r] = tile[x][y + k];
     }
+}
+
+// Rows of `columns` values one behind the other, each filled with 0 up to a multiple of eight: what tiles that go straight to LDS ask for.
+template <typename E>
+__global__ __launch_bounds__(256) void k_fill_up(const Operand<E> in, E* out, uint32_t rows, int columns, uint32_t chunks, unsigned wide)
+{
+    constexpr int V = 8;
+    const int64_t at = spread_block(wide) * 256 + threadIdx.x;
+    if (at >= (int64_t)rows * chunks) return;
+    const uint32_t row = (uint32_t)((uint64_t)at / chunks);
+    const int c = (int)((uint64_t)at % chunks) * V;
+    const E* from = in.data + in.rows.at(row);
+    Pack<E, V> q;
+    if (c + V <= columns) {
+        q = *reinterpret_cast<const Pack<E, V>*>(from + c);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) q.v[j] = c + j < columns ? from[c + j] : (E)0.0f;
+    }
+    *reinterpret_cast<Pack<E, V>*>(out + at * V) = q;
 }
 
 // dp = dout act'(pre), rounded to the activations' type (not stored where it is dout itself), and its sums over rows: a thread owns
@@ -305,38 +269,56 @@ template <typename E, typename R> struct SlopeParams {
     int64_t dp_row;
     float* part;
     uint32_t m;
-    int n, act;
+    int n;
 };
-template <typename P> __device__ __forceinline__ void load_row(const P* p, int count, float (&v)[SLOPE_V])
-{
-    if (count >= SLOPE_V) {
-        const Pack<P, SLOPE_V> q = *reinterpret_cast<const Pack<P, SLOPE_V>*>(p);
-#pragma unroll
-        for (int j = 0; j < SLOPE_V; ++j) v[j] = Elem<P>::up(q.v[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < SLOPE_V; ++j) v[j] = j < count ? Elem<P>::up(p[j]) : 0.0f;
-    }
-}
-template <typename E, typename R>
+// EDGE: VECTORS where eight divide the columns, else VALUES.
+template <typename E, typename R, int ACT, Edge EDGE>
 __global__ __launch_bounds__(256) void k_slope(const SlopeParams<E, R> p)
 {
+    constexpr int GO = 1;              // rows under way together (two or four were no faster)
     __shared__ float sums[SLOPE_V][256];
     const int x = threadIdx.x % 64, y = threadIdx.x / 64, c = ((int)blockIdx.x * 64 + x) * SLOPE_V, count = p.n - c;
     float total[SLOPE_V] = {};
     if (count > 0) {
-        for (uint32_t m = blockIdx.y * 4 + y; m < p.m; m += gridDim.y * 4) {
-            float d[SLOPE_V];
-            load_row(p.dout + p.dout_rows.at(m) + c, count, d);
-            if (p.pre) {
-                float v[SLOPE_V];
-                load_row(p.pre + p.pre_rows.at(m) + c, count, v);
+        const uint32_t step = gridDim.y * 4, last = p.m - 1;
+        struct Raw { Pack<R, SLOPE_V> d; Pack<E, SLOPE_V> v; } raw[GO];
+        auto take = [&](auto* from, auto& to) {
+            if (EDGE == VECTORS || count >= SLOPE_V) {
+                to = *reinterpret_cast<const std::remove_reference_t<decltype(to)>*>(from);
+            } else {
 #pragma unroll
-                for (int j = 0; j < SLOPE_V; ++j) d[j] *= slope_of(v[j], p.act);
+                for (int j = 0; j < SLOPE_V; ++j) to.v[j] = from[j < count ? j : 0];
             }
-            if (p.dp) Finish<E, R>::template store<E, SLOPE_V>(p.dp + (int64_t)m * p.dp_row + c, count, d);
+        };
+        auto load = [&](uint32_t row, Raw& q) {
+            const uint32_t m = row < last ? row : last;
+            take(p.dout + p.dout_rows.at(m) + c, q.d);
+            if (ACT != CRAFTAX_ACT_NONE) take(p.pre + p.pre_rows.at(m) + c, q.v);
+        };
+        uint32_t m = blockIdx.y * 4 + y;
 #pragma unroll
-            for (int j = 0; j < SLOPE_V; ++j) total[j] += d[j];
+        for (int g = 0; g < GO; ++g) load(m + g * step, raw[g]);
+        for (; m < p.m; m += GO * step) {
+            float d[GO][SLOPE_V];
+#pragma unroll
+            for (int g = 0; g < GO; ++g)
+#pragma unroll
+                for (int j = 0; j < SLOPE_V; ++j) {
+                    d[g][j] = Elem<R>::up(raw[g].d.v[j]);
+                    if (ACT != CRAFTAX_ACT_NONE) d[g][j] *= slope_of<ACT>(Elem<E>::up(raw[g].v.v[j]));
+                    if (EDGE == VALUES && j >= count) d[g][j] = 0.0f;         // rows of dp are filled up to a multiple of eight
+                }
+            // the next rows are under way in front of the stores: behind them the wait for the rows would be for those too
+#pragma unroll
+            for (int g = 0; g < GO; ++g) load(m + (GO + g) * step, raw[g]);
+#pragma unroll
+            for (int g = 0; g < GO; ++g) {
+                const uint32_t row = m + g * step;
+                if (row >= p.m) continue;
+#pragma unroll
+                for (int j = 0; j < SLOPE_V; ++j) total[j] += d[g][j];
+                if (p.dp) Finish<E, R>::template store<E, SLOPE_V>(p.dp + (int64_t)row * p.dp_row + c, SLOPE_V, d[g]);
+            }
         }
     }
     if (!p.part) return;
@@ -357,8 +339,9 @@ struct PutBias {
 namespace host {
 
 // ---- how a product is cut ------------------------------------------------------------------------------
-// ROWS: by fragments, straight from memory.  SMALL, LARGE: tiles of 64 x 64, 128 x 128.
-enum class Cut { ROWS, SMALL, LARGE };
+// ROWS: by fragments, straight from memory.  SMALL, LARGE: tiles of 64 x 64, 128 x 128 through registers.  DIRECT, DIRECT_LARGE: tiles of
+// 128 x 128, 256 x 256 that go straight to LDS.
+enum class Cut { ROWS, SMALL, LARGE, DIRECT, DIRECT_LARGE };
 struct Plan {
     Cut cut;
     uint32_t m_tiles, n_tiles;
@@ -369,25 +352,34 @@ struct Plan {
 constexpr int64_t CHIP_UNITS = 256;
 constexpr int64_t MOST_VALUES = (int64_t)1 << 42;       // of a matrix: its tiles are counted in 32 bits
 
-static Plan plan(int64_t m, int64_t n, int64_t k, size_t elem, bool inside)
+static int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return ceil_div(m, side) * ceil_div(n, side); }
+// Enough rows and columns for tiles that go straight to LDS: one for every compute unit.  (3,000 rows of 1,344 values onto 700 are 144 of them, 30 us;
+// in tiles of 64 x 64 through registers 22.  4,096 of 512 onto 1,024 are 256: 11.7 us and 14.5.)
+static bool tiled(int64_t m, int64_t n) { return tiles_of(m, n, 128) >= CHIP_UNITS; }
+
+static Plan plan(int64_t m, int64_t n, int64_t k, size_t elem, bool inside, bool direct)
 {
     Plan c{};
-    const int64_t step = TILE_BYTES / (int64_t)elem, small = ceil_div(m, 64) * ceil_div(n, 64), large = ceil_div(m, 128) * ceil_div(n, 128);
+    const int64_t step = TILE_BYTES / (int64_t)elem;
+    auto tiles = [&](int64_t side) { return tiles_of(m, n, side); };
     c.parts = 1;
     c.k_part = ceil_div(k, step) * step;
-    if (inside && ceil_div(m, 16) * ceil_div(n, 16) <= 4 * CHIP_UNITS) {
+    if (inside && tiles(16) <= 4 * CHIP_UNITS) {
         c.cut = Cut::ROWS;
         c.m_tiles = (uint32_t)ceil_div(m, 16);
         c.n_tiles = (uint32_t)ceil_div(n, 16);
         return c;
     }
-    c.cut = large >= CHIP_UNITS || (!inside && m >= 128 && n >= 128) ? Cut::LARGE : Cut::SMALL;
-    const int64_t side = c.cut == Cut::LARGE ? 128 : 64, tiles = c.cut == Cut::LARGE ? large : small;
+    // A compute unit takes 0.4 times as long for a tile of 128 x 128 as for one of 256 x 256 (1,200 and 740 TFLOP/s for 8,192 squared, bfloat16).
+    const bool larger = 10 * ceil_div(tiles(256), CHIP_UNITS) <= 4 * ceil_div(tiles(128), CHIP_UNITS) || (!inside && m > 128 && n > 128);
+    if (direct) c.cut = larger ? Cut::DIRECT_LARGE : Cut::DIRECT;
+    else c.cut = tiles(128) >= CHIP_UNITS || (!inside && m >= 128 && n >= 128) ? Cut::LARGE : Cut::SMALL;
+    const int64_t side = c.cut == Cut::DIRECT_LARGE ? 256 : c.cut == Cut::SMALL ? 64 : 128;
     c.m_tiles = (uint32_t)ceil_div(m, side);
     c.n_tiles = (uint32_t)ceil_div(n, side);
-    // long sums of few tiles are cut, into parts of eight tiles along k at least
-    int64_t parts = tiles < 2 * CHIP_UNITS ? 2 * CHIP_UNITS / tiles : 1;
-    const int64_t most = k / (8 * step);
+    // long sums of few tiles are cut, into parts of eight tiles along k at least, until every compute unit has what it holds at once
+    const int64_t have = tiles(side), room = c.cut == Cut::DIRECT_LARGE ? CHIP_UNITS : 2 * CHIP_UNITS, most = k / (8 * step);
+    int64_t parts = have < room ? room / have : 1;
     if (parts > most) parts = most;
     if (parts > 1) {
         c.k_part = ceil_div(ceil_div(k, parts), step) * step;
@@ -402,15 +394,36 @@ static void launch_product(const Plan& c, ProductParams<E, R> p, float* part, hi
 {
     p.m_tiles = c.m_tiles; p.n_tiles = c.n_tiles; p.k_part = c.k_part;
     p.part = c.parts > 1 ? part : nullptr;
-    if (c.cut == Cut::ROWS) {
-        hipLaunchKernelGGL((k_product_rows<E, R>), dim3(c.m_tiles * c.n_tiles), dim3(64 * ROW_WAVES), 0, st, p);
-        return;
+    if constexpr (INSIDE) {
+        if (c.cut == Cut::ROWS) {
+            // rows that begin at odd places
+            auto odd = [](const Operand<E>& o) { return !aligned(o.data, 4) || o.rows.step % 2 || o.rows.env % 2; };
+            const uint32_t tiles = c.m_tiles * c.n_tiles;
+            auto rows = [&](auto is_odd, auto waves) {
+                hipLaunchKernelGGL((k_product_rows<E, R, decltype(is_odd)::value, decltype(waves)::value>), dim3(tiles), dim3(64 * decltype(waves)::value), 0, st, p);
+            };
+            auto waves = [&](auto is_odd) {
+                if (tiles <= CHIP_UNITS && p.k * (int64_t)sizeof(E) >= 1024) rows(is_odd, std::integral_constant<int, 16>{});
+                else rows(is_odd, std::integral_constant<int, 8>{});
+            };
+            if constexpr (sizeof(E) == 2) {
+                if (odd(p.p) || odd(p.q)) return waves(std::true_type{});
+            }
+            return waves(std::false_type{});
+        }
     }
-    const Spread grid = spread(ceil_div(c.m_tiles, 8) * 8 * (int64_t)c.n_tiles * c.parts, 256);
+    const int64_t tiles = ceil_div((int64_t)c.m_tiles * c.n_tiles * c.parts, DIES) * DIES;
+    const Spread grid = spread(tiles, 256);
+    p.tiles = (uint32_t)tiles;
     p.wide = grid.x;
     const dim3 blocks(grid.x, 1, grid.z);
-    if (c.cut == Cut::LARGE) hipLaunchKernelGGL((k_product<E, R, INSIDE, 4, 4, 2, 2>), blocks, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((k_product<E, R, INSIDE, 2, 2, 2, 2>), blocks, dim3(256), 0, st, p);
+    if (c.cut == Cut::DIRECT || c.cut == Cut::DIRECT_LARGE) {
+        if constexpr (sizeof(E) == 2) launch_direct<INSIDE>(p, tiles, c.cut == Cut::DIRECT_LARGE, st);
+    } else if (c.cut == Cut::LARGE) {
+        hipLaunchKernelGGL((k_product<E, R, INSIDE, 4, 4, 2, 2>), blocks, dim3(256), 0, st, p);
+    } else {
+        hipLaunchKernelGGL((k_product<E, R, INSIDE, 2, 2, 2, 2>), blocks, dim3(256), 0, st, p);
+    }
     if (c.parts > 1) {
         const uint32_t vectors = (uint32_t)ceil_div(p.n, 4);
         const Spread sum = spread(ceil_div((int64_t)p.m * vectors, 256), 256);
@@ -427,6 +440,19 @@ static Rows rows_of(const craftax_projection_args* a, const craftax_view& v)
     return {v.step, v.env, (uint32_t)a->n};
 }
 static Rows dense_rows(int64_t stride) { return {stride, 0, 1}; }
+
+// Batch first: environments count as steps, so that rows lie one behind the other.
+static craftax_projection_args ordered(const craftax_projection_args* given)
+{
+    craftax_projection_args a = *given;
+    if (a.x.step < a.x.env) {
+        const int32_t steps = a.steps;
+        a.steps = a.n;
+        a.n = steps;
+        for (craftax_view* v : {&a.x, &a.residual, &a.out, &a.pre, &a.dout, &a.dx}) *v = {v->data, v->env, v->step};
+    }
+    return a;
+}
 
 // the weight's rows lie with the inputs side by side
 static bool by_rows(const craftax_projection_args* a) { return a->weight_column == 1 || a->inputs == 1; }
@@ -464,12 +490,17 @@ static int projection_check(const craftax_projection_args* a, bool backward, con
 struct Project {
     int64_t rows;
     Plan forward, dx, dweight;
-    bool turn;               // the weight is turned first
-    int64_t turned_row, dp_row;
+    bool turn, fill_weight;  // the weight is turned, or its rows are filled up, first
+    bool fill_x;             // the rows of x are
+    int64_t weight_row, x_row, dp_row;   // of what lies in the workspace
     bool has_dp;
     unsigned slope_x, slope_y;
-    size_t turned_at, dp_at, sums_at, part_at, total;
+    size_t weight_at, x_at, dp_at, sums_at, part_at, total;
 };
+// Where rows cannot go straight to LDS they are copied to where they can, if a product is worth it: reading and writing them takes as long as
+// this many columns of the result gain by it (262,144 rows of 1,345 values onto 512 in bfloat16: 700 us, through registers 858; 4,096 rows 34 and 24).
+constexpr int64_t WORTH_COLUMNS = 256, WORTH_ROWS = 16384;
+
 static Project project(const craftax_projection_args* a, bool backward)
 {
     Project c{};
@@ -477,18 +508,35 @@ static Project project(const craftax_projection_args* a, bool backward)
     c.rows = (int64_t)a->steps * a->n;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
+    auto filled = [](int64_t count) { return ceil_div(count, 8) * 8; };
+    // whether rows can go straight to LDS, 16 bytes at a time: those of a tile lie within 2^32 bytes, one stride apart
+    auto near = [&](int64_t row) { return e == 2 && row >= 0 && row < ((int64_t)1 << 23) - 512; };
+    auto fits = [&](const void* data, int64_t row, int64_t count) { return near(row) && count % 8 == 0 && aligned(data, 16) && row % 8 == 0; };
+    auto whole = [&](const craftax_view& v, int64_t count) { return flat(a, v) && fits(v.data, rows_of(a, v).step, count); };
+    c.x_row = filled(a->inputs);
+    c.dp_row = filled(a->outputs);
     if (!backward) {
+        c.weight_row = c.x_row;
         c.turn = !by_rows(a);
-        c.turned_row = ceil_div(a->inputs, 8) * 8;
-        if (c.turn) c.turned_at = take((size_t)a->outputs * c.turned_row * e);
-        c.forward = plan(c.rows, a->outputs, a->inputs, e, true);
+        bool direct = near(c.x_row) && tiled(c.rows, a->outputs);
+        if (direct && !whole(a->x, a->inputs)) direct = c.fill_x = a->outputs >= WORTH_COLUMNS && c.rows >= WORTH_ROWS;
+        if (direct && !c.turn) c.fill_weight = !fits(a->weight, a->weight_row, a->inputs);
+        if (c.turn || c.fill_weight) c.weight_at = take((size_t)a->outputs * c.weight_row * e);
+        if (c.fill_x) c.x_at = take((size_t)c.rows * c.x_row * e);
+        c.forward = plan(c.rows, a->outputs, a->inputs, e, true, direct);
         c.part_at = take(c.forward.part_bytes);
     } else {
+        c.weight_row = c.dp_row;
         c.turn = a->dx.data && by_rows(a) && a->weight_row != 1;
-        c.turned_row = ceil_div(a->outputs, 8) * 8;
-        if (c.turn) c.turned_at = take((size_t)a->inputs * c.turned_row * e);
         c.has_dp = (a->act != CRAFTAX_ACT_NONE || a->out_dtype != a->dtype) && (a->dx.data || a->dweight);
-        c.dp_row = ceil_div(a->outputs, 8) * 8;
+        const bool wide = near(c.dp_row) && near(c.x_row) && c.rows < (int64_t)1 << 30, worth = wide && c.rows >= WORTH_ROWS;
+        if (!c.has_dp && worth && !whole(a->dout, a->outputs)) c.has_dp = (a->dx.data || a->dweight) && a->inputs >= WORTH_COLUMNS;
+        const bool dp_fits = wide && (c.has_dp || whole(a->dout, a->outputs));
+        bool direct_dx = a->dx.data && dp_fits && tiled(c.rows, a->inputs), direct_dw = a->dweight && dp_fits;
+        if (direct_dx && !c.turn) c.fill_weight = !fits(a->weight, a->weight_column, a->outputs);
+        if (direct_dw && !whole(a->x, a->inputs)) direct_dw = c.fill_x = worth && a->outputs >= WORTH_COLUMNS;
+        if (c.turn || c.fill_weight) c.weight_at = take((size_t)a->inputs * c.weight_row * e);
+        if (c.fill_x) c.x_at = take((size_t)c.rows * c.x_row * e);
         if (c.has_dp) c.dp_at = take((size_t)c.rows * c.dp_row * e);
         c.slope_x = (unsigned)ceil_div(a->outputs, 64 * SLOPE_V);
         int64_t y = ceil_div(c.rows, 4), most = ceil_div(2048, c.slope_x);
@@ -496,11 +544,11 @@ static Project project(const craftax_projection_args* a, bool backward)
         if (a->dbias) c.sums_at = take((size_t)c.slope_y * a->outputs * sizeof(float));
         size_t part = 0;
         if (a->dx.data) {
-            c.dx = plan(c.rows, a->inputs, a->outputs, e, true);
+            c.dx = plan(c.rows, a->inputs, a->outputs, e, true, direct_dx);
             part = c.dx.part_bytes;
         }
         if (a->dweight) {
-            c.dweight = plan(a->outputs, a->inputs, c.rows, e, false);
+            c.dweight = plan(a->outputs, a->inputs, c.rows, e, false, direct_dw);
             if (c.dweight.part_bytes > part) part = c.dweight.part_bytes;
         }
         c.part_at = take(part);
@@ -514,7 +562,8 @@ size_t projection_workspace_bytes(const craftax_projection_args* a, bool backwar
     if (!a || a->dtype > CRAFTAX_F16 || a->steps < 1 || a->n < 1 || a->inputs < 1 || a->outputs < 1 || a->inputs > MOST_COUNT || a->outputs > MOST_COUNT ||
         (int64_t)a->steps * a->n >= (int64_t)1 << 31)
         return 0;
-    return project(a, backward).total;
+    const craftax_projection_args ours = ordered(a);
+    return project(&ours, backward).total;
 }
 
 static int projection_room(const craftax_projection_args* a, size_t need, const char** why)
@@ -527,9 +576,25 @@ static int projection_room(const craftax_projection_args* a, size_t need, const 
 
 template <typename E> static void turn(const E* in, int64_t in_row, E* out, int64_t out_row, int rows, int columns, hipStream_t st)
 {
-    const unsigned x = (unsigned)ceil_div(columns, 64);
-    const Spread grid = spread(ceil_div(rows, 64) * x, 256);
+    const unsigned x = (unsigned)ceil_div(columns, 32);
+    const Spread grid = spread(ceil_div(rows, 32) * x, 256);
     hipLaunchKernelGGL((k_turn<E>), dim3(grid.x, 1, grid.z), dim3(256), 0, st, in, in_row, out, out_row, rows, columns, x, grid.x);
+}
+
+template <typename E> static void fill_up(const Operand<E>& in, E* out, int64_t rows, int columns, hipStream_t st)
+{
+    const int64_t chunks = ceil_div(columns, 8);
+    const Spread grid = spread(ceil_div(rows * chunks, 256), 256);
+    hipLaunchKernelGGL((k_fill_up<E>), dim3(grid.x, 1, grid.z), dim3(256), 0, st, in, out, (uint32_t)rows, columns, (uint32_t)chunks, grid.x);
+}
+// x as the products read it
+template <typename E> static Operand<E> x_of(const craftax_projection_args* a, const Project& c, char* work, hipStream_t st)
+{
+    const Operand<E> given{static_cast<const E*>(a->x.data), rows_of(a, a->x)};
+    if (!c.fill_x) return given;
+    E* ours = reinterpret_cast<E*>(work + c.x_at);
+    fill_up<E>(given, ours, c.rows, a->inputs, st);
+    return {ours, dense_rows(c.x_row)};
 }
 
 // calls f with values of the activations' and the outputs' type
@@ -541,9 +606,10 @@ template <typename F> static void with_types(uint32_t dtype, uint32_t out, F&& f
     });
 }
 
-int projection(const craftax_projection_args* a, void* stream, const char** why)
+int projection(const craftax_projection_args* given, void* stream, const char** why)
 {
-    if (int rc = projection_check(a, false, why)) return rc;
+    if (int rc = projection_check(given, false, why)) return rc;
+    const craftax_projection_args ours = ordered(given), *a = &ours;
     const Project c = project(a, false);
     if (int rc = projection_room(a, c.total, why)) return rc;
     const hipStream_t st = (hipStream_t)stream;
@@ -554,14 +620,15 @@ int projection(const craftax_projection_args* a, void* stream, const char** why)
         ProductParams<E, R> p{};
         const E* weight = static_cast<const E*>(a->weight);
         int64_t ld = a->weight_row;
-        if (c.turn) {
-            E* turned = reinterpret_cast<E*>(work + c.turned_at);
-            turn<E>(weight, a->weight_column, turned, c.turned_row, a->inputs, a->outputs, st);
-            weight = turned;
-            ld = c.turned_row;
+        if (c.turn || c.fill_weight) {
+            E* ours = reinterpret_cast<E*>(work + c.weight_at);
+            if (c.turn) turn<E>(weight, a->weight_column, ours, c.weight_row, a->inputs, a->outputs, st);
+            else fill_up<E>({weight, dense_rows(ld)}, ours, a->outputs, a->inputs, st);
+            weight = ours;
+            ld = c.weight_row;
         }
         p.p = {weight, dense_rows(ld)};
-        p.q = {static_cast<const E*>(a->x.data), rows_of(a, a->x)};
+        p.q = x_of<E>(a, c, work, st);
         p.k = a->inputs; p.m = (uint32_t)c.rows; p.n = a->outputs;
         p.finish = {a->bias, static_cast<const R*>(a->residual.data), static_cast<R*>(a->out.data), static_cast<E*>(a->pre.data),
                     rows_of(a, a->residual), rows_of(a, a->out), rows_of(a, a->pre), (int)a->act, a->outputs};
@@ -570,9 +637,10 @@ int projection(const craftax_projection_args* a, void* stream, const char** why)
     return launched(why);
 }
 
-int projection_backward(const craftax_projection_args* a, void* stream, const char** why)
+int projection_backward(const craftax_projection_args* given, void* stream, const char** why)
 {
-    if (int rc = projection_check(a, true, why)) return rc;
+    if (int rc = projection_check(given, true, why)) return rc;
+    const craftax_projection_args ours = ordered(given), *a = &ours;
     const Project c = project(a, true);
     if (int rc = projection_room(a, c.total, why)) return rc;
     const hipStream_t st = (hipStream_t)stream;
@@ -585,10 +653,18 @@ int projection_backward(const craftax_projection_args* a, void* stream, const ch
             SlopeParams<E, R> s{};
             s.dout = static_cast<const R*>(a->dout.data); s.dout_rows = rows_of(a, a->dout);
             s.pre = a->act == CRAFTAX_ACT_NONE ? nullptr : static_cast<const E*>(a->pre.data); s.pre_rows = rows_of(a, a->pre);
-            s.dp = own; s.dp_row = c.dp_row; s.act = (int)a->act;
+            s.dp = own; s.dp_row = c.dp_row;
             s.part = a->dbias ? reinterpret_cast<float*>(work + c.sums_at) : nullptr;
             s.m = (uint32_t)c.rows; s.n = a->outputs;
-            hipLaunchKernelGGL((k_slope<E, R>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
+            auto slope = [&](auto act) {
+                constexpr int ACT = decltype(act)::value;
+                if (s.n % SLOPE_V == 0) hipLaunchKernelGGL((k_slope<E, R, ACT, VECTORS>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
+                else hipLaunchKernelGGL((k_slope<E, R, ACT, VALUES>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
+            };
+            if (a->act == CRAFTAX_ACT_NONE) slope(std::integral_constant<int, CRAFTAX_ACT_NONE>{});
+            else if (a->act == CRAFTAX_ACT_RELU) slope(std::integral_constant<int, CRAFTAX_ACT_RELU>{});
+            else if (a->act == CRAFTAX_ACT_SILU) slope(std::integral_constant<int, CRAFTAX_ACT_SILU>{});
+            else slope(std::integral_constant<int, CRAFTAX_ACT_GELU_TANH>{});
             if (a->dbias) sum_rows(s.part, (int)c.slope_y, a->outputs, PutBias{a->dbias}, st);
         }
         const Operand<E> dp = own ? Operand<E>{own, dense_rows(c.dp_row)} : Operand<E>{static_cast<const E*>(a->dout.data), rows_of(a, a->dout)};
@@ -597,11 +673,12 @@ int projection_backward(const craftax_projection_args* a, void* stream, const ch
             ProductParams<E, E> p{};
             const E* weight = static_cast<const E*>(a->weight);
             int64_t ld = a->weight_column;
-            if (c.turn) {
-                E* turned = reinterpret_cast<E*>(work + c.turned_at);
-                turn<E>(weight, a->weight_row, turned, c.turned_row, a->outputs, a->inputs, st);
-                weight = turned;
-                ld = c.turned_row;
+            if (c.turn || c.fill_weight) {
+                E* ours = reinterpret_cast<E*>(work + c.weight_at);
+                if (c.turn) turn<E>(weight, a->weight_row, ours, c.weight_row, a->outputs, a->inputs, st);
+                else fill_up<E>({weight, dense_rows(ld)}, ours, a->inputs, a->outputs, st);
+                weight = ours;
+                ld = c.weight_row;
             }
             p.p = {weight, dense_rows(ld)};
             p.q = dp;
@@ -613,7 +690,7 @@ int projection_backward(const craftax_projection_args* a, void* stream, const ch
             auto weight = [&](auto w) {
                 using W = decltype(w);
                 ProductParams<E, W> p{};
-                p.p = {static_cast<const E*>(a->x.data), rows_of(a, a->x)};
+                p.p = x_of<E>(a, c, work, st);
                 p.q = dp;
                 p.k = c.rows; p.m = (uint32_t)a->outputs; p.n = a->inputs;
                 p.finish.out = static_cast<W*>(a->dweight); p.finish.out_rows = dense_rows(a->inputs); p.finish.columns = a->inputs;
