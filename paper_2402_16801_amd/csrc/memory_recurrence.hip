@@ -15,7 +15,7 @@
 namespace mem {
 
 constexpr int REC_THREADS = 256;
-constexpr int REC_SPAN = 8;             // steps between two saved states
+constexpr int REC_SPAN = 4;             // steps between two saved states
 
 template <typename E> struct RecParams {
     const float* rate;
@@ -29,26 +29,31 @@ template <typename E> struct RecParams {
     float* part;             // backward: [rows of blocks][channels], gradients of the rates
     int steps, n, channels, vectors, lanes_log2;
     int parts, stretch;      // parts of a sequence, steps of one
-    uint32_t items, xblocks; // rows that are walked along, and blocks side by side on channels
-    int64_t stride;          // backward: a thread goes on to the row that many behind
+    uint32_t items, xblocks; // sequences, and blocks side by side on channels
+    uint32_t groups;         // of parts, of a sequence
+    int group;               // parts in one
+    int64_t stride;          // backward: a thread goes on to the sequence that many behind; with parts there is none
     unsigned wide;
 };
 
-// What a block works on: channels side by side on 2^lanes_log2 lanes, and as many rows (a part of an environment each) as there is room.
-struct RecPlace {
-    int vec, side;
-    uint32_t item, row_block;
+// What a block works on: channels side by side on 2^lanes_log2 lanes, and rows: a sequence each, or, where sequences are split into parts, as many
+// parts of one of them, one behind the other.
+constexpr int REC_GROUP = 16;           // parts of a sequence that a block goes along, at most
+template <bool SPLIT> struct RecPlace {
+    int vec, side, group;
+    uint32_t row_block;
+    int64_t item;
     bool on;
     template <typename P> __device__ __forceinline__ explicit RecPlace(const P& p)
     {
-        const int64_t block = spread_block(p.wide);
-        const int lanes = 1 << p.lanes_log2, rows = REC_THREADS >> p.lanes_log2;
+        const uint32_t block = (uint32_t)spread_block(p.wide);
+        const int lanes = 1 << p.lanes_log2, rows = SPLIT ? p.group : REC_THREADS >> p.lanes_log2;
         side = threadIdx.x >> p.lanes_log2;
-        row_block = (uint32_t)block / p.xblocks;
-        vec = (int)((uint32_t)block % p.xblocks) * lanes + (threadIdx.x & (lanes - 1));
-        const int64_t at = (int64_t)row_block * rows + side;
-        item = (uint32_t)at;
-        on = vec < p.vectors && at < (int64_t)p.items;
+        row_block = block / p.xblocks;
+        vec = (int)(block % p.xblocks) * lanes + (threadIdx.x & (lanes - 1));
+        group = SPLIT ? (int)(row_block % p.groups) : 0;
+        item = SPLIT ? (int64_t)(row_block / p.groups) : (int64_t)row_block * rows + side;
+        on = vec < p.vectors && item < (int64_t)p.items;
     }
 };
 
@@ -87,32 +92,66 @@ template <typename P> __device__ __forceinline__ float* sum_at(const P& p, int s
     return p.sums + ((int64_t)(2 * slot + which) * p.n + i) * p.channels + c;
 }
 
-// state (or gradient) = factor * state + term of `count` parts from slot `from` on, in steps of `by`; a factor below 0 stands for a part
-// that forgets what came before it, whatever that was
-template <int V, typename P> __device__ __forceinline__ void go_through(const P& p, int from, int by, int count, int i, int c, float (&h)[V])
+// What parts do to a state (or its gradient): factor * state + term; a factor below 0 stands for parts that forget what came before them,
+// whatever that was.
+template <int V> struct Effect {
+    Pack<float, V> f, b;
+    __device__ __forceinline__ static Effect none()
+    {
+        Effect e;
+#pragma unroll
+        for (int j = 0; j < V; ++j) { e.f.v[j] = 1.0f; e.b.v[j] = 0.0f; }
+        return e;
+    }
+    __device__ __forceinline__ void then(const Effect& o)
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const bool cut = o.f.v[j] < 0.0f;
+            b.v[j] = cut ? o.b.v[j] : __builtin_fmaf(o.f.v[j], b.v[j], o.b.v[j]);
+            f.v[j] = cut || f.v[j] < 0.0f ? -1.0f : f.v[j] * o.f.v[j];
+        }
+    }
+};
+// of `count` slots from `from` on, in steps of `by`
+template <int V, typename P> __device__ __forceinline__ Effect<V> effect_of(const P& p, int from, int by, int count, int i, int c)
 {
     constexpr int GO = 8;
-    auto apply = [&](const Pack<float, V>& f, const Pack<float, V>& b) {
+    Effect<V> all = Effect<V>::none();
+    for (int k = 0; k < count; k += GO) {
+        Effect<V> e[GO];
 #pragma unroll
-        for (int j = 0; j < V; ++j) h[j] = f.v[j] < 0.0f ? b.v[j] : __builtin_fmaf(f.v[j], h[j], b.v[j]);
-    };
-    int k = 0;
-    for (; k + GO <= count; k += GO) {
-        Pack<float, V> f[GO], b[GO];
+        for (int g = 0; g < GO; ++g)
+            if (k + g < count) {
+                fetch<float, V>(e[g].f, sum_at(p, from + (k + g) * by, 0, i, c));
+                fetch<float, V>(e[g].b, sum_at(p, from + (k + g) * by, 1, i, c));
+            }
 #pragma unroll
-        for (int g = 0; g < GO; ++g) {
-            fetch<float, V>(f[g], sum_at(p, from + (k + g) * by, 0, i, c));
-            fetch<float, V>(b[g], sum_at(p, from + (k + g) * by, 1, i, c));
-        }
-#pragma unroll
-        for (int g = 0; g < GO; ++g) apply(f[g], b[g]);
+        for (int g = 0; g < GO; ++g)
+            if (k + g < count) all.then(e[g]);
     }
-    for (; k < count; ++k) {
-        Pack<float, V> f, b;
-        fetch<float, V>(f, sum_at(p, from + k * by, 0, i, c));
-        fetch<float, V>(b, sum_at(p, from + k * by, 1, i, c));
-        apply(f, b);
+    return all;
+}
+// The state behind `far` slots and then `near` rows of this block.  The rows share the slots; `own` is what this row's part does.
+// FORWARD: the slots are those from 0 on and the rows those before this one, else the slots are those from `first` down and the rows those behind.
+template <int V, bool FORWARD, typename P>
+__device__ __forceinline__ void state_behind(const P& p, const RecPlace<true>& at, int first, int far, int own, int i, int c, bool rows_behind, Effect<V> (&maps)[2][REC_GROUP][WAVE],
+                                             float (&h)[V])
+{
+    const int lane = threadIdx.x & ((1 << p.lanes_log2) - 1), each = (far + p.group - 1) / p.group, mine = at.side * each;
+    const int count = far - mine < each ? far - mine : each;
+    maps[0][at.side][lane] = at.on ? effect_of<V>(p, FORWARD ? mine : first - mine, FORWARD ? 1 : -1, count, i, c) : Effect<V>::none();
+    maps[1][at.side][lane] = at.on && own >= 0 ? effect_of<V>(p, own, 1, 1, i, c) : Effect<V>::none();
+    __syncthreads();
+    Effect<V> all = Effect<V>::none();
+    for (int s = 0; s < p.group; ++s) all.then(maps[0][s][lane]);
+    if (FORWARD) {
+        for (int s = 0; s < at.side; ++s) all.then(maps[1][s][lane]);
+    } else if (rows_behind) {
+        for (int s = p.group - 1; s > at.side; --s) all.then(maps[1][s][lane]);
     }
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = all.f.v[j] < 0.0f ? all.b.v[j] : __builtin_fmaf(all.f.v[j], h[j], all.b.v[j]);
 }
 
 template <int V> __device__ __forceinline__ void put_sum(float* factor, float* term, const Span& w, const float (&f)[V], const float (&b)[V])
@@ -125,23 +164,25 @@ template <int V> __device__ __forceinline__ void put_sum(float* factor, float* t
 // state at the begin, slot 1 + q part q, and the last part is not asked for.
 enum RecMode { RUN, SAVE, PARTS };
 
-template <typename E, int V, RecMode MODE, bool GATE, bool CUTS>
-__global__ __launch_bounds__(REC_THREADS) void k_recurrence(const RecParams<E> p)
+// SPLIT: sequences are split into parts, sixteen of one to a block.
+template <typename E, int V, RecMode MODE, bool GATE, bool CUTS, bool SPLIT>
+__global__ __launch_bounds__(SPLIT ? REC_GROUP * WAVE : REC_THREADS) void k_recurrence(const RecParams<E> p)
 {
-    constexpr int AHEAD = 4;
-    const RecPlace at(p);
-    if (!at.on) return;
-    const uint32_t split = MODE == PARTS ? p.parts - 1 : p.parts;
-    const int i = (int)(at.item / split), part = (int)(at.item % split);
-    const Span w = Span::of<V>(at.vec, p.channels);
-    const int t0 = part * p.stretch, t1 = p.steps - t0 < p.stretch ? p.steps : t0 + p.stretch;
+    // few wavefronts wait for memory more often than many
+    constexpr int AHEAD = V == 1 ? 8 : 4;
+    const RecPlace<SPLIT> at(p);
+    if (!SPLIT && !at.on) return;
+    const int i = at.on ? (int)at.item : 0, part = SPLIT ? at.group * p.group + at.side : 0;
+    const bool on = at.on && part < p.parts - (MODE == PARTS ? 1 : 0);
+    const Span w = Span::of<V>(at.on ? at.vec : 0, p.channels);
+    const int t0 = on ? part * p.stretch : 0, t1 = p.steps - t0 < p.stretch ? p.steps : t0 + p.stretch;
     const int length = length_of(p.lengths, p.steps, i);
     const int live = t1 < length ? t1 : length;
     const int64_t state_at = (int64_t)i * p.channels + w.c;
     float h[V] = {}, keep[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) keep[j] = 1.0f;
-    if (part == 0) {
+    if (on && part == 0 && (MODE == PARTS || !SPLIT)) {
         if (p.state_in) {
             const Pack<float, V> q = *reinterpret_cast<const Pack<float, V>*>(p.state_in + state_at);
             expand<float, V>(q, h);
@@ -153,7 +194,11 @@ __global__ __launch_bounds__(REC_THREADS) void k_recurrence(const RecParams<E> p
         }
     }
     // With parts the state at the begin comes from slot 0: another thread may write the new state to its place.
-    if (MODE != PARTS && p.parts > 1) go_through<V>(p, 0, 1, part + 1, i, w.c, h);
+    if constexpr (MODE != PARTS && SPLIT) {
+        __shared__ Effect<V> maps[2][REC_GROUP][WAVE];
+        state_behind<V, true>(p, at, 0, at.group * p.group + 1, part < p.parts - 1 ? part + 1 : -1, i, w.c, false, maps, h);
+    }
+    if (SPLIT && !on) return;
     if (t0 < live) {
         float rate[V];
         load_rates<V>(p.rate, w.c, rate);
@@ -192,6 +237,7 @@ __global__ __launch_bounds__(REC_THREADS) void k_recurrence(const RecParams<E> p
                 put<E, V>(to, w, shrink<E, V>(y));
                 to += p.y.step;
             }
+            __builtin_amdgcn_sched_barrier(0);       // step by step: several at a time take the registers of further wavefronts
         };
         int t = t0;
         for (; t + AHEAD <= live; t += AHEAD) {
@@ -256,36 +302,43 @@ template <typename E, int V, bool GATE> struct RecRaw {
     uint32_t first[REC_SPAN];
 };
 
-template <typename E, int V, RecMode MODE, bool GATE, bool CUTS>
-__global__ __launch_bounds__(REC_THREADS) void k_recurrence_backward(const RecParams<E> p)
+template <typename E, int V, RecMode MODE, bool GATE, bool CUTS, bool SPLIT>
+__global__ __launch_bounds__(SPLIT ? REC_GROUP * WAVE : REC_THREADS) void k_recurrence_backward(const RecParams<E> p)
 {
-    __shared__ float sums[REC_THREADS * V];
-    const RecPlace at(p);
-    const uint32_t split = MODE == PARTS ? p.parts - 1 : p.parts;
+    __shared__ float sums[(SPLIT ? REC_GROUP * WAVE : REC_THREADS) * V];
+    const RecPlace<SPLIT> at(p);
     float total[V] = {};
-    for (int64_t item = at.on ? at.item : (int64_t)p.items; item < (int64_t)p.items; item += p.stride) {
-        const int i = (int)((uint32_t)item / split), part = (int)((uint32_t)item % split) + (MODE == PARTS ? 1 : 0);
-        const Span w = Span::of<V>(at.vec, p.channels);
-        const int t0 = part * p.stretch, t1 = p.steps - t0 < p.stretch ? p.steps : t0 + p.stretch;
+    for (int64_t item = SPLIT || at.on ? at.item : (int64_t)p.items; item < (int64_t)p.items; item += p.stride) {
+        const int i = (int)item, part = SPLIT ? at.group * p.group + at.side : 0;
+        const bool on = at.on && part < p.parts && (MODE != PARTS || part > 0);
+        const Span w = Span::of<V>(at.on ? at.vec : 0, p.channels);
+        const int t0 = on ? part * p.stretch : 0, t1 = p.steps - t0 < p.stretch ? p.steps : t0 + p.stretch;
         const int length = length_of(p.lengths, p.steps, i);
         const int live = t1 < length ? t1 : length;
         const int64_t state_at = (int64_t)i * p.channels + w.c;
         float g[V] = {}, keep[V];              // gradient of the state behind the step that is next
 #pragma unroll
         for (int j = 0; j < V; ++j) keep[j] = 1.0f;
-        const bool last = t0 < length ? live == length : part == 0 && length == 0;
+        const bool last = on && (t0 < length ? live == length : part == 0 && length == 0);
+        if constexpr (MODE != PARTS && SPLIT) {
+            // the parts behind this one, up to that of the last step that counts, which starts with the gradient of the state behind it
+            __shared__ Effect<V> maps[2][REC_GROUP][WAVE];
+            const int behind = length > 0 ? (length - 1) / p.stretch : 0, here = at.group * p.group + p.group - 1;
+            state_behind<V, false>(p, at, behind, behind > here ? behind - here : 0, part > 0 && part <= behind ? part : -1, i, w.c, true, maps, g);
+        }
         if (last && p.dstate_out) {
             Pack<float, V> q;
             fetch<float, V>(q, p.dstate_out + state_at);
             expand<float, V>(q, g);
+        } else if (last) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) g[j] = 0.0f;
         }
         if (last) {
 #pragma unroll
             for (int j = 0; j < V; ++j) keep[j] = -1.0f;
-        } else if (MODE != PARTS && t0 < length) {
-            const int behind = (length - 1) / p.stretch;
-            go_through<V>(p, behind, -1, behind - part, i, w.c, g);
         }
+        if (!on) break;
         if (MODE != PARTS) {
             for (int t = t0 > live ? t0 : live; t < t1; ++t) {
                 put<E, V>(p.dx.at(t, i) + w.c, w, Pack<E, V>{});
@@ -390,16 +443,17 @@ __global__ __launch_bounds__(REC_THREADS) void k_recurrence_backward(const RecPa
     }
     if (MODE == PARTS || p.part == nullptr) return;
     // one partial row per block
+    constexpr int THREADS = SPLIT ? REC_GROUP * WAVE : REC_THREADS;
 #pragma unroll
-    for (int j = 0; j < V; ++j) sums[j * REC_THREADS + threadIdx.x] = total[j];
+    for (int j = 0; j < V; ++j) sums[j * THREADS + threadIdx.x] = total[j];
     __syncthreads();
     if (at.side != 0 || at.vec >= p.vectors) return;
-    const int rows = REC_THREADS >> p.lanes_log2;
+    const int rows = SPLIT ? p.group : REC_THREADS >> p.lanes_log2;
     const Span w = Span::of<V>(at.vec, p.channels);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         float v = 0.0f;
-        for (int r = 0; r < rows; ++r) v += sums[j * REC_THREADS + (r << p.lanes_log2) + threadIdx.x];
+        for (int r = 0; r < rows; ++r) v += sums[j * THREADS + (r << p.lanes_log2) + threadIdx.x];
         total[j] = v;
     }
     put<float, V>(p.part + (int64_t)at.row_block * p.channels + w.c, w, shrink<float, V>(total));
@@ -439,33 +493,42 @@ static int rec_check(const craftax_recurrence_args* a, bool backward, const char
     return CRAFTAX_OK;
 }
 
-// Wavefronts per SIMD from which on sequences are walked whole with several channels per thread, and those that parts make.
-constexpr int REC_ENOUGH = 2, REC_FILL = 4, REC_SHORTEST = 32;
+// Wavefronts per SIMD from which on threads take several channels (of fewer, one), from which on sequences are walked whole, and that parts make;
+// steps of the shortest part.
+constexpr int REC_WIDE = 2, REC_ENOUGH = 1, REC_FILL = 4, REC_SHORTEST = 16;
 constexpr int REC_BLOCKS = 4096;
 
 // How a call is cut: channels per thread, parts of a sequence, blocks.
 struct RecCut {
     int width, vectors, lanes_log2, parts, stretch;
     uint32_t xblocks;
-    // blocks over rows; backward no more than fill the chip several times over, each with rows in turn, for their partial sums
-    uint32_t row_blocks(int64_t items, bool backward) const
+    // Blocks of few parts are placed more easily, those of many read fewer parts before their own (37 ragged sequences of 1,000 steps of 647 channels,
+    // forward and backward, in groups of 4 and 16: 310 and 340 us; one of 10,000 steps of 512 channels, 512 parts, groups of 16: 32).
+    int groups() const { return parts > 1 ? (int)ceil_div(parts, parts <= 128 ? 4 : REC_GROUP) : 1; }
+    int group() const { return (int)ceil_div(parts, groups()); }
+    // blocks over sequences, or groups of their parts; backward no more than fill the chip several times over, each with sequences in turn, for
+    // their partial sums
+    uint32_t row_blocks(int64_t n, bool backward) const
     {
-        const int64_t need = ceil_div(items, REC_THREADS >> lanes_log2), most = ceil_div(REC_BLOCKS, xblocks);
+        if (parts > 1) return (uint32_t)(n * groups());
+        const int64_t need = ceil_div(n, REC_THREADS >> lanes_log2), most = ceil_div(REC_BLOCKS, xblocks);
         return (uint32_t)(backward && need > most ? most : need);
     }
 };
+
 static RecCut rec_cut(const craftax_recurrence_args* a, bool backward)
 {
     RecCut c;
     c.width = backward ? 2 : 4;
     auto waves = [&] { return (int64_t)a->n * ceil_div(a->channels, c.width) / WAVE; };
-    if (a->channels < c.width || waves() < REC_ENOUGH * CHIP_SIMDS) c.width = 1;
+    if (a->channels < c.width || waves() < REC_WIDE * CHIP_SIMDS) c.width = 1;
     c.vectors = (int)ceil_div(a->channels, c.width);
     c.lanes_log2 = 0;
     while (c.lanes_log2 < 6 && (1 << c.lanes_log2) < c.vectors) ++c.lanes_log2;
     c.xblocks = (uint32_t)ceil_div(c.vectors, 1 << c.lanes_log2);
     const int64_t have = waves() < 1 ? 1 : waves();
-    int64_t parts = have >= REC_ENOUGH * CHIP_SIMDS ? 1 : REC_FILL * CHIP_SIMDS / have;
+    // where lengths are given, about half of the parts have nothing to do
+    int64_t parts = have >= REC_ENOUGH * CHIP_SIMDS ? 1 : (a->lengths ? REC_FILL * 3 / 2 : REC_FILL) * CHIP_SIMDS / have;
     if (parts > a->steps / REC_SHORTEST) parts = a->steps / REC_SHORTEST;
     if (parts < 1) parts = 1;
     c.stretch = (int)(ceil_div(ceil_div(a->steps, parts), REC_SPAN) * REC_SPAN);
@@ -488,7 +551,7 @@ size_t recurrence_workspace_bytes(const craftax_recurrence_args* a, bool backwar
     if (!a || a->steps < 1 || a->n < 1 || a->channels < 1 || a->steps > MOST_COUNT || (int64_t)a->n * a->channels > MOST_COUNT) return 0;
     const RecCut c = rec_cut(a, backward);
     size_t bytes = rec_sums_bytes(a, c);
-    if (backward && a->drate) bytes += round256((size_t)c.row_blocks((int64_t)a->n * c.parts, true) * a->channels * sizeof(float));
+    if (backward && a->drate) bytes += round256((size_t)c.row_blocks(a->n, true) * a->channels * sizeof(float));
     return bytes;
 }
 
@@ -529,15 +592,18 @@ template <typename F> static void with_options(const craftax_recurrence_args* a,
     else cuts(std::false_type{});
 }
 
-// launches over `items` rows
-template <typename P, typename K> static void rec_launch(K kernel, P& p, const RecCut& c, int64_t items, bool backward, hipStream_t st)
+// launches over all sequences
+template <typename P, typename K> static void rec_launch(K kernel, P& p, const RecCut& c, bool backward, hipStream_t st)
 {
-    const uint32_t blocks = c.row_blocks(items, backward);
-    p.items = (uint32_t)items;
-    p.stride = (int64_t)blocks * (REC_THREADS >> c.lanes_log2);
-    const Spread grid = spread((int64_t)c.xblocks * blocks, REC_THREADS);
+    const uint32_t blocks = c.row_blocks(p.n, backward);
+    const int threads = c.parts > 1 ? c.group() << c.lanes_log2 : REC_THREADS;
+    p.items = (uint32_t)p.n;
+    p.groups = (uint32_t)c.groups();
+    p.group = c.group();
+    p.stride = c.parts > 1 ? (int64_t)1 << 40 : (int64_t)blocks * (REC_THREADS >> c.lanes_log2);
+    const Spread grid = spread((int64_t)c.xblocks * blocks, threads);
     p.wide = grid.x;
-    hipLaunchKernelGGL(kernel, dim3(grid.x, 1, grid.z), dim3(REC_THREADS), 0, st, p);
+    hipLaunchKernelGGL(kernel, dim3(grid.x, 1, grid.z), dim3(threads), 0, st, p);
 }
 
 template <typename E, int V> static void rec_token(const craftax_recurrence_args* a, hipStream_t st)
@@ -573,9 +639,16 @@ int recurrence(const craftax_recurrence_args* a, void* stream, const char** why)
             constexpr int V = decltype(width)::value;
             with_options(a, [&](auto gate, auto cuts) {
                 constexpr bool GATE = decltype(gate)::value, CUTS = decltype(cuts)::value;
-                if (c.parts > 1) rec_launch(k_recurrence<E, V, PARTS, false, CUTS>, p, c, (int64_t)a->n * (c.parts - 1), false, st);
-                if (a->saved) rec_launch(k_recurrence<E, V, SAVE, GATE, CUTS>, p, c, (int64_t)a->n * c.parts, false, st);
-                else rec_launch(k_recurrence<E, V, RUN, GATE, CUTS>, p, c, (int64_t)a->n * c.parts, false, st);
+                if constexpr (V == 1) {
+                    if (c.parts > 1) {
+                        rec_launch(k_recurrence<E, V, PARTS, false, CUTS, true>, p, c, false, st);
+                        if (a->saved) rec_launch(k_recurrence<E, V, SAVE, GATE, CUTS, true>, p, c, false, st);
+                        else rec_launch(k_recurrence<E, V, RUN, GATE, CUTS, true>, p, c, false, st);
+                        return;
+                    }
+                }
+                if (a->saved) rec_launch(k_recurrence<E, V, SAVE, GATE, CUTS, false>, p, c, false, st);
+                else rec_launch(k_recurrence<E, V, RUN, GATE, CUTS, false>, p, c, false, st);
             });
         };
         if (c.width == 4) run(std::integral_constant<int, 4>{});
@@ -590,7 +663,6 @@ int recurrence_backward(const craftax_recurrence_args* a, void* stream, const ch
     if (int rc = rec_room(a, recurrence_workspace_bytes(a, true), why)) return rc;
     const hipStream_t st = (hipStream_t)stream;
     const RecCut c = rec_cut(a, true);
-    const int64_t items = (int64_t)a->n * c.parts;
     float* part = a->drate ? reinterpret_cast<float*>(static_cast<char*>(a->workspace) + rec_sums_bytes(a, c)) : nullptr;
     with_type(a->dtype, [&](auto e) {
         using E = decltype(e);
@@ -601,15 +673,21 @@ int recurrence_backward(const craftax_recurrence_args* a, void* stream, const ch
             constexpr int V = decltype(width)::value;
             with_options(a, [&](auto gate, auto cuts) {
                 constexpr bool GATE = decltype(gate)::value, CUTS = decltype(cuts)::value;
-                if (c.parts > 1) rec_launch(k_recurrence_backward<E, V, PARTS, GATE, CUTS>, p, c, (int64_t)a->n * (c.parts - 1), true, st);
-                rec_launch(k_recurrence_backward<E, V, RUN, GATE, CUTS>, p, c, items, true, st);
+                if constexpr (V == 1) {
+                    if (c.parts > 1) {
+                        rec_launch(k_recurrence_backward<E, V, PARTS, GATE, CUTS, true>, p, c, true, st);
+                        rec_launch(k_recurrence_backward<E, V, RUN, GATE, CUTS, true>, p, c, true, st);
+                        return;
+                    }
+                }
+                rec_launch(k_recurrence_backward<E, V, RUN, GATE, CUTS, false>, p, c, true, st);
             });
         };
         if (c.width == 2) run(std::integral_constant<int, 2>{});
         else run(std::integral_constant<int, 1>{});
     });
     if (int rc = launched(why)) return rc;
-    if (part) sum_rows(part, (int)c.row_blocks(items, true), a->channels, PutRate{a->drate}, st);
+    if (part) sum_rows(part, (int)c.row_blocks(a->n, true), a->channels, PutRate{a->drate}, st);
     return launched(why);
 }
 
