@@ -518,13 +518,19 @@ constexpr int64_t CHIP_UNITS = 256;
 constexpr int64_t MOST_VALUES = (int64_t)1 << 42;       // of a matrix: its tiles are counted in 32 bits
 
 static int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return ceil_div(m, side) * ceil_div(n, side); }
-// Whether tiles of 128 x 128 are enough for every compute unit, with long sums cut into parts of eight tiles along k at least.  (3,003 rows of
-// 8,268 float32 values onto 256 are 48 of them, in ten parts each.  4,096 rows of 512 bfloat16 values onto 1,024 are 256: 11.7 us, in tiles of 64 x 64
-// 14.5.)
-static bool tiled(int64_t m, int64_t n, int64_t k, size_t elem)
+// The parts that a sum of k products may be cut into: eight tiles along k at least each, for the gradient of a weight, whose tiles are few, four.
+// (A backward pass of 4,096 rows of 512 bfloat16 values onto 512 takes 42 us, with eight for both 54, with four for both 53; of 1,024 rows 30, 43
+// and 32.)
+static int64_t most_parts(int64_t k, size_t elem, bool inside)
 {
-    const int64_t parts = k * (int64_t)elem / (8 * TILE_BYTES);
-    return m > 64 && n > 64 && tiles_of(m, n, 128) * (parts > 1 ? parts : 1) >= CHIP_UNITS;
+    const int64_t parts = k * (int64_t)elem / ((inside ? 8 : 4) * TILE_BYTES);
+    return parts > 1 ? parts : 1;
+}
+// Whether tiles of that size are enough for every compute unit, with long sums cut into parts.  (3,003 rows of 8,268 float32 values onto 256 are
+// 48 of 128 x 128, in ten parts each.  4,096 rows of 512 bfloat16 values onto 1,024 are 256: 11.7 us, in tiles of 64 x 64 14.5.)
+static bool tiled(int64_t m, int64_t n, int64_t k, size_t elem, bool inside = true, int64_t side = 128)
+{
+    return m > side / 2 && n > side / 2 && tiles_of(m, n, side) * most_parts(k, elem, inside) >= CHIP_UNITS;
 }
 
 static Plan plan(int64_t m, int64_t n, int64_t k, size_t elem, bool inside, bool direct)
@@ -541,15 +547,16 @@ static Plan plan(int64_t m, int64_t n, int64_t k, size_t elem, bool inside, bool
         return c;
     }
     // A compute unit takes 0.4 times as long for a tile of 128 x 128 as for one of 256 x 256 (1,200 and 740 TFLOP/s for 8,192 squared, bfloat16).
-    const bool larger = 10 * ceil_div(tiles(256), CHIP_UNITS) <= 4 * ceil_div(tiles(128), CHIP_UNITS) || (!inside && m > 128 && n > 128);
+    const bool larger = 10 * ceil_div(tiles(256), CHIP_UNITS) <= 4 * ceil_div(tiles(128), CHIP_UNITS) || (!inside && tiled(m, n, k, elem, false, 256));
     if (direct) c.cut = larger ? Cut::DIRECT_LARGE : Cut::DIRECT;
-    else c.cut = tiled(m, n, k, elem) || (!inside && m >= 128 && n >= 128) ? Cut::LARGE : Cut::SMALL;
+    else c.cut = tiled(m, n, k, elem, inside) ? Cut::LARGE : Cut::SMALL;
     if (inside && n <= 32) c.cut = Cut::NARROW;
     const int64_t side = c.cut == Cut::DIRECT_LARGE ? 256 : c.cut == Cut::SMALL ? 64 : 128;
     c.m_tiles = (uint32_t)ceil_div(m, side);
     c.n_tiles = (uint32_t)ceil_div(n, c.cut == Cut::NARROW ? 32 : side);
-    // long sums of few tiles are cut, into parts of eight tiles along k at least, until every compute unit has what it holds at once
-    const int64_t have = (int64_t)c.m_tiles * c.n_tiles, room = c.cut == Cut::DIRECT_LARGE ? CHIP_UNITS : c.cut == Cut::NARROW ? 4 * CHIP_UNITS : 2 * CHIP_UNITS, most = k / (8 * step);
+    // long sums of few tiles are cut until every compute unit has what it holds at once
+    const int64_t have = (int64_t)c.m_tiles * c.n_tiles, most = most_parts(k, elem, inside);
+    const int64_t room = c.cut == Cut::DIRECT_LARGE ? CHIP_UNITS : c.cut == Cut::NARROW ? 4 * CHIP_UNITS : 2 * CHIP_UNITS;
     int64_t parts = have < room ? room / have : 1;
     if (parts > most) parts = most;
     if (parts > 1) {
