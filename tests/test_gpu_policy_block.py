@@ -59,6 +59,8 @@ REC_CASES = [
     ("f32", 301, 6, 70, "batch", True, False, 0.01, True),
     ("f16", 1025, 2, 33, "slice", False, True, 0.004, False),
     ("f32", 2050, 1, 130, "time", True, True, 0.001, True),
+    ("bf16", 4099, 1, 64, "time", True, True, 0.0, False),
+    ("f32", 3001, 2, 20, "batch", False, True, 0.0005, True),
 ]
 
 
@@ -367,6 +369,70 @@ def test_projection_of_exact_values(mem):
         assert torch.equal(g.weight.cpu().double(), d.t() @ x), (dtype, rows)
         assert torch.equal(g.bias.cpu().double(), d.sum(0)), (dtype, rows)
         assert torch.equal(g.x.cpu().double(), (d @ w).to(TYPES[dtype]).double()), (dtype, rows)
+
+
+def test_projection_of_exact_values_in_large_tiles(mem):
+    """The same where operands go straight to LDS: more columns than biases are kept for, tiles that end inside the matrix, rows that are copied to where
+    they can be read (odd counts, a slice of wider rows, environments first), sums in parts."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+
+    def whole(most, *shape):
+        return torch.randint(-most, most + 1, shape, generator=gen, device="cuda").double()
+
+    for dtype, T, n, I, O, layout in (("bf16", 1, 1500, 64, 4200, "time"), ("f16", 1, 4000, 64, 4200, "time"), ("bf16", 1, 4000, 72, 4100, "time"),
+                                      ("bf16", 60, 351, 701, 300, "time"), ("f16", 50, 410, 704, 300, "slice"), ("bf16", 300, 70, 704, 301, "batch"),
+                                      ("bf16", 1, 900, 8192, 520, "time"), ("f16", 40, 400, 512, 264, "batch")):
+        kind = TYPES[dtype]
+        x, w, b, d, res = whole(2, T, n, I), whole(1, O, I), whole(30, O), whole(1, T, n, O), whole(30, T, n, O)
+        if layout == "batch":
+            gx, gres, gd = (v.to(kind).transpose(0, 1).contiguous().transpose(0, 1) for v in (x, res, d))
+        elif layout == "slice":
+            gx = torch.full((T, n + 3, I), float("nan"), dtype=kind, device="cuda")[:, 2:n + 2].copy_(x)
+            gres, gd = res.to(kind), torch.full((T, n, O + 8), float("nan"), dtype=kind, device="cuda")[..., :O].copy_(d)
+        else:
+            gx, gres, gd = x.to(kind), res.to(kind), d.to(kind)
+        out, pre = mem.projection(gx, w.to(kind), b.float(), residual=gres, act="relu", save=True)
+        want = x.reshape(-1, I) @ w.t() + b
+        assert torch.equal(pre.double(), want.to(kind).double().reshape(T, n, O)), (dtype, T, n, I, O)
+        exact = (want.clamp(min=0.0).reshape(T, n, O) + res).to(kind).double()
+        assert torch.equal(out.double(), exact), (dtype, T, n, I, O)
+        for weight in (w.to(kind), w.to(kind).t().contiguous().t()):
+            g = mem.projection_backward(gd, gx, weight, b.float(), float_weight=True)
+            flat = d.reshape(-1, O)
+            assert torch.equal(g.weight.double(), flat.t() @ x.reshape(-1, I)), (dtype, T, n, I, O)
+            assert torch.equal(g.bias.double(), flat.sum(0)), (dtype, T, n, I, O)
+            assert torch.equal(g.x.double(), (d @ w).to(kind).double()), (dtype, T, n, I, O)
+
+
+@pytest.mark.parametrize("rows,I,O", [(700, 300, 400), (3000, 500, 24), (40, 2000, 1100)])
+def test_projection_of_float32_at_the_ends_of_its_range(mem, rows, I, O):
+    """Float32 values go through the matrix units in three parts: infinities, NaN and the largest numbers come out as from a plain sum, in their
+    rows alone, and every other value of the same tile to the same digits as without them.  Very large and very small rows keep their digits."""
+    src = Source(rows, torch.float32)
+    x, w = src.normal(rows, I), src.normal(O, I, spread=I ** -0.5)
+    x[1], x[2] = x[1] * 2.0 ** 100, x[2] * 2.0 ** -80
+    want = x @ w.t()
+    off = sums(x.abs() @ w.abs().t(), I)
+    spoilt = x.clone()
+    spoilt[5, I - 1], spoilt[9, 0], spoilt[11, I // 2] = float("inf"), float("nan"), -float("inf")
+    spoilt[13] = 0.0
+    spoilt[13, 3] = torch.finfo(torch.float32).max
+    for given in (x, spoilt):
+        out, _ = mem.projection(plain(given), plain(w))
+        got = out.cpu().double()
+        for m in range(rows):
+            if given is x or m not in (5, 9, 11, 13):
+                assert bool(((got[m] - want[m]).abs() <= 2 * ROUND[torch.float32] * want[m].abs() + 2 * off[m]).all()), m
+    assert bool(got[9].isnan().all()) and torch.equal(got[5], float("inf") * w[:, I - 1].sign()) and torch.equal(got[11], -float("inf") * w[:, I // 2].sign())
+    exact = torch.finfo(torch.float32).max * w[:, 3]
+    assert bool(((got[13] - exact).abs() <= 2 * ROUND[torch.float32] * exact.abs()).all())
+    d = src.normal(rows, O)
+    g = mem.projection_backward(plain(d), plain(spoilt), plain(w))
+    fine = [c for c in range(I) if c not in (0, 3, I // 2, I - 1)]
+    keep = spoilt[:, fine]
+    size = d.abs().t() @ keep.abs()
+    assert bool(((g.weight.cpu().double()[:, fine] - d.t() @ keep).abs() <= 2 * sums(size, rows)).all())
+    assert bool(g.weight[:, 0].isnan().all()) and bool(g.weight[:, I - 1].isinf().all())
 
 
 def test_projection_leaves_what_is_beside_its_outputs(mem):
