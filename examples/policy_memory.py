@@ -1,9 +1,9 @@
 """A policy with memory on the simulator: acts one step at a time, learns from whole rollouts.
 
-    python examples/policy_memory.py [--envs N] [--steps T] [--updates U] [--dtype bf16|f32]
+    python examples/policy_memory.py [--envs N] [--steps T] [--updates U] [--dtype bf16|f32] [--cell scan|recurrence] [--dropout P]
 
 Two recurrent blocks (short causal convolution, selective state space scan, and the norm that joins a
-block to the next) between an embedding of Craftax-Classic's symbolic observation and the heads for
+block to the next; or projections around a gated recurrence, with dropout onto the residual) between an embedding of Craftax-Classic's symbolic observation and the heads for
 actions and values.  While acting, the blocks take one token per environment and carry their states;
 an environment whose episode has ended starts with empty ones, by the simulator's own `done`.  For
 the update the same blocks take the rollout as [steps][n] sequences, from the states it began with,
@@ -78,12 +78,61 @@ class Block(torch.nn.Module):
         return residual, u, state
 
 
+class GatedBlock(torch.nn.Module):
+    """Projection, convolution, gated recurrence, projection, dropout onto the residual, norm.  The dropout's mask belongs to a step's
+    number, which is a part of the state: a rollout is learned with the masks that it was acted with."""
+    SEED = 1
+
+    def __init__(self, width, inner=None, taps=4, drop=0.0, number=0, dtype=torch.bfloat16):
+        super().__init__()
+        inner = 2 * width if inner is None else inner
+
+        def weight(outputs, inputs):
+            return torch.nn.Parameter(torch.randn(outputs, inputs, device="cuda") * inputs ** -0.5)
+
+        self.inner, self.taps, self.drop, self.seed, self.dtype = inner, taps, drop, self.SEED + number, dtype
+        self.w_in, self.w_out = weight(4 * inner, width), weight(width, inner)
+        self.b_in = torch.nn.Parameter(torch.zeros(4 * inner, device="cuda"))
+        self.conv_weight = torch.nn.Parameter(torch.randn(inner, taps, device="cuda") * taps ** -0.5)
+        # rates of 0.002 to 1 a step, half of them where a gate is half open: memories from two to a thousand steps
+        self.log_rate = torch.nn.Parameter(torch.linspace(-6.2, 0.0, inner, device="cuda"))
+        self.pre_weight = torch.nn.Parameter(torch.ones(width, device="cuda"))
+
+    def empty(self, n):
+        return [torch.zeros(n, self.taps - 1, self.inner, dtype=self.dtype, device="cuda"), torch.zeros(n, self.inner, device="cuda"),
+                torch.zeros(1, dtype=torch.int64, device="cuda")]
+
+    def forward(self, residual, u, state, first):
+        """As Block's."""
+        step, rate = u.dim() == 2, -self.log_rate.exp()
+        x, decay, intake, z = memory.project(u, self.w_in, self.b_in).split(self.inner, -1)
+        if step:
+            x, _ = memory.causal_conv_step(x, self.conv_weight, None, state[0], first=first)
+            y, _ = memory.gated_recurrence_step(x, decay, intake, rate, state[1], z=z, first=first)
+        else:
+            x, tail = memory.conv(x, self.conv_weight, state=state[0], first=first)
+            y, h = memory.recurrence(x, decay, intake, rate, z=z, state=state[1], first=first)
+        y = memory.project(y, self.w_out)
+        if step:
+            residual, u = (v[0] for v in memory.residual_norm(torch.zeros_like(y)[None], memory.residual_dropout(
+                y, self.drop, self.seed, residual=residual, step=state[2])[None], pre_weight=self.pre_weight))
+            state[2] += 1
+        else:
+            residual = memory.dropout(y, self.drop, self.seed, residual=residual, step=state[2])
+            residual, u = memory.norm(torch.zeros_like(residual), residual, pre_weight=self.pre_weight)
+            state = [tail, h, state[2] + len(y)]
+        return residual, u, state
+
+
 class Policy(torch.nn.Module):
-    def __init__(self, inputs, width=256, blocks=2, dtype=torch.bfloat16, **how):
+    def __init__(self, inputs, width=256, blocks=2, dtype=torch.bfloat16, cell="scan", drop=0.0, **how):
         super().__init__()
         self.dtype = dtype
         self.embed = torch.nn.Parameter(torch.randn(inputs, width, device="cuda") * inputs ** -0.5)
-        self.blocks = torch.nn.ModuleList(Block(width, dtype=dtype, **how) for _ in range(blocks))
+        if cell == "scan":
+            self.blocks = torch.nn.ModuleList(Block(width, dtype=dtype, **how) for _ in range(blocks))
+        else:
+            self.blocks = torch.nn.ModuleList(GatedBlock(width, drop=drop, number=k, dtype=dtype, **how) for k in range(blocks))
         self.head = torch.nn.Parameter(torch.randn(width, ACTIONS + 1, device="cuda") * (0.1 * width ** -0.5))
 
     def empty(self, n):
@@ -140,11 +189,13 @@ def main():
     ap.add_argument("--steps", type=int, default=64)
     ap.add_argument("--updates", type=int, default=10)
     ap.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
+    ap.add_argument("--cell", choices=("scan", "recurrence"), default="scan", help="what a block's memory is")
+    ap.add_argument("--dropout", type=float, default=0.1, help="share of a block's output that is dropped (recurrence)")
     args = ap.parse_args()
     torch.manual_seed(0)
     sim = cx.Craftax(args.envs, cx.default_config(obs_mode=cx.OBS_SYM_F32))
     sim.reset(synth.seeds_for(args.envs))
-    policy = Policy(sim.obs_bytes // 4, dtype={"bf16": torch.bfloat16, "f32": torch.float32}[args.dtype])
+    policy = Policy(sim.obs_bytes // 4, dtype={"bf16": torch.bfloat16, "f32": torch.float32}[args.dtype], cell=args.cell, drop=args.dropout)
     optimizer = torch.optim.Adam(policy.parameters(), lr=3e-4, eps=1e-5)
     states, first = policy.empty(args.envs), torch.ones(args.envs, dtype=torch.uint8, device="cuda")
     for update in range(args.updates):

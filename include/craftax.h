@@ -381,7 +381,8 @@ int craftax_stats_static(const void *state, craftax_metrics *out, int n, void *s
  *
  * A window of 7x9 or 9x11 cells shows little of a world, so a policy needs a memory (section
  * "Baselines" of the paper: its strongest baseline is recurrent).  These calls are the parts of a
- * recurrent policy block that are no plain matrix product, for acting (one token per environment
+ * recurrent policy block: two memories (a selective scan, a gated recurrence), a convolution, norms,
+ * products with what follows them, and dropout, for acting (one token per environment
  * and step), for reading prompts and for training on rollouts as this library writes them.  They
  * take no state object and know nothing of the game.
  *

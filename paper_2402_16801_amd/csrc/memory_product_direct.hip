@@ -2,9 +2,10 @@
 // each, or 128 x 128 by four of 64 by 64, two tiles of 64 along k.
 //
 // What bounds them: a step of 64 along k of a 256 x 256 tile is 2,048 cycles of matrix instructions for a SIMD and 2,048 cycles of a compute unit's
-// LDS at 128 bytes each (192 KiB of fragments read, 64 KiB written), and it takes about 4,000.  8,192 squared in bfloat16: 917 us, 1,200
-// TFLOP/s.  At the widths of a policy sums are short (512 is eight steps) and a tile's results, 128 KiB, take memory as long as a third of
-// its sums; blocks go on to further tiles, whose first operands are under way while results are stored.
+// LDS at 128 bytes each (192 KiB of fragments read, 64 KiB written), and it takes about 4,000.  8,192 squared in bfloat16: 920 to 1,040 us, 1,060
+// to 1,200 TFLOP/s, the library's product 1,400.  At the widths of a policy sums are short (512 is eight steps) and a tile's results, 128 KiB
+// (256 with what an activation's backward pass needs), take memory as long as a third of its sums or longer; blocks go on to further tiles, whose
+// first operands are under way while results are stored.  262,144 rows of 512 onto 1,024 with gelu, its argument kept: 468 us, 1.49 GB.
 #include "memory_product.hpp"
 
 #include <type_traits>
