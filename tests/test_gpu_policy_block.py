@@ -435,6 +435,30 @@ def test_projection_of_float32_at_the_ends_of_its_range(mem, rows, I, O):
     assert bool(g.weight[:, 0].isnan().all()) and bool(g.weight[:, I - 1].isinf().all())
 
 
+@pytest.mark.parametrize("rows", [(7, 5), (60, 70), (90, 500)])
+def test_projection_of_tensors_in_different_orders(mem, rows):
+    """x lies environments first, residual and the gradient steps first, pre in a slice: whole numbers, so everything is exact."""
+    T, n = rows
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    I, O = 136, 264
+
+    def whole(most, *shape):
+        return torch.randint(-most, most + 1, shape, generator=gen, device="cuda").double()
+
+    for dtype in TYPES.values():
+        x, w, d, res = whole(2, T, n, I), whole(1, O, I), whole(1, T, n, O), whole(9, T, n, O)
+        gx = x.to(dtype).transpose(0, 1).contiguous().transpose(0, 1)
+        out, pre = mem.projection(gx, w.to(dtype), residual=res.float(), act="relu", save=True)
+        want = x @ w.t()
+        assert torch.equal(out.double(), want.clamp(min=0.0) + res) and torch.equal(pre.double(), want)
+        kept = torch.full((T, n + 1, O + 3), float("nan"), dtype=dtype, device="cuda")[:, 1:, 2:O + 2].copy_(pre)
+        g = mem.projection_backward(d.float(), gx, w.to(dtype), torch.zeros(O, device="cuda"), pre=kept, act="relu", float_weight=True)
+        dp = d * (want > 0)
+        assert torch.equal(g.x.double(), (dp @ w).to(dtype).double())
+        assert torch.equal(g.weight.double(), dp.reshape(-1, O).t() @ x.reshape(-1, I))
+        assert torch.equal(g.bias.double(), dp.reshape(-1, O).sum(0))
+
+
 def test_projection_leaves_what_is_beside_its_outputs(mem):
     """At the C entry: outputs inside wider rows, everything around them as it was; and inputs beside NaN."""
     from paper_2402_16801_amd import binding as cx
@@ -715,6 +739,48 @@ def test_operators_on_another_stream_and_in_a_graph(mem, T, n, width, inner):
         assert all(torch.equal(a, b) for a, b in zip(outs, want[k])), k
         mem.projection(sets[0]["x"], w["in"])
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T", [1, 8, 40, 2000])
+@pytest.mark.parametrize("D", [66, 3])
+def test_recurrence_updates_a_state_in_place(mem, T, D):
+    """At the C entry state_out may be state_in, for one part of steps as for many."""
+    from paper_2402_16801_amd import binding as cx
+    lib, n = cx.load(), 2
+    x, decay, intake, y = (torch.randn(T, n, D, device="cuda") for _ in range(4))
+    rate, state = -torch.rand(D, device="cuda") * 0.01, torch.randn(n, D, device="cuda")
+    want_y, want, _ = mem.gated_recurrence(x, decay, intake, rate, state=state)
+    views = {f: v for k, t in (("x", x), ("decay", decay), ("intake", intake), ("y", y)) for f, v in ((k, t.data_ptr()), (k + "_step", n * D), (k + "_env", D))}
+    args = cx.RecurrenceArgs(dtype=0, steps=T, n=n, channels=D, rate=rate.data_ptr(), state_in=state.data_ptr(), state_out=state.data_ptr(), **views)
+    need = lib.craftax_gated_recurrence_workspace_bytes(args, 0)
+    work = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+    args.workspace, args.workspace_bytes = work.data_ptr(), need
+    torch.cuda.synchronize()
+    assert lib.craftax_gated_recurrence(args, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(y, want_y) and torch.equal(state, want)
+
+
+@pytest.mark.parametrize("size", [(40, 130, 72, 88), (150, 2, 96, 64)])
+def test_calls_on_two_streams_at_once(mem, size):
+    """Each call has its own workspace: two streams that work at the same time give what they give alone, again and again."""
+    T, n, width, inner = size
+    src = Source(53, torch.bfloat16)
+    w = {"in": src.gpu(src.normal(3 * inner, width, spread=0.1)), "bias": plain(src.normal(3 * inner)), "rate": plain(-torch.exp(src.normal(inner))),
+         "out": src.gpu(src.normal(width, inner, spread=0.1))}
+    sets = [{"x": src.gpu(src.seq(T, n, width)), "state": plain(src.normal(n, inner))} for _ in range(2)]
+    first = src.flags(T, n, 0.05).cuda()
+    number = torch.zeros(1, dtype=torch.int64, device="cuda")
+    want = [[v.clone() for v in _all_operators(mem, s, w, first, number)] for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(4):
+        got = []
+        for s, stream in zip(sets, streams):
+            with torch.cuda.stream(stream):
+                got.append(_all_operators(mem, s, w, first, number))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, v in zip(got, want) for a, b in zip(g, v))
 
 
 def test_states_of_the_recurrence_as_autograd_sees_them(mem):
