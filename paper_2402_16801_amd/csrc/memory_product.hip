@@ -520,6 +520,7 @@ struct Plan {
     size_t part_bytes;
 };
 constexpr int64_t CHIP_UNITS = 256;
+constexpr int64_t FRAGMENT_BYTES = 2 << 20;
 constexpr int64_t MOST_VALUES = (int64_t)1 << 42;       // of a matrix: its tiles are counted in 32 bits
 
 static int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return ceil_div(m, side) * ceil_div(n, side); }
@@ -531,11 +532,12 @@ static int64_t most_parts(int64_t k, size_t elem, bool inside)
     const int64_t parts = k * (int64_t)elem / ((inside ? 8 : 4) * TILE_BYTES);
     return parts > 1 ? parts : 1;
 }
-// Whether tiles of that size are enough for every compute unit, with long sums cut into parts.  (3,003 rows of 8,268 float32 values onto 256 are
-// 48 of 128 x 128, in ten parts each.  4,096 rows of 512 bfloat16 values onto 1,024 are 256: 11.7 us, in tiles of 64 x 64 14.5.)
+// Whether tiles of that size are enough for every compute unit, with long sums cut into parts, of sixteen tiles along k at least where k lies inside.
+// (3,003 rows of 8,268 float32 values onto 256 are 48 of 128 x 128, in ten parts each: 104 us, in tiles of 64 x 64 160.  4,096 rows of 1,024
+// bfloat16 values onto 512, 128 in two parts of eight, would take 25, in tiles of 64 x 64 16.  4,096 of 512 onto 1,024, 256 tiles: 11.7 and 14.5.)
 static bool tiled(int64_t m, int64_t n, int64_t k, size_t elem, bool inside = true, int64_t side = 128)
 {
-    return m > side / 2 && n > side / 2 && tiles_of(m, n, side) * most_parts(k, elem, inside) >= CHIP_UNITS;
+    return m > side / 2 && n > side / 2 && tiles_of(m, n, side) * most_parts(inside ? k / 2 : k, elem, inside) >= CHIP_UNITS;
 }
 
 static Plan plan(int64_t m, int64_t n, int64_t k, size_t elem, bool inside, bool direct)
@@ -545,7 +547,10 @@ static Plan plan(int64_t m, int64_t n, int64_t k, size_t elem, bool inside, bool
     auto tiles = [&](int64_t side) { return tiles_of(m, n, side); };
     c.parts = 1;
     c.k_part = ceil_div(k, step) * step;
-    if (inside && tiles(16) <= 4 * CHIP_UNITS) {
+    // Fragments straight from memory leave no operand to read again, and each block goes along the whole of k: for few and short ones.  (512 rows of
+    // bfloat16 onto 512, 1,024 fragments: 1,024 values a row 10.7 us, in tiles 12.0, 2,048 values 17.9 and 13.5, 8,192 59 and 23.  256 fragments:
+    // 4,096 values 10.1 and 13.9, 8,192 17.4 and 13.2.)
+    if (inside && tiles(16) <= 4 * CHIP_UNITS && tiles(16) * k * (int64_t)elem <= FRAGMENT_BYTES) {
         c.cut = Cut::ROWS;
         c.m_tiles = (uint32_t)ceil_div(m, 16);
         c.n_tiles = (uint32_t)ceil_div(n, 16);
