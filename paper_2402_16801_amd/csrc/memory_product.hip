@@ -705,8 +705,8 @@ struct Project {
     size_t weight_at, x_at, dp_at, sums_at, part_at, total;
 };
 // Where rows cannot go straight to LDS they are copied to where they can, if the product is worth it: reading and writing them takes as long as
-// this many columns of the result gain by it, and a copy is a launch more.  (bfloat16, 1,345 values a row onto 512: 262,144 rows, 1.8e11 products,
-// take 700 us, through registers 858; 4,096 rows, 2.8e9 products, 37 us, through registers 24.)
+// this many columns of the result gain by it, and a copy is a launch more.  (bfloat16: 16,384 rows of 333 values onto 1,024, 5.6e9 products, take 36 us,
+// through registers 57; 262,144 rows of 1,345 onto 512 700 and 858; but 4,096 rows of 1,345 onto 512, 2.8e9 products, 33 and 23.)
 constexpr int64_t WORTH_COLUMNS = 256;
 constexpr double WORTH_PRODUCTS = 4e9;
 
