@@ -542,7 +542,8 @@ int craftax_gated_recurrence_backward(const craftax_recurrence_args *args, void 
  * [inputs] values per step and environment, out [outputs].  Element (o, i) of weight lies at weight[o * weight_row + i * weight_column],
  * and one of the two strides is 1.  pre, rounded to dtype, is what the backward call needs unless act is CRAFTAX_ACT_NONE.
  * Backward: dp = dout * act'(pre), dx = dp * weight, dweight = dp^T * x, dbias = the sum of dp (the gradient of residual is dout).  The
- * products take dp rounded to dtype, the sum of dbias does not.  Sums are in 32 bits. */
+ * products take dp rounded to dtype, the sum of dbias does not.  Sums are in 32 bits.  float32 values go through the matrix units as three
+ * bfloat16 parts, which hold all of their digits down to 2^-110, and an absolute 2^-126 below. */
 enum { CRAFTAX_ACT_NONE = 0, CRAFTAX_ACT_RELU = 1, CRAFTAX_ACT_SILU = 2, CRAFTAX_ACT_GELU_TANH = 3 };
 typedef struct craftax_projection_args {
     uint32_t dtype;             /* of x, weight, pre and dx */
@@ -581,7 +582,7 @@ typedef struct craftax_dropout_args {
     uint64_t seed;
     int64_t step, env;          /* numbers of the first step and environment: step + steps below 2^63, env + n at most 2^32 */
     const int64_t *step_at;     /* one number that is added to step, or NULL */
-    craftax_view x, residual, out;     /* residual may be absent: 0; out may be x or residual */
+    craftax_view x, residual, out;     /* residual may be absent: 0; out may be x or residual, if types and strides are its own */
 } craftax_dropout_args;
 int craftax_residual_dropout(const craftax_dropout_args *args, void *stream);
 

@@ -663,6 +663,12 @@ static craftax_projection_args ordered(const craftax_projection_args* given)
 // the weight's rows lie with the inputs side by side
 static bool by_rows(const craftax_projection_args* a) { return a->weight_column == 1 || a->inputs == 1; }
 
+static bool countable(const craftax_projection_args* a)
+{
+    const int64_t rows = (int64_t)a->steps * a->n, wide = a->inputs > a->outputs ? a->inputs : a->outputs;
+    return rows <= MOST_VALUES / wide && a->inputs <= MOST_VALUES / a->outputs;
+}
+
 static int projection_check(const craftax_projection_args* a, bool backward, const char** why)
 {
     if (!a) return refuse(CRAFTAX_E_NULL, "args is NULL", why);
@@ -672,8 +678,7 @@ static int projection_check(const craftax_projection_args* a, bool backward, con
     if (a->steps < 1 || a->n < 1 || a->inputs < 1 || a->outputs < 1) return refuse(CRAFTAX_E_COUNT, "steps, n, inputs and outputs must be positive", why);
     if ((int64_t)a->steps * a->n >= (int64_t)1 << 31) return refuse(CRAFTAX_E_COUNT, "steps * n must be below 2^31", why);
     if (a->inputs > MOST_COUNT || a->outputs > MOST_COUNT) return refuse(CRAFTAX_E_COUNT, "inputs and outputs must be below 2^31 - 4095", why);
-    const int64_t rows = (int64_t)a->steps * a->n, wide = a->inputs > a->outputs ? a->inputs : a->outputs;
-    if (rows > MOST_VALUES / wide || a->inputs > MOST_VALUES / a->outputs) return refuse(CRAFTAX_E_COUNT, "more values than memory holds", why);
+    if (!countable(a)) return refuse(CRAFTAX_E_COUNT, "more values than memory holds", why);
     if (!by_rows(a) && a->weight_row != 1 && a->outputs != 1) return refuse(CRAFTAX_E_COUNT, "weight_row or weight_column must be 1", why);
     if (!a->weight || !a->x.data) return refuse(CRAFTAX_E_NULL, "weight or x is NULL", why);
     const size_t e = elem_bytes(a->dtype), r = elem_bytes(a->out_dtype);
@@ -771,7 +776,7 @@ static Project project(const craftax_projection_args* a, bool backward)
 size_t projection_workspace_bytes(const craftax_projection_args* a, bool backward)
 {
     if (!a || a->dtype > CRAFTAX_F16 || a->steps < 1 || a->n < 1 || a->inputs < 1 || a->outputs < 1 || a->inputs > MOST_COUNT || a->outputs > MOST_COUNT ||
-        (int64_t)a->steps * a->n >= (int64_t)1 << 31)
+        (int64_t)a->steps * a->n >= (int64_t)1 << 31 || !countable(a))
         return 0;
     const craftax_projection_args ours = ordered(a);
     return project(&ours, backward).total;

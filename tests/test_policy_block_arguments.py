@@ -42,6 +42,11 @@ def test_counts_out_of_range_are_refused_at_the_c_entry():
     pro = binding.ProjectionArgs(dtype=1, out_dtype=1, steps=1 << 16, n=1 << 15, inputs=1, outputs=1, weight=at, weight_row=1, weight_column=1, x=at, out=at, dout=at)
     for call in (lib.craftax_projection, lib.craftax_projection_backward):
         assert call(pro, None) == -3 and b"steps * n" in lib.craftax_last_error()
+    for steps, n, inputs, outputs in ((1 << 15, 1 << 15, 1 << 13, 1), (1, 1, 1 << 30, 1 << 13), (1 << 20, 1 << 10, 1, most)):
+        pro.steps, pro.n, pro.inputs, pro.outputs = steps, n, inputs, outputs
+        for backward, call in enumerate((lib.craftax_projection, lib.craftax_projection_backward)):
+            assert call(pro, None) == -3 and b"memory" in lib.craftax_last_error()
+            assert lib.craftax_projection_workspace_bytes(pro, backward) == 0
     drop = binding.DropoutArgs(dtype=1, out_dtype=1, steps=1 << 16, n=1 << 15, channels=1, p=0.5, x=at, out=at)
     assert lib.craftax_residual_dropout(drop, None) == -3 and b"steps * n" in lib.craftax_last_error()
 
