@@ -542,7 +542,8 @@ int craftax_gated_recurrence_backward(const craftax_recurrence_args *args, void 
  * [inputs] values per step and environment, out [outputs].  Element (o, i) of weight lies at weight[o * weight_row + i * weight_column],
  * and one of the two strides is 1.  pre, rounded to dtype, is what the backward call needs unless act is CRAFTAX_ACT_NONE.
  * Backward: dp = dout * act'(pre), dx = dp * weight, dweight = dp^T * x, dbias = the sum of dp (the gradient of residual is dout).  The
- * products take dp rounded to dtype, the sum of dbias does not.  Sums are in 32 bits.  float32 values go through the matrix units as three
+ * products take dp rounded to dtype (float16 beside a float32 dout: times a power of two that brings its largest value below 2^15, taken back from
+ * their sums), the sum of dbias does not.  Sums are in 32 bits.  float32 values go through the matrix units as three
  * bfloat16 parts, which hold all of their digits down to 2^-110, and an absolute 2^-126 below. */
 enum { CRAFTAX_ACT_NONE = 0, CRAFTAX_ACT_RELU = 1, CRAFTAX_ACT_SILU = 2, CRAFTAX_ACT_GELU_TANH = 3 };
 typedef struct craftax_projection_args {

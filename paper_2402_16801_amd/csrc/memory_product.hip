@@ -429,10 +429,71 @@ template <typename E, typename R> struct SlopeParams {
     E* dp;
     Rows dout_rows, pre_rows;
     int64_t dp_row;
+    float* factor;           // what takes the power of two back that dp is stored with (see k_largest), or nullptr: stored as it is
+    float* largest;          // of k_largest's blocks
+    int blocks;
     float* part;
     uint32_t m;
     int n, across;
 };
+// a row's eight columns, or as many as there are, and the values of dp they are
+template <Edge EDGE, typename P> __device__ __forceinline__ void slope_take(const P* from, int count, Pack<P, SLOPE_V>& to)
+{
+    if (EDGE == VECTORS || count >= SLOPE_V) {
+        to = *reinterpret_cast<const Pack<P, SLOPE_V>*>(from);
+    } else {
+#pragma unroll
+        for (int j = 0; j < SLOPE_V; ++j) to.v[j] = from[j < count ? j : 0];
+    }
+}
+
+// The range of float16.  dp of a float32 gradient may be anything that float32 holds, and float16 ends at 65,504 and at 6e-8: dp is stored times a power of
+// two that brings its largest value to 2^14 .. 2^15, which both products take back from their sums (ACT_SCALED).  Values keep their eleven bits down to
+// 2^-29 of the largest, and an absolute 2^-40 of it below.  This pass finds the largest finite value of every block, k_slope that of all: it reads what
+// k_slope reads once more (262,144 rows of 1,024, without and with an activation: 190 and 290 us).
+__device__ __forceinline__ float block_largest(float most, float (&sums)[256])
+{
+    sums[threadIdx.x] = most;
+    for (int half = 128; half > 0; half /= 2) {
+        __syncthreads();
+        if ((int)threadIdx.x < half) sums[threadIdx.x] = __builtin_fmaxf(sums[threadIdx.x], sums[threadIdx.x + half]);
+    }
+    __syncthreads();
+    return sums[0];
+}
+template <typename E, typename R, int ACT, Edge EDGE>
+__global__ __launch_bounds__(256) void k_largest(const SlopeParams<E, R> p)
+{
+    __shared__ float sums[256];
+    const int across = 1 << p.across, x = threadIdx.x & (across - 1), y = threadIdx.x >> p.across, c = ((int)blockIdx.x * across + x) * SLOPE_V, count = p.n - c;
+    float most = 0.0f;
+    if (count > 0) {
+        const uint32_t rows = 256u >> p.across, step = gridDim.y * rows;
+        for (uint32_t m = blockIdx.y * rows + y; m < p.m; m += step) {
+            Pack<R, SLOPE_V> d;
+            Pack<E, SLOPE_V> v = {};
+            slope_take<EDGE>(p.dout + p.dout_rows.at(m) + c, count, d);
+            if (ACT != CRAFTAX_ACT_NONE) slope_take<EDGE>(p.pre + p.pre_rows.at(m) + c, count, v);
+#pragma unroll
+            for (int j = 0; j < SLOPE_V; ++j) {           // of a ragged end the first value comes up again
+                float size = Elem<R>::up(d.v[j]);
+                if (ACT != CRAFTAX_ACT_NONE) size *= slope_of<ACT>(Elem<E>::up(v.v[j]));
+                size = __builtin_fabsf(size);
+                most = size > most && size <= __FLT_MAX__ ? size : most;
+            }
+        }
+    }
+    most = block_largest(most, sums);
+    if (threadIdx.x == 0) p.largest[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = most;
+}
+// The power of two of dp whose largest value is `most`, and what takes it back (`back`): both normal numbers.
+__device__ __forceinline__ float power_for(float most, float& back)
+{
+    const int exponent = (int)(__float_as_uint(most) >> 23) - 127;          // -127: 0, or below the normal numbers
+    const int by = most == 0.0f ? 0 : (14 - exponent < 126 ? 14 - exponent : 126);
+    back = __uint_as_float((uint32_t)(127 - by) << 23);
+    return __uint_as_float((uint32_t)(127 + by) << 23);
+}
 // EDGE: VECTORS where eight divide the columns, else VALUES.
 template <typename E, typename R, int ACT, Edge EDGE>
 __global__ __launch_bounds__(256) void k_slope(const SlopeParams<E, R> p)
@@ -440,22 +501,22 @@ __global__ __launch_bounds__(256) void k_slope(const SlopeParams<E, R> p)
     constexpr int GO = 1;              // rows under way together (two or four were no faster)
     __shared__ float sums[SLOPE_V][256];
     const int across = 1 << p.across, x = threadIdx.x & (across - 1), y = threadIdx.x >> p.across, c = ((int)blockIdx.x * across + x) * SLOPE_V, count = p.n - c;
-    float total[SLOPE_V] = {};
+    float total[SLOPE_V] = {}, scale = 1.0f;
+    constexpr bool SCALED = std::is_same_v<E, _Float16> && std::is_same_v<R, float>;
+    if (SCALED && p.factor) {
+        float most = 0.0f, back;
+        for (int k = threadIdx.x; k < p.blocks; k += 256) most = __builtin_fmaxf(most, p.largest[k]);
+        scale = power_for(block_largest(most, sums[0]), back);
+        if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *p.factor = back;
+        __syncthreads();
+    }
     if (count > 0) {
         const uint32_t rows = 256u >> p.across, step = gridDim.y * rows, last = p.m - 1;
         struct Raw { Pack<R, SLOPE_V> d; Pack<E, SLOPE_V> v; } raw[GO];
-        auto take = [&](auto* from, auto& to) {
-            if (EDGE == VECTORS || count >= SLOPE_V) {
-                to = *reinterpret_cast<const std::remove_reference_t<decltype(to)>*>(from);
-            } else {
-#pragma unroll
-                for (int j = 0; j < SLOPE_V; ++j) to.v[j] = from[j < count ? j : 0];
-            }
-        };
         auto load = [&](uint32_t row, Raw& q) {
             const uint32_t m = row < last ? row : last;
-            take(p.dout + p.dout_rows.at(m) + c, q.d);
-            if (ACT != CRAFTAX_ACT_NONE) take(p.pre + p.pre_rows.at(m) + c, q.v);
+            slope_take<EDGE>(p.dout + p.dout_rows.at(m) + c, count, q.d);
+            if (ACT != CRAFTAX_ACT_NONE) slope_take<EDGE>(p.pre + p.pre_rows.at(m) + c, count, q.v);
         };
         uint32_t m = blockIdx.y * rows + y;
 #pragma unroll
@@ -478,7 +539,10 @@ __global__ __launch_bounds__(256) void k_slope(const SlopeParams<E, R> p)
                 const uint32_t row = m + g * step;
                 if (row >= p.m) continue;
 #pragma unroll
-                for (int j = 0; j < SLOPE_V; ++j) total[j] += d[g][j];
+                for (int j = 0; j < SLOPE_V; ++j) {
+                    total[j] += d[g][j];
+                    if (SCALED) d[g][j] *= scale;
+                }
                 if (p.dp) Finish<E, R>::template store<E, SLOPE_V>(p.dp + (int64_t)row * p.dp_row + c, SLOPE_V, d[g]);
             }
         }
@@ -704,10 +768,10 @@ struct Project {
     bool turn, fill_weight;  // the weight is turned, or its rows are filled up, first
     bool fill_x;             // the rows of x are
     int64_t weight_row, x_row, dp_row;   // of what lies in the workspace
-    bool has_dp;
+    bool has_dp, scaled;     // dp lies in the workspace; times a power of two
     int slope_across;
     unsigned slope_x, slope_y;
-    size_t weight_at, x_at, dp_at, sums_at, part_at, total;
+    size_t weight_at, x_at, dp_at, scale_at, sums_at, part_at, total;
 };
 // Where rows cannot go straight to LDS they are copied to where they can, if the product is worth it: reading and writing them takes as long as
 // this many columns of the result gain by it, and a copy is a launch more.  (bfloat16: 16,384 rows of 333 values onto 1,024, 5.6e9 products, take 36 us,
@@ -757,6 +821,8 @@ static Project project(const craftax_projection_args* a, bool backward)
         c.slope_x = (unsigned)ceil_div(a->outputs, SLOPE_V << c.slope_across);
         int64_t y = ceil_div(c.rows, 256 >> c.slope_across), most = ceil_div(2048, c.slope_x);
         c.slope_y = (unsigned)(y < most ? y : most);
+        c.scaled = c.has_dp && a->dtype == CRAFTAX_F16 && a->out_dtype == CRAFTAX_F32;
+        if (c.scaled) c.scale_at = take((1 + (size_t)c.slope_x * c.slope_y) * sizeof(float));
         if (a->dbias) c.sums_at = take((size_t)c.slope_y * a->outputs * sizeof(float));
         size_t part = 0;
         if (a->dx.data) {
@@ -847,7 +913,7 @@ int projection(const craftax_projection_args* given, void* stream, const char** 
         p.q = x_of<E>(a, c, work, st);
         p.k = a->inputs; p.m = (uint32_t)c.rows; p.n = a->outputs;
         p.finish = {a->bias, static_cast<const R*>(a->residual.data), static_cast<R*>(a->out.data), static_cast<E*>(a->pre.data),
-                    rows_of(a, a->residual), rows_of(a, a->out), rows_of(a, a->pre), (int)a->act, a->outputs};
+                    rows_of(a, a->residual), rows_of(a, a->out), rows_of(a, a->pre), (int)a->act, a->outputs, nullptr};
         launch_product<true>(c.forward, p, reinterpret_cast<float*>(work + c.part_at), st);
     });
     return launched(why);
@@ -865,15 +931,23 @@ int projection_backward(const craftax_projection_args* given, void* stream, cons
         using E = decltype(e);
         using R = decltype(r);
         E* own = c.has_dp ? reinterpret_cast<E*>(work + c.dp_at) : nullptr;
+        float* factor = c.scaled ? reinterpret_cast<float*>(work + c.scale_at) : nullptr;
         if (own || a->dbias) {
             SlopeParams<E, R> s{};
             s.dout = static_cast<const R*>(a->dout.data); s.dout_rows = rows_of(a, a->dout);
             s.pre = a->act == CRAFTAX_ACT_NONE ? nullptr : static_cast<const E*>(a->pre.data); s.pre_rows = rows_of(a, a->pre);
             s.dp = own; s.dp_row = c.dp_row;
+            s.factor = factor; s.largest = factor ? factor + 1 : nullptr; s.blocks = (int)(c.slope_x * c.slope_y);
             s.part = a->dbias ? reinterpret_cast<float*>(work + c.sums_at) : nullptr;
             s.m = (uint32_t)c.rows; s.n = a->outputs; s.across = c.slope_across;
             auto slope = [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
+                if constexpr (std::is_same_v<E, _Float16> && std::is_same_v<R, float>) {
+                    if (factor) {
+                        if (s.n % SLOPE_V == 0) hipLaunchKernelGGL((k_largest<E, R, ACT, VECTORS>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
+                        else hipLaunchKernelGGL((k_largest<E, R, ACT, VALUES>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
+                    }
+                }
                 if (s.n % SLOPE_V == 0) hipLaunchKernelGGL((k_slope<E, R, ACT, VECTORS>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
                 else hipLaunchKernelGGL((k_slope<E, R, ACT, VALUES>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
             };
@@ -885,8 +959,14 @@ int projection_backward(const craftax_projection_args* given, void* stream, cons
         }
         const Operand<E> dp = own ? Operand<E>{own, dense_rows(c.dp_row)} : Operand<E>{static_cast<const E*>(a->dout.data), rows_of(a, a->dout)};
         float* part = reinterpret_cast<float*>(work + c.part_at);
+        auto unscale = [&](auto& finish) {
+            if (!factor) return;
+            finish.act = ACT_SCALED;
+            finish.factor = factor;
+        };
         if (a->dx.data) {
             ProductParams<E, E> p{};
+            unscale(p.finish);
             const E* weight = static_cast<const E*>(a->weight);
             int64_t ld = a->weight_column;
             if (c.turn || c.fill_weight) {
@@ -906,6 +986,7 @@ int projection_backward(const craftax_projection_args* given, void* stream, cons
             auto weight = [&](auto w) {
                 using W = decltype(w);
                 ProductParams<E, W> p{};
+                unscale(p.finish);
                 p.p = x_of<E>(a, c, work, st);
                 p.q = dp;
                 p.k = c.rows; p.m = (uint32_t)a->outputs; p.n = a->inputs;

@@ -7,6 +7,8 @@
 
 #include "memory_common.hpp"
 
+#include <type_traits>
+
 namespace mem {
 
 // Where row m of a matrix lies: rows are numbered as steps times environments.  n is 1 where one stride does.
@@ -57,6 +59,9 @@ template <int ACT> __device__ __forceinline__ float slope_of(float p)
     return 1.0f;
 }
 
+// Not of the header's activations: what float16 products of a gradient end with (see k_largest), a multiplication by a number that lies on the device.
+constexpr int ACT_SCALED = CRAFTAX_ACT_GELU_TANH + 1;
+
 // How many of COUNT neighbouring columns are there: all of them; all or none, where COUNT divides their number; any number.
 enum Edge { INNER, VECTORS, VALUES };
 
@@ -69,6 +74,7 @@ template <typename E, typename R> struct Finish {
     E* pre;
     Rows residual_rows, out_rows, pre_rows;
     int act, columns;
+    const float* factor;     // ACT_SCALED
     template <typename P, int COUNT> static __device__ __forceinline__ void store(P* p, int count, const float (&v)[COUNT])
     {
         Pack<P, COUNT> q;
@@ -120,8 +126,14 @@ template <typename E, typename R> struct Finish {
         if (EDGE != INNER && columns <= n) return;
         const int count = EDGE == VALUES ? columns - n : COUNT;
         if (pre) store(pre + pre_rows.at(m) + n, count, v);
-        if constexpr (ACT < 0) activate(v, act);
-        else activate<ACT>(v);
+        if (std::is_same_v<E, _Float16> && (ACT == ACT_SCALED || (ACT < 0 && act == ACT_SCALED))) {
+#pragma unroll
+            for (int j = 0; j < COUNT; ++j) v[j] *= *factor;
+        } else if constexpr (ACT < 0) {
+            activate(v, act);
+        } else {
+            activate<ACT>(v);
+        }
         if (residual) {
 #pragma unroll
             for (int j = 0; j < COUNT; ++j) v[j] += Elem<R>::up(r.v[j]);

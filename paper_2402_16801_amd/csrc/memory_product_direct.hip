@@ -285,6 +285,9 @@ template <bool INSIDE, typename E, typename R> void launch_direct(const ProductP
         else hipLaunchKernelGGL((k_product_direct<E, R, ACT, INSIDE, 4, 4, 2, 2>), dim3(blocks), dim3(256), 0, st, p);
     };
     const int act = p.part ? CRAFTAX_ACT_NONE : p.finish.act;
+    if constexpr (std::is_same_v<E, _Float16> && (!INSIDE || std::is_same_v<E, R>)) {
+        if (act == ACT_SCALED) return go(std::integral_constant<int, ACT_SCALED>{});
+    }
     if constexpr (INSIDE) {
         if (act == CRAFTAX_ACT_RELU) return go(std::integral_constant<int, CRAFTAX_ACT_RELU>{});
         if (act == CRAFTAX_ACT_SILU) return go(std::integral_constant<int, CRAFTAX_ACT_SILU>{});

@@ -1,0 +1,86 @@
+"""The digits that the gated recurrence, the projection and the norm's gate keep where numbers are far from 1: gates that are nearly open, activations
+beyond the range of their type, small and large gradients, parts of float32 values.  Tolerances are relative and derived beside each test."""
+import pytest
+import torch
+
+import policy_block_reference as ref
+from test_gpu_memory import ROUND, TYPES, Source, plain
+from test_gpu_policy_block import near, sums
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mem():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2402_16801_amd import memory
+    return memory
+
+
+def relative(what, got, want, allowed):
+    """Every value, however small, off by no more than that share of itself."""
+    got64 = got.detach().cpu().double()
+    assert got64.shape == want.shape, (what, got64.shape, want.shape)
+    off = ((got64 - want).abs() / want.abs())
+    assert bool((off <= allowed).all()), f"{what}: off by {float(off.max()):.3g} of a value, {allowed:.3g} are allowed"
+
+
+# ---- float32 gradients of float16 activations --------------------------------------------------------------------
+
+GRADIENT_CASES = [
+    # rows, inputs, outputs, act: fragments, heads, tiles through registers, straight to LDS, in parts
+    (5, 40, 30, "none"),
+    (64, 1345, 18, "silu"),
+    (700, 300, 400, "gelu_tanh"),
+    (3000, 72, 44, "relu"),
+    (33000, 128, 136, "none"),
+    (20000, 512, 264, "silu"),
+]
+
+
+@pytest.mark.parametrize("size", [2.0 ** -30, 2.0 ** 24, 2.0 ** -140], ids=["small", "large", "smallest"])
+@pytest.mark.parametrize("case", GRADIENT_CASES, ids=str)
+def test_projection_of_float16_takes_float32_gradients_of_any_size(mem, case, size):
+    """dp comes to the matrix units in float16: values above 65,504 and below 6e-8 have to get there.  Rounded relative to itself, 2^-11, as long as
+    it is above 2^-29 of the largest; rows are up to 2^-20 apart here.  Gradients of the weight are compared in units of `size`, an exact scaling; those of
+    x have 16 bits (near's 2^-25 is half of their smallest step).  The smallest: float32 numbers below the normal ones, whole multiples of 2^-149, so that
+    dp has 2^-150 more, 2^-10 in units of `size`, and what is computed of them 2^-149 on top."""
+    rows, I, O, act = case
+    src = Source(rows + I, torch.float16)
+    x, w = src.seq(1, rows, I)[0], src.normal(O, I, spread={2.0 ** -30: 2.0 ** 10, 2.0 ** 24: 2.0 ** -20, 2.0 ** -140: 2.0 ** 10}[size], dtype=torch.float16)
+    dout = (src.normal(rows, O) * size).float().double()
+    dout[rows // 2] = (dout[rows // 2] * 2.0 ** -20).float().double() if size > 2.0 ** -100 else 0.0
+    pre = src.normal(rows, O, spread=2.0, dtype=torch.float16)
+    given = pre.clone().requires_grad_(True)
+    (dp,) = torch.autograd.grad(ref.act(given, act), given, dout)
+    step = 2.0 ** -9 if size < 2.0 ** -100 else 0.0
+    g = mem.projection_backward(plain(dout), src.gpu(x), src.gpu(w), torch.zeros(O, device="cuda"), pre=None if act == "none" else src.gpu(pre), act=act,
+                                float_weight=True)
+    off = 1.1 * ROUND[torch.float16] + 2.0 ** -21
+    terms = dp.abs().t() @ x.abs()
+    near("gradient of weight", (g.weight.double() / size).float(), (dp.t() @ x) / size, (terms * off + sums(terms, rows)) / size + step * x.abs().sum(0))
+    near("gradient of bias", (g.bias.double() / size).float(), dp.sum(0) / size, (dp.abs().sum(0) * 2.0 ** -21 + sums(dp.abs().sum(0), rows)) / size + step * rows)
+    terms = dp.abs() @ w.abs()
+    near("gradient of x", g.x, dp @ w, terms * off + sums(terms, O))
+    assert size < 2.0 ** -100 or bool((g.weight != 0).any(1).all())
+
+
+@pytest.mark.parametrize("case", GRADIENT_CASES, ids=str)
+def test_projection_of_float16_keeps_infinite_gradients_in_their_rows(mem, case):
+    """Infinities and NaN among float32 gradients stay in their row of dx, whatever the others' size; gradients that are all 0 give 0."""
+    rows, I, O, act = case
+    src = Source(rows, torch.float16)
+    x, w, pre = src.seq(1, rows, I)[0], src.normal(O, I, spread=2.0 ** 10, dtype=torch.float16), src.normal(rows, O, dtype=torch.float16)
+    dout = (src.normal(rows, O) * 2.0 ** -30).float().double()
+    spoilt = dout.clone()
+    spoilt[1, 0], spoilt[rows - 1, O - 1] = float("inf"), float("nan")
+    how = {"pre": None if act == "none" else src.gpu(pre).abs(), "act": act, "float_weight": True}
+    given = pre.abs().requires_grad_(True)
+    (dp,) = torch.autograd.grad(ref.act(given, act), given, dout)
+    g = mem.projection_backward(plain(spoilt), src.gpu(x), src.gpu(w), None, **how)
+    fine = [m for m in range(rows) if m not in (1, rows - 1)]
+    terms = dp[fine].abs() @ w.abs()
+    near("gradient of x", g.x[fine], dp[fine] @ w, terms * (1.1 * ROUND[torch.float16] + 2.0 ** -21) + sums(terms, O))
+    assert not bool(torch.isfinite(g.x[1]).any()) and bool(g.x[rows - 1].isnan().all())
+    g = mem.projection_backward(torch.zeros(rows, O, device="cuda"), src.gpu(x), src.gpu(w), torch.zeros(O, device="cuda"), **how)
+    assert all(bool((v == 0).all()) for v in g)
