@@ -41,17 +41,18 @@ template <int COUNT> __device__ __forceinline__ void activate(float (&v)[COUNT],
     else if (act == CRAFTAX_ACT_SILU) activate<CRAFTAX_ACT_SILU>(v);
     else if (act == CRAFTAX_ACT_GELU_TANH) activate<CRAFTAX_ACT_GELU_TANH>(v);
 }
-// the derivative at p
+// the derivative at p; beyond `END` it is 0 or 1, and infinities would come up against a 0
 template <int ACT> __device__ __forceinline__ float slope_of(float p)
 {
+    constexpr float END = ACT == CRAFTAX_ACT_GELU_TANH ? 16.0f : 256.0f;
     if (ACT == CRAFTAX_ACT_RELU) return p > 0.0f ? 1.0f : (p <= 0.0f ? 0.0f : p);
+    p = p > END ? END : (p < -END ? -END : p);
     if (ACT == CRAFTAX_ACT_SILU) {
         const float g = sigmoid(p);
         return g * __builtin_fmaf(p, 1.0f - g, 1.0f);
     }
     if (ACT == CRAFTAX_ACT_GELU_TANH) {
-        // beyond 16 it is 0 or 1, and the square would leave the range of numbers
-        const float square = __builtin_fminf(p * p, 256.0f);
+        const float square = p * p;
         const float e = exp2_fast(p * __builtin_fmaf(square, -GELU_2K * GELU_C * LOG2E, -GELU_2K * LOG2E));
         const float g = __builtin_amdgcn_rcpf(1.0f + e);
         return g * __builtin_fmaf(1.0f - g, p * __builtin_fmaf(square, 3.0f * GELU_C * GELU_2K, GELU_2K), 1.0f);

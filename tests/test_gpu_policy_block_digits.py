@@ -84,3 +84,30 @@ def test_projection_of_float16_keeps_infinite_gradients_in_their_rows(mem, case)
     assert not bool(torch.isfinite(g.x[1]).any()) and bool(g.x[rows - 1].isnan().all())
     g = mem.projection_backward(torch.zeros(rows, O, device="cuda"), src.gpu(x), src.gpu(w), torch.zeros(O, device="cuda"), **how)
     assert all(bool((v == 0).all()) for v in g)
+
+
+# ---- activations beyond the range of their type ---------------------------------------------------------------------
+
+def test_slopes_of_infinite_arguments_are_0_and_1(mem):
+    """pre in 16 bits may be an infinity where the sum was not."""
+    for dtype in TYPES.values():
+        most = torch.finfo(dtype).max
+        pre = torch.tensor([[-float("inf"), -most, -most / 8, most / 8, most, float("inf"), float("nan")]], dtype=dtype, device="cuda")
+        for act in ("relu", "silu", "gelu_tanh"):
+            g = mem.projection_backward(torch.ones(1, 7, dtype=dtype, device="cuda"), torch.ones(1, 1, dtype=dtype, device="cuda"),
+                                        torch.ones(7, 1, dtype=dtype, device="cuda"), torch.zeros(7, device="cuda"), pre=pre, act=act, want_x=False)
+            for got in (g.weight[:, 0].float(), g.bias):
+                assert got[:6].tolist() == [0.0, 0.0, 0.0, 1.0, 1.0, 1.0] and bool(got[6].isnan()), (act, dtype, got)
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu_tanh"])
+def test_projection_beyond_the_range_of_float16(mem, act):
+    """Sums of 160,000 on a float32 residual: out holds them, pre does not, and the backward pass has their slope."""
+    x = torch.full((40, 64), 50.0, dtype=torch.float16, device="cuda")
+    x[::2] = -50.0
+    w = torch.full((24, 64), 50.0, dtype=torch.float16, device="cuda")
+    out, pre = mem.projection(x, w, residual=torch.ones(40, 24, device="cuda"), act=act, save=True)
+    assert bool((out[1::2] == 160001.0).all()) and bool((out[::2] == 1.0).all()) and bool(pre.isinf().all())
+    g = mem.projection_backward(torch.ones(40, 24, device="cuda"), x, w, torch.zeros(24, device="cuda"), pre=pre, act=act, float_weight=True)
+    assert bool((g.x[1::2] == 1200.0).all()) and bool((g.x[::2] == 0.0).all())
+    assert bool((g.weight == 1000.0).all()) and bool((g.bias == 20.0).all())
