@@ -51,6 +51,9 @@ __device__ __forceinline__ float sigmoid(float v)
     return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-v * LOG2E));
 }
 
+// 1 - s for s = 1 / (1 + e): the subtraction would lose the digits of a gate that is nearly open, whose rest is e s (and e may be infinite where s is small)
+__device__ __forceinline__ float rest_of(float s, float e) { return s < 0.5f ? 1.0f - s : e * s; }
+
 // max(v, 0) + log(1 + e) with e = exp(-|v|): log(1 + e) = 2 artanh(q) with q = e / (2 + e) <= 1/3, whose
 // series q (2 + 2/3 q^2 + 2/5 q^4 + ...) is below 2^-24 of its sum after eight terms.  No digit of a
 // small e is lost, as it would be in 1 + e.

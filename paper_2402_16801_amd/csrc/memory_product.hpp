@@ -48,14 +48,14 @@ template <int ACT> __device__ __forceinline__ float slope_of(float p)
     if (ACT == CRAFTAX_ACT_RELU) return p > 0.0f ? 1.0f : (p <= 0.0f ? 0.0f : p);
     p = p > END ? END : (p < -END ? -END : p);
     if (ACT == CRAFTAX_ACT_SILU) {
-        const float g = sigmoid(p);
-        return g * __builtin_fmaf(p, 1.0f - g, 1.0f);
+        const float e = exp2_fast(-p * LOG2E), g = __builtin_amdgcn_rcpf(1.0f + e);
+        return g * __builtin_fmaf(p, rest_of(g, e), 1.0f);
     }
     if (ACT == CRAFTAX_ACT_GELU_TANH) {
         const float square = p * p;
         const float e = exp2_fast(p * __builtin_fmaf(square, -GELU_2K * GELU_C * LOG2E, -GELU_2K * LOG2E));
         const float g = __builtin_amdgcn_rcpf(1.0f + e);
-        return g * __builtin_fmaf(1.0f - g, p * __builtin_fmaf(square, 3.0f * GELU_C * GELU_2K, GELU_2K), 1.0f);
+        return g * __builtin_fmaf(rest_of(g, e), p * __builtin_fmaf(square, 3.0f * GELU_C * GELU_2K, GELU_2K), 1.0f);
     }
     return 1.0f;
 }

@@ -69,13 +69,25 @@ template <int V> __device__ __forceinline__ void load_rates(const float* rate, i
     for (int j = 0; j < V; ++j) v[j] = q.v[j] < -3.0e38f ? -3.0e38f : q.v[j];
 }
 
+// A sigmoid with all digits of what it leaves of 1, in one register: itself below 1/2, else its rest with a minus sign (-0 is a gate that is open).
+struct Folded {
+    float v;
+    __device__ __forceinline__ static float of(float s, float e) { return s < 0.5f ? s : -(e * s); }
+    __device__ __forceinline__ explicit Folded(float folded) : v(folded) {}
+    __device__ __forceinline__ bool open() const { return (int)__float_as_uint(v) < 0; }
+    __device__ __forceinline__ float other() const { return 1.0f - __builtin_fabsf(v); }
+    __device__ __forceinline__ float sigmoid() const { return open() ? other() : v; }
+    __device__ __forceinline__ float rest() const { return open() ? -v : other(); }
+};
+
 // The gate of one step: a = exp(rate s), and 1 - a a without the digits that the subtraction would lose where a is near 1:
 // 1 - exp(-t) = t (1 - t / 2 + t^2 / 6 - ..) is below 2^-22 of its sum after eight terms for t < 1/2.
 struct Gate {
-    float s, a, rest;        // rest = 1 - a a, 0 where that is negative (rates above 0)
+    float e, s, a, rest;     // s = 1 / (1 + e), rest = 1 - a a, 0 where that is negative (rates above 0)
     __device__ __forceinline__ Gate(float decay, float rate)
     {
-        s = sigmoid(decay);
+        e = exp2_fast(-decay * LOG2E);
+        s = __builtin_amdgcn_rcpf(1.0f + e);
         const float l = rate * s, t = -2.0f * l;
         a = exp2_fast(l * LOG2E);
         float r = -1.0f / 40320.0f;
@@ -392,19 +404,24 @@ __global__ __launch_bounds__(SPLIT ? REC_GROUP * WAVE : REC_THREADS) void k_recu
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const Gate gate(vd[j], rate[j]);
-                        s[k][j] = gate.s;
+                        s[k][j] = Folded::of(gate.s, gate.e);
                         a[k][j] = gate.a;
                         rest[k][j] = gate.rest;
                         if (MODE != PARTS) {
-                            q[k][j] = sigmoid(vi[j]);
+                            const float eq = exp2_fast(-vi[j] * LOG2E), vq = __builtin_amdgcn_rcpf(1.0f + eq);
+                            q[k][j] = Folded::of(vq, eq);
                             before[k][j] = CUTS && first[k] ? 0.0f : h[j];
-                            h[j] = __builtin_fmaf(gate.a, before[k][j], __builtin_amdgcn_sqrtf(gate.rest) * q[k][j] * vx[j]);
+                            h[j] = __builtin_fmaf(gate.a, before[k][j], __builtin_amdgcn_sqrtf(gate.rest) * vq * vx[j]);
                         }
                         if (GATE) {
                             const float sg = sigmoid(vz[j]), open = vz[j] * sg;
                             if (MODE != PARTS) dz[j] = e[k][j] * h[j] * sg * __builtin_fmaf(vz[j], 1.0f - sg, 1.0f);
                             e[k][j] *= open;
                         }
+                    }
+                    if (MODE != PARTS) {               // folded here: kept as two numbers each they cost 15 registers more
+                        pin(s[k]);
+                        pin(q[k]);
                     }
                     if (MODE != PARTS && GATE && k < count) put<E, V>(p.dz.at(t + k, i) + w.c, w, shrink<E, V>(dz));
                 }
@@ -421,12 +438,14 @@ __global__ __launch_bounds__(SPLIT ? REC_GROUP * WAVE : REC_THREADS) void k_recu
                         if (MODE != PARTS) {
                             const float root = rest[k][j] < 0x1p-126f ? 0.0f : __builtin_amdgcn_rsqf(rest[k][j]);
                             const float m = rest[k][j] * root, gm = G * m;
-                            dx[j] = gm * q[k][j];
-                            di[j] = dx[j] * vx[j] * (1.0f - q[k][j]);
-                            const float dl = G * a[k][j] * __builtin_fmaf(-q[k][j] * vx[j], a[k][j] * root, before[k][j]);
-                            const float ds = dl * s[k][j];
+                            const Folded fs(s[k][j]), fq(q[k][j]);
+                            const float vq = fq.sigmoid();
+                            dx[j] = gm * vq;
+                            di[j] = dx[j] * vx[j] * fq.rest();
+                            const float dl = G * a[k][j] * __builtin_fmaf(-vq * vx[j], a[k][j] * root, before[k][j]);
+                            const float ds = dl * fs.sigmoid();
                             spans[j] += ds;
-                            dd[j] = ds * rate[j] * (1.0f - s[k][j]);
+                            dd[j] = ds * rate[j] * fs.rest();
                         } else {
                             keep[j] = first[k] || keep[j] < 0.0f ? -1.0f : keep[j] * a[k][j];
                         }

@@ -111,3 +111,42 @@ def test_projection_beyond_the_range_of_float16(mem, act):
     g = mem.projection_backward(torch.ones(40, 24, device="cuda"), x, w, torch.zeros(24, device="cuda"), pre=pre, act=act, float_weight=True)
     assert bool((g.x[1::2] == 1200.0).all()) and bool((g.x[::2] == 0.0).all())
     assert bool((g.weight == 1000.0).all()) and bool((g.bias == 20.0).all())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+def test_slopes_keep_their_digits(mem, act):
+    """A slope is a product of at most eight factors and sums of size 1.2 or less, each rounded once to 2^-24, and an exponential whose argument, at most
+    3 where it counts for that much, is rounded to 2^-23: 2^-20 in all."""
+    pre = torch.linspace(-20.0, 20.0, 40001).double().float()
+    given = pre.double().requires_grad_(True)
+    (want,) = torch.autograd.grad(ref.act(given, act).sum(), given)
+    g = mem.projection_backward(torch.ones(1, 40001, device="cuda"), torch.ones(1, 1, device="cuda"), torch.ones(40001, 1, device="cuda"),
+                                torch.zeros(40001, device="cuda"), pre=pre.cuda()[None], act=act, want_x=False)
+    off = (g.bias.cpu().double() - want).abs()
+    assert float(off.max()) <= 2.0 ** -20, (float(off.max()), float(pre[off.argmax()]))
+
+
+# ---- gates that are nearly open -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,n,D", [(1, 3, 64), (300, 2, 64), (3, 5000, 64)])
+def test_recurrence_gradients_of_gates_that_are_nearly_open(mem, dtype, T, n, D):
+    """Gates of 10 to 25, value by value.  Every step begins an episode, so that a gradient is a product: dintake = dy m x q (1 - q), ddecay = -dy q x a a / m
+    rate s (1 - s).  1 - q is an exponential whose argument, up to 36 in units of the base's, is rounded to 2^-19 and has a constant right to 2^-25 of it:
+    2.1e-6.  Some 16 factors and roundings of 2^-23 are 1.9e-6, together below 2^-17."""
+    src = Source(T + n, TYPES[dtype])
+    decay, intake = (10.0 + 15.0 * torch.rand(T, n, D, generator=src.gen) for _ in range(2))
+    decay, intake = decay.to(TYPES[dtype]).double(), intake.to(TYPES[dtype]).double()
+    x, dy = (src.seq(T, n, D).abs().clamp(min=0.1).to(TYPES[dtype]).double() for _ in range(2))
+    rate = (-torch.exp(src.normal(D) - 1.0)).float().double()
+    args = [src.gpu(x), src.gpu(decay), src.gpu(intake), plain(rate)]
+    first = torch.ones(T, n, dtype=torch.uint8, device="cuda")
+    _, _, saved = mem.gated_recurrence(*args, first=first, save=True)
+    g = mem.gated_recurrence_backward(src.gpu(dy), saved, *args, first=first)
+    s, q = torch.sigmoid(decay), torch.sigmoid(intake)
+    log_a = rate * s
+    m = torch.sqrt(-torch.expm1(2 * log_a))
+    allowed = 2.0 ** -17 + (ROUND[TYPES[dtype]] * (1 + 2.0 ** -8) if dtype != "f32" else 0.0)
+    relative("gradient of intake", g.intake, dy * m * x * q * torch.sigmoid(-intake), allowed)
+    relative("gradient of decay", g.decay, -dy * q * x * torch.exp(2 * log_a) / m * rate * s * torch.sigmoid(-decay), allowed)
+    relative("gradient of x", g.x, dy * m * q, allowed)
