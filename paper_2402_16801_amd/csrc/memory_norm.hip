@@ -66,7 +66,7 @@ __device__ __forceinline__ float gate_value(float g, int act)
 }
 __device__ __forceinline__ float gate_slope(float g, int act)
 {
-    const float s = sigmoid(g), t = 1.0f - s, of_sigmoid = s * t, of_silu = s * __builtin_fmaf(g, t, 1.0f);
+    const float e = exp2_fast(-g * LOG2E), s = __builtin_amdgcn_rcpf(1.0f + e), t = rest_of(s, e), of_sigmoid = s * t, of_silu = s * __builtin_fmaf(g, t, 1.0f);
     const float v = act == CRAFTAX_GATE_SILU ? of_silu : of_sigmoid;
     return act == CRAFTAX_GATE_LINEAR ? 1.0f : v;
 }

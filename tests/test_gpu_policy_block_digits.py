@@ -150,3 +150,16 @@ def test_recurrence_gradients_of_gates_that_are_nearly_open(mem, dtype, T, n, D)
     relative("gradient of intake", g.intake, dy * m * x * q * torch.sigmoid(-intake), allowed)
     relative("gradient of decay", g.decay, -dy * q * x * torch.exp(2 * log_a) / m * rate * s * torch.sigmoid(-decay), allowed)
     relative("gradient of x", g.x, dy * m * q, allowed)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+def test_norm_gradients_of_gates_that_are_nearly_open(mem, dtype, act):
+    """As for the recurrence's gates.  Without a norm after the block and with du = 0 the gradient of the gate is dout y act'(gate)."""
+    src = Source(7, TYPES[dtype])
+    gate = (10.0 + 15.0 * torch.rand(5, 9, 200, generator=src.gen)).to(TYPES[dtype]).double()
+    y, dout = (src.seq(5, 9, 200).abs().clamp(min=0.1).to(TYPES[dtype]).double() for _ in range(2))
+    g = mem.residual_norm_backward(src.gpu(dout), torch.zeros(5, 9, 200, dtype=TYPES[dtype], device="cuda"), src.gpu(y), src.gpu(y), gate=src.gpu(gate), gate_act=act)
+    rest = torch.sigmoid(-gate)
+    slope = torch.sigmoid(gate) * (rest if act == "sigmoid" else 1 + gate * rest)
+    relative("gradient of gate", g.gate, dout * y * slope, 2.0 ** -17 + (ROUND[TYPES[dtype]] * (1 + 2.0 ** -8) if dtype != "f32" else 0.0))
