@@ -544,7 +544,7 @@ int craftax_gated_recurrence_backward(const craftax_recurrence_args *args, void 
  * Backward: dp = dout * act'(pre), dx = dp * weight, dweight = dp^T * x, dbias = the sum of dp (the gradient of residual is dout).  The
  * products take dp rounded to dtype (float16 beside a float32 dout: times a power of two that brings its largest value below 2^15, taken back from
  * their sums), the sum of dbias does not.  Sums are in 32 bits.  float32 values go through the matrix units as three
- * bfloat16 parts, which hold all of their digits down to 2^-110, and an absolute 2^-126 below. */
+ * bfloat16 parts, which hold all of their digits down to 2^-110, and an absolute 2^-133 below. */
 enum { CRAFTAX_ACT_NONE = 0, CRAFTAX_ACT_RELU = 1, CRAFTAX_ACT_SILU = 2, CRAFTAX_ACT_GELU_TANH = 3 };
 typedef struct craftax_projection_args {
     uint32_t dtype;             /* of x, weight, pre and dx */

@@ -153,6 +153,7 @@ template <typename E, typename R> struct Finish {
 // ---- operands of the matrix instructions --------------------------------------------------------------
 // A fragment is 16 rows by 64 bytes along k: lane l holds 16 bytes of row l % 16, from byte 16 (l / 16) on.
 typedef float F4 __attribute__((ext_vector_type(4)));
+typedef __bf16 BF2 __attribute__((ext_vector_type(2)));
 typedef __bf16 BF8 __attribute__((ext_vector_type(8)));
 typedef _Float16 H8 __attribute__((ext_vector_type(8)));
 typedef short S4 __attribute__((ext_vector_type(4)));

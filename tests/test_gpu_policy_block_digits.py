@@ -163,3 +163,49 @@ def test_norm_gradients_of_gates_that_are_nearly_open(mem, dtype, act):
     rest = torch.sigmoid(-gate)
     slope = torch.sigmoid(gate) * (rest if act == "sigmoid" else 1 + gate * rest)
     relative("gradient of gate", g.gate, dout * y * slope, 2.0 ** -17 + (ROUND[TYPES[dtype]] * (1 + 2.0 ** -8) if dtype != "f32" else 0.0))
+
+
+# ---- parts of float32 values -------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("shift", [0, -110, -120, 100])
+def test_projection_of_float32_by_value(mem, shift):
+    """Sums of one product, by tiles: every value right to 2^-22 of itself, whatever its last digits.  What the three parts leave out of a product is
+    below 2^-24 + 2^-34 of it, an addition of the matrix units may cut off 2^-23, and the smaller products' additions add 2^-30 each.  Values from 2^-110
+    on have all of their digits in three parts; smaller ones lose half a step of bfloat16's smallest numbers, 2^-134."""
+    src = Source(3, torch.float32)
+    allowed = 2.0 ** -22 + (2.0 ** (-134 - shift) if shift < -110 else 0.0)
+    bits = torch.tensor([0x3F80FFFF, 0x3FFFFFFF, 0x3F807FFF, 0x3F808000, 0x3F80FF80, 0x3F80807F, 0x3F807F7F, 0x3F808080, 0x3F800001, 0x3FFF7FFF, 0x3FFF8000, 0x3FFF8001],
+                        dtype=torch.int32).view(torch.float32).double()
+
+    def some(count):
+        v = torch.cat([bits, 1.0 + torch.rand(count, generator=src.gen, dtype=torch.float64) / 128, 1.0 + torch.rand(count, generator=src.gen, dtype=torch.float64)])
+        return v[torch.randperm(len(v), generator=src.gen)[:count]].float().double() * (1 - 2 * torch.randint(0, 2, (count,), generator=src.gen))
+
+    x, w = some(700) * 2.0 ** shift, some(400) * 2.0 ** -shift
+    x[:12], w[:12] = bits * 2.0 ** shift, bits * 2.0 ** -shift
+    out, _ = mem.projection(plain(x)[:, None], plain(w)[:, None])
+    relative("out", out, x[:, None] * w[None], allowed)
+    # a sum over rows that begins anywhere: the other values are 0
+    for k in (0, 5, 69):
+        wide, other = torch.zeros(700, 70, dtype=torch.float64), torch.zeros(400, 70, dtype=torch.float64)
+        wide[:, k], other[:, k] = x, w
+        out, _ = mem.projection(plain(wide), plain(other))
+        relative("out", out, x[:, None] * w[None], allowed)
+    d = torch.zeros(90, 400, dtype=torch.float64)
+    d[17] = w
+    wide = torch.zeros(90, 700, dtype=torch.float64)
+    wide[17] = x
+    g = mem.projection_backward(plain(d), plain(wide), torch.zeros(400, 700, device="cuda"), want_x=False)
+    relative("gradient of weight", g.weight, w[:, None] * x[None], allowed)
+
+
+def test_projection_of_float32_next_to_the_largest_number(mem):
+    """Numbers that bfloat16 would round to infinity."""
+    most = torch.finfo(torch.float32).max
+    x = torch.ones(700, 40, dtype=torch.float64)
+    w = torch.ones(400, 40, dtype=torch.float64)
+    x[5], x[6] = 0.0, 0.0
+    x[5, 3], x[6, 39] = most, -most
+    w[:, 3] = w[:, 39] = 2.0 ** -20
+    out, _ = mem.projection(plain(x), plain(w))
+    relative("out", out, x @ w.t(), 2.0 ** -20)
