@@ -562,9 +562,15 @@ static RecCut rec_cut(const craftax_recurrence_args* a, bool backward)
     return c;
 }
 
+// sizes that the calls take: of others no size is told, whose products might not fit one
+static bool rec_shape_ok(const craftax_recurrence_args* a)
+{
+    return a && a->dtype <= CRAFTAX_F16 && a->steps >= 1 && a->n >= 1 && a->channels >= 1 && a->steps <= MOST_COUNT && (int64_t)a->n * a->channels <= MOST_COUNT;
+}
+
 size_t recurrence_saved_bytes(const craftax_recurrence_args* a)
 {
-    if (!a || a->steps < 1 || a->n < 1 || a->channels < 1) return 0;
+    if (!rec_shape_ok(a)) return 0;
     return round256((size_t)ceil_div(a->steps, REC_SPAN) * a->n * a->channels * sizeof(float));
 }
 
@@ -574,7 +580,7 @@ static size_t rec_sums_bytes(const craftax_recurrence_args* a, const RecCut& c)
 }
 size_t recurrence_workspace_bytes(const craftax_recurrence_args* a, bool backward)
 {
-    if (!a || a->steps < 1 || a->n < 1 || a->channels < 1 || a->steps > MOST_COUNT || (int64_t)a->n * a->channels > MOST_COUNT) return 0;
+    if (!rec_shape_ok(a)) return 0;
     const RecCut c = rec_cut(a, backward);
     size_t bytes = rec_sums_bytes(a, c);
     if (backward && a->drate) bytes += round256((size_t)c.row_blocks(a->n, true) * a->channels * sizeof(float));
