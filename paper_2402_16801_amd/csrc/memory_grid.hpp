@@ -19,6 +19,14 @@ inline Spread spread(int64_t blocks, int threads)
     return {(unsigned)x, (unsigned)z};
 }
 
+// Blocks over `tiles` tiles, of a kernel whose blocks go on to the tile as many behind as there are blocks: one a tile, and of very many tiles as many
+// as one dimension of a launch has threads for, so that the tiles' dies stay those of their blocks (the number is a multiple of eight, or all tiles).
+inline unsigned blocks_in_turn(int64_t tiles)
+{
+    constexpr int64_t MOST = (int64_t)1 << 21;
+    return (unsigned)(tiles < MOST ? tiles : MOST);
+}
+
 // Environments that are taken side by side by kernels whose threads go on by that many: `want` or all of them, and so few that what is
 // behind the last one still has a number.
 inline int side_by_side(int64_t want, int n)

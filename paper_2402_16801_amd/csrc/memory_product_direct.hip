@@ -278,7 +278,7 @@ namespace host {
 template <bool INSIDE, typename E, typename R> void launch_direct(const ProductParams<E, R>& p, int64_t tiles, bool large, hipStream_t st)
 {
     // large tiles fill a compute unit one at a time: blocks go on to further ones
-    const unsigned blocks = (unsigned)(large && tiles > 256 ? 256 : tiles);
+    const unsigned blocks = large && tiles > 256 ? 256 : blocks_in_turn(tiles);
     auto go = [&](auto act) {
         constexpr int ACT = decltype(act)::value;
         if (large) hipLaunchKernelGGL((k_product_direct<E, R, ACT, INSIDE, 4, 8, 4, 2>), dim3(blocks), dim3(512), 0, st, p);

@@ -81,3 +81,15 @@ def test_recurrence_of_one_channel_and_more_environments_than_blocks_are_for(mem
     got = mem.gated_recurrence_backward(src.gpu(dy), saved, *args, dstate=plain(dstate), **how)
     for name, value in got._asdict().items():
         close("gradient of " + name, value, want[name], T * n if name == "rate" else T)
+
+
+def test_projection_of_more_tiles_than_blocks_are_launched(mem):
+    """2,097,199 tiles of 128 x 128, 2^21 blocks: the first ones go on to a second tile.  Whole numbers, every value checked."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rows, I, O = (2 ** 21 + 47) * 128 - 37, 8, 72
+    x = torch.randint(-2, 3, (rows, I), generator=gen, device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    w, b = _whole(gen, 2, O, I), _whole(gen, 9, O)
+    out, _ = mem.projection(x, w.to(torch.bfloat16), b.float(), act="relu")
+    for at in range(0, rows, 2 ** 24):
+        want = torch.relu(x[at:at + 2 ** 24].float() @ w.float().t() + b.float())
+        assert torch.equal(out[at:at + 2 ** 24].float(), want), at
