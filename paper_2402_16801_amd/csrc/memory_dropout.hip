@@ -12,13 +12,15 @@
 #include "memory_api.hpp"
 #include "memory_common.hpp"
 
+#include <type_traits>
+
 namespace mem {
 
 constexpr int DROP_THREADS = 256, DROP_V = 8;
 
-template <typename E, typename R, typename O> struct DropParams {
+template <typename E, typename O> struct DropParams {
     Seq<const E> x;
-    Seq<const R> residual;
+    Seq<const O> residual;
     Seq<O> out;
     uint32_t key0, key1, limit, env;
     uint64_t step;
@@ -42,8 +44,8 @@ template <typename P> __device__ __forceinline__ void drop_load(const P* p, int 
     }
 }
 
-template <typename E, typename R, typename O>
-__global__ __launch_bounds__(DROP_THREADS) void k_dropout(const DropParams<E, R, O> p)
+template <typename E, typename O>
+__global__ __launch_bounds__(DROP_THREADS) void k_dropout(const DropParams<E, O> p)
 {
     const int64_t at = spread_block(p.wide) * DROP_THREADS + threadIdx.x;
     if (at >= p.items) return;
@@ -99,7 +101,7 @@ int dropout(const craftax_dropout_args* a, void* stream, const char** why)
         using E = decltype(e);
         auto launch = [&](auto o) {
             using O = decltype(o);
-            DropParams<E, O, O> p{};
+            DropParams<E, O> p{};
             p.x = seq_in<E>(a->x); p.residual = seq_in<O>(a->residual); p.out = seq<O>(a->out);
             p.key0 = (uint32_t)a->seed; p.key1 = (uint32_t)(a->seed >> 32);
             p.limit = limit; p.env = (uint32_t)a->env; p.step = (uint64_t)a->step; p.step_at = a->step_at;
@@ -107,12 +109,15 @@ int dropout(const craftax_dropout_args* a, void* stream, const char** why)
             p.items = items; p.vectors = (uint32_t)vectors; p.n = (uint32_t)a->n; p.channels = a->channels;
             const Spread grid = spread(ceil_div(items, DROP_THREADS), DROP_THREADS);
             p.wide = grid.x;
-            hipLaunchKernelGGL((k_dropout<E, O, O>), dim3(grid.x, 1, grid.z), dim3(DROP_THREADS), 0, (hipStream_t)stream, p);
+            hipLaunchKernelGGL((k_dropout<E, O>), dim3(grid.x, 1, grid.z), dim3(DROP_THREADS), 0, (hipStream_t)stream, p);
         };
-        if (a->out_dtype == a->dtype) launch(E{});
-        else if (a->out_dtype == CRAFTAX_F32) launch(float{});
-        else if (a->out_dtype == CRAFTAX_BF16) launch(__bf16{});
-        else launch(_Float16{});
+        if (a->out_dtype == a->dtype) return launch(E{});
+        if constexpr (std::is_same_v<E, float>) {
+            if (a->out_dtype == CRAFTAX_BF16) launch(__bf16{});
+            else launch(_Float16{});
+        } else {
+            launch(float{});
+        }
     });
     return launched(why);
 }

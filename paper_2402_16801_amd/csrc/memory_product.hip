@@ -504,7 +504,6 @@ __device__ __forceinline__ float power_for(float most, float& back)
 template <typename E, typename R, int ACT, Edge EDGE>
 __global__ __launch_bounds__(256) void k_slope(const SlopeParams<E, R> p)
 {
-    constexpr int GO = 1;              // rows under way together (two or four were no faster)
     __shared__ float sums[SLOPE_V][256];
     const int across = 1 << p.across, x = threadIdx.x & (across - 1), y = threadIdx.x >> p.across, c = ((int)blockIdx.x * across + x) * SLOPE_V, count = p.n - c;
     float total[SLOPE_V] = {}, scale = 1.0f;
@@ -518,39 +517,30 @@ __global__ __launch_bounds__(256) void k_slope(const SlopeParams<E, R> p)
     }
     if (count > 0) {
         const uint32_t rows = 256u >> p.across, step = gridDim.y * rows, last = p.m - 1;
-        struct Raw { Pack<R, SLOPE_V> d; Pack<E, SLOPE_V> v; } raw[GO];
+        struct Raw { Pack<R, SLOPE_V> d; Pack<E, SLOPE_V> v; } raw;       // one row under way (two or four were no faster)
         auto load = [&](uint32_t row, Raw& q) {
             const uint32_t m = row < last ? row : last;
             slope_take<EDGE>(p.dout + p.dout_rows.at(m) + c, count, q.d);
             if (ACT != CRAFTAX_ACT_NONE) slope_take<EDGE>(p.pre + p.pre_rows.at(m) + c, count, q.v);
         };
         uint32_t m = blockIdx.y * rows + y;
+        load(m, raw);
+        for (; m < p.m; m += step) {
+            float d[SLOPE_V];
 #pragma unroll
-        for (int g = 0; g < GO; ++g) load(m + g * step, raw[g]);
-        for (; m < p.m; m += GO * step) {
-            float d[GO][SLOPE_V];
-#pragma unroll
-            for (int g = 0; g < GO; ++g)
-#pragma unroll
-                for (int j = 0; j < SLOPE_V; ++j) {
-                    d[g][j] = Elem<R>::up(raw[g].d.v[j]);
-                    if (ACT != CRAFTAX_ACT_NONE) d[g][j] *= slope_of<ACT>(Elem<E>::up(raw[g].v.v[j]));
-                    if (EDGE == VALUES && j >= count) d[g][j] = 0.0f;         // rows of dp are filled up to a multiple of eight
-                }
-            // the next rows are under way in front of the stores: behind them the wait for the rows would be for those too
-#pragma unroll
-            for (int g = 0; g < GO; ++g) load(m + (GO + g) * step, raw[g]);
-#pragma unroll
-            for (int g = 0; g < GO; ++g) {
-                const uint32_t row = m + g * step;
-                if (row >= p.m) continue;
-#pragma unroll
-                for (int j = 0; j < SLOPE_V; ++j) {
-                    total[j] += d[g][j];
-                    if (SCALED) d[g][j] *= scale;
-                }
-                if (p.dp) Finish<E, R>::template store<E, SLOPE_V>(p.dp + (int64_t)row * p.dp_row + c, SLOPE_V, d[g]);
+            for (int j = 0; j < SLOPE_V; ++j) {
+                d[j] = Elem<R>::up(raw.d.v[j]);
+                if (ACT != CRAFTAX_ACT_NONE) d[j] *= slope_of<ACT>(Elem<E>::up(raw.v.v[j]));
+                if (EDGE == VALUES && j >= count) d[j] = 0.0f;         // rows of dp are filled up to a multiple of eight
             }
+            // the next row is under way in front of the stores: behind them the wait for it would be for those too
+            load(m + step, raw);
+#pragma unroll
+            for (int j = 0; j < SLOPE_V; ++j) {
+                total[j] += d[j];
+                if (SCALED) d[j] *= scale;
+            }
+            if (p.dp) Finish<E, R>::template store<E, SLOPE_V>(p.dp + (int64_t)m * p.dp_row + c, SLOPE_V, d);
         }
     }
     if (!p.part) return;

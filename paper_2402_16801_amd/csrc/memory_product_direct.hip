@@ -12,8 +12,8 @@
 
 namespace mem {
 
-// What lies behind the end of the sums or of the columns comes from here.
-static __device__ const uint32_t g_zeros[4] = {0, 0, 0, 0};
+// What lies behind the end of the sums or of the columns comes from here, 16 bytes at a time.
+alignas(16) static __device__ const uint32_t g_zeros[4] = {0, 0, 0, 0};
 
 // Fragment f of P, with k inside, stands for rows 32 (f / 2) + 8 (i / 4) + 4 (f % 2) + i % 4, so that a lane holds eight columns in a row of two
 // fragments.
