@@ -86,6 +86,34 @@ def test_projection_of_float16_keeps_infinite_gradients_in_their_rows(mem, case)
     assert all(bool((v == 0).all()) for v in g)
 
 
+def test_projection_of_float16_finds_the_size_of_its_gradients_at_every_replay(mem):
+    """Captured once, replayed with gradients of other sizes in the same tensor, on a side stream beside eager calls: bit for bit as eager."""
+    src = Source(5, torch.float16)
+    x, w, pre = src.gpu(src.normal(3000, 72, dtype=torch.float16)), src.gpu(src.normal(136, 72, dtype=torch.float16)), src.gpu(src.normal(3000, 136, dtype=torch.float16))
+    douts = [plain(src.normal(3000, 136) * size) for size in (1.0, 2.0 ** -40, 2.0 ** 30, 0.0, 2.0 ** -20)]
+    bias = torch.zeros(136, device="cuda")
+
+    def back(dout):
+        return mem.projection_backward(dout, x, w, bias, pre=pre, act="silu", float_weight=True)
+
+    want = [[v.clone() for v in back(d)] for d in douts]
+    given, side, graph = douts[0].clone(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        back(given)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        got = back(given)
+    for turn in range(2):
+        for d, exp in zip(douts, want):
+            given.copy_(d)
+            graph.replay()
+            eager = back(douts[turn + 1])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, exp))
+            assert all(torch.equal(a, b) for a, b in zip(eager, want[turn + 1]))
+
+
 # ---- activations beyond the range of their type ---------------------------------------------------------------------
 
 def test_slopes_of_infinite_arguments_are_0_and_1(mem):
