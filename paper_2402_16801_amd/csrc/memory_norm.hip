@@ -13,7 +13,7 @@
 // Blocks go on to further rows with the weights, and in the backward pass their gradients, in registers.
 // 262,144 rows of 512 values in bfloat16 with a gate: forward 250 us, 5.3 TB/s; backward 500 us, 4.3 TB/s, with vector issue
 // at about half beside it (131,072 rows in float32: 258 us, 5.2 TB/s, and 418, 5.1).  Beyond 4,096 values the backward pass has no room for a
-// row's eight arrays: 112 to 276 bytes of scratch a lane (16,384 rows of 8,192 bfloat16: 640 us, 3.4 TB/s).
+// row's eight arrays: 128 to 276 bytes of scratch a lane (16,384 rows of 8,192 bfloat16: 730 us, 2.9 TB/s).
 #include "memory_api.hpp"
 #include "memory_common.hpp"
 
@@ -64,9 +64,11 @@ __device__ __forceinline__ float gate_value(float g, int act)
     const float v = act == CRAFTAX_GATE_SILU ? both : s;
     return act == CRAFTAX_GATE_LINEAR ? g : v;
 }
-__device__ __forceinline__ float gate_slope(float g, int act)
+// FULL: the registers are all taken.  The exponential is not kept beside the sigmoid through the sums of the row then, and what that leaves of 1 is a sigmoid,
+// too (16,384 rows of 8,192 bfloat16 values 733 us, of 6,000 float16 values 641; with the exponential kept 829 and 819.  65,536 rows of 1,000: 234, and 233).
+template <bool FULL> __device__ __forceinline__ float gate_slope(float g, int act)
 {
-    const float e = exp2_fast(-g * LOG2E), s = __builtin_amdgcn_rcpf(1.0f + e), t = rest_of(s, e), of_sigmoid = s * t, of_silu = s * __builtin_fmaf(g, t, 1.0f);
+    const float e = exp2_fast(-g * LOG2E), s = __builtin_amdgcn_rcpf(1.0f + e), t = FULL ? sigmoid(-g) : rest_of(s, e), of_sigmoid = s * t, of_silu = s * __builtin_fmaf(g, t, 1.0f);
     const float v = act == CRAFTAX_GATE_SILU ? of_silu : of_sigmoid;
     return act == CRAFTAX_GATE_LINEAR ? 1.0f : v;
 }
@@ -364,7 +366,7 @@ __global__ __launch_bounds__(RowBlock<W>::THREADS) void k_norm_backward(const No
                 const float value = gate_value(g[c][j], p.gate_act), act = gated ? value : 1.0f;
                 const float v = y[c][j] * w1[c][j], dv = d * scale[c][j] * act;
                 add(d * v, act, ds[c][j]);
-                g[c][j] = d * v * scale[c][j] * gate_slope(g[c][j], p.gate_act);
+                g[c][j] = d * v * scale[c][j] * gate_slope<(CHUNKS * V > 8)>(g[c][j], p.gate_act);
                 add(dv, y[c][j], d1[c][j]);
                 du[c][j] = dv * w1[c][j];
                 q = w.add(c, j, du[c][j], y[c][j], q, before);

@@ -182,12 +182,13 @@ def test_recurrence_gradients_of_gates_that_are_nearly_open(mem, dtype, T, n, D)
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["sigmoid", "silu"])
-def test_norm_gradients_of_gates_that_are_nearly_open(mem, dtype, act):
-    """As for the recurrence's gates.  Without a norm after the block and with du = 0 the gradient of the gate is dout y act'(gate)."""
+@pytest.mark.parametrize("D", [200, 5000])
+def test_norm_gradients_of_gates_that_are_nearly_open(mem, dtype, act, D):
+    """As for the recurrence's gates, in rows that registers hold and in long ones.  Without a norm after the block and with du = 0 the gradient of the gate is dout y act'(gate)."""
     src = Source(7, TYPES[dtype])
-    gate = (10.0 + 15.0 * torch.rand(5, 9, 200, generator=src.gen)).to(TYPES[dtype]).double()
-    y, dout = (src.seq(5, 9, 200).abs().clamp(min=0.1).to(TYPES[dtype]).double() for _ in range(2))
-    g = mem.residual_norm_backward(src.gpu(dout), torch.zeros(5, 9, 200, dtype=TYPES[dtype], device="cuda"), src.gpu(y), src.gpu(y), gate=src.gpu(gate), gate_act=act)
+    gate = (10.0 + 15.0 * torch.rand(5, 9, D, generator=src.gen)).to(TYPES[dtype]).double()
+    y, dout = (src.seq(5, 9, D).abs().clamp(min=0.1).to(TYPES[dtype]).double() for _ in range(2))
+    g = mem.residual_norm_backward(src.gpu(dout), torch.zeros(5, 9, D, dtype=TYPES[dtype], device="cuda"), src.gpu(y), src.gpu(y), gate=src.gpu(gate), gate_act=act)
     rest = torch.sigmoid(-gate)
     slope = torch.sigmoid(gate) * (rest if act == "sigmoid" else 1 + gate * rest)
     relative("gradient of gate", g.gate, dout * y * slope, 2.0 ** -17 + (ROUND[TYPES[dtype]] * (1 + 2.0 ** -8) if dtype != "f32" else 0.0))
