@@ -616,7 +616,10 @@ static Plan plan(int64_t m, int64_t n, int64_t k, size_t elem, bool inside, bool
         c.n_tiles = (uint32_t)ceil_div(n, 16);
         return c;
     }
-    // A compute unit takes 0.4 times as long for a tile of 128 x 128 as for one of 256 x 256 (1,200 and 740 TFLOP/s for 8,192 squared, bfloat16).
+    // A compute unit is taken to need 0.4 times as long for a tile of 128 x 128 as for one of 256 x 256.  With many tiles the large ones are 1.1 to 1.4
+    // times as fast, short sums and heavy epilogues among them: bfloat16, tiles of 256 and of 128: 262,144 rows of 512 onto 1,024 337 and 459 us, with gelu
+    // and its argument kept 455 and 593; 65,536 rows of 1,024 onto 512 67 and 77; 256 onto 1,024 47 and 63; 8,192 squared 1,070 and 1,197.  Two rounds of
+    // large tiles for five of small ones are the rule's border and its worst case: 40,960 rows of 512 onto 512 37 and 33.
     const bool larger = 10 * ceil_div(tiles(256), CHIP_UNITS) <= 4 * ceil_div(tiles(128), CHIP_UNITS) || (!inside && tiled(m, n, k, elem, false, 256));
     if (direct) c.cut = larger ? Cut::DIRECT_LARGE : Cut::DIRECT;
     else c.cut = tiled(m, n, k, elem, inside) ? Cut::LARGE : Cut::SMALL;

@@ -1,11 +1,11 @@
 // Gated linear recurrence of every channel, one state each: whole sequences, single tokens and the backward pass.
 //
-//   s = sigmoid(decay), L = min(rate s, ..), a = exp(L), m = sqrt(1 - a a), h_t = a h_(t-1) + m sigmoid(intake) x,  y = h z sigmoid(z)
+//   s = sigmoid(decay), L = rate s, a = exp(L), m = sqrt(1 - a a), h_t = a h_(t-1) + m sigmoid(intake) x,  y = h z sigmoid(z)
 //
 // Bound by memory: 4 activations move per step and channel (5 with a gate), 7 in the backward pass (9), and a float of state every REC_SPAN steps
-// in each, beside some 40 and 100 vector instructions, 6 to 8 of them transcendental.  A thread owns V channels of one environment and walks
+// in each, beside some 40 and 115 vector instructions, 6 to 8 of them transcendental.  A thread owns V channels of one environment and walks
 // along the steps, states in registers; nothing is exchanged between lanes.  64 steps of 4,096 environments of 512 bfloat16 channels: 318 us
-// forward (1.50 GB, 4.7 TB/s), 640 backward (2.58 GB, 4.0 TB/s); a token of 65,536 x 512 113 us (5.2 TB/s).
+// forward (1.50 GB, 4.7 TB/s), 650 backward (2.58 GB, 4.0 TB/s, 179 registers, which leave room for two wavefronts per SIMD); a token of 65,536 x 512 113 us (5.2 TB/s).
 //
 // Few environments are split into parts along time: a first kernel finds what each part does to the state (a factor and a term), and each block
 // goes through the parts before its own.  That reads the inputs twice: 10,000 steps of one environment of 512 floats take 32 us in 625

@@ -191,13 +191,16 @@ def _act(name):
 def projection(x, weight, bias=None, *, residual=None, act="none", save=False):
     """(out, pre): pre = x weight^T + bias, out = residual + act(pre).  weight: [outputs][inputs], of the type of x, either dimension side by
     side; out has the type of residual (that of x or float32).  pre, of the type of x, is what a backward pass through an activation needs, None
-    without `save`."""
+    without `save`.  What this saves over torch.nn.functional.linear is what would follow it (the activation, its argument and the residual in one
+    pass) and, for float32, digits.  A bare product forward is as fast there or faster: in 16 bits 1.1 to 1.5 times, for rows of odd lengths 1.8 times, in
+    float32 only onto few columns or from few rows."""
     return _ready().projection(x, weight, bias, _act(act), residual, save)
 
 
 def projection_backward(dout, x, weight, bias=None, *, pre=None, act="none", want_x=True, want_weight=True, float_weight=False) -> ProjectionGrads:
     """Gradients for dout = dL/d(out), which is the gradient of residual, too; `pre` from the forward call, the rest as it was there.  The
-    gradient of weight has its type, or is float32 with `float_weight`."""
+    gradient of weight has its type, or is float32 with `float_weight`.  The products take dL/d(pre) rounded to the type of x, as PyTorch's backward pass of
+    an activation hands it on; float16 beside a float32 dout is scaled by a power of two on the way, so that its size does not matter."""
     return ProjectionGrads._make(_ready().projection_backward(x, weight, bias, _act(act), pre, dout, want_x, want_weight, float_weight))
 
 
@@ -369,7 +372,7 @@ def recurrence(x, decay, intake, rate, *, z=None, state=None, first=None, length
 
 def project(x, weight, bias=None, *, residual=None, act="none"):
     """projection, differentiable in every tensor.  weight may be float32 beside activations of 16 bits: it is rounded to their type where it is
-    used, and its gradient is float32."""
+    used, at every call (one that acts step by step keeps a rounded copy and calls projection), and its gradient is float32."""
     save = act != "none" and torch.is_grad_enabled() and any(isinstance(v, Tensor) and v.requires_grad for v in (x, weight, bias))
     return _Project.apply(x, weight, bias, residual, act, save)
 
