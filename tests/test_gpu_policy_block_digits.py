@@ -238,3 +238,28 @@ def test_projection_of_float32_next_to_the_largest_number(mem):
     w[:, 3] = w[:, 39] = 2.0 ** -20
     out, _ = mem.projection(plain(x), plain(w))
     relative("out", out, x @ w.t(), 2.0 ** -20)
+
+
+# ---- states that grow ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,n", [(2000, 1), (2000, 3), (300, 1), (40, 3000)])
+def test_recurrence_of_nothing_is_nothing_whatever_its_rate(mem, T, n):
+    """Rates above 0, where the root counts as 0: a state of 0 stays 0 however large the product of the factors becomes, and so does a gradient of 0.  One
+    that begins at 1e-30 grows alike in one walk and in parts, as long as it is a number (a sum of T logarithms of factors, each off by 2^-22: 2^-11 for T = 2,000)."""
+    src = Source(T, torch.float32)
+    D = 70
+    t = {k: src.normal(T, n, D) for k in ("x", "decay", "intake", "z")}
+    rate = torch.full((D,), 2.0)
+    rate[::2] = -2.0
+    args, z = [plain(t[k]) for k in ("x", "decay", "intake")] + [rate.cuda()], plain(t["z"])
+    y, h, saved = mem.gated_recurrence(*args, z=z, save=True)
+    assert bool(torch.isfinite(y).all()) and bool((y[..., 1::2] == 0).all()) and bool((h[:, 1::2] == 0).all()) and bool((h[:, ::2] != 0).all())
+    g = mem.gated_recurrence_backward(torch.zeros_like(y), saved, *args, z=z, state=torch.zeros_like(h), dstate=torch.zeros_like(h))
+    assert all(bool((v == 0).all()) for v in g)
+    state = torch.full((n, D), 1e-30, device="cuda")
+    y, h, _ = mem.gated_recurrence(*args, state=state)
+    log = torch.cumsum(2.0 * torch.sigmoid(t["decay"][..., 1::2]), 0)
+    want = 1e-30 * torch.exp(log)
+    number = want < 1e38
+    got = y[..., 1::2].cpu().double()
+    assert bool(((got / want - 1).abs()[number] <= 2.0 ** -11).all()) and bool(number.any(0).all())
