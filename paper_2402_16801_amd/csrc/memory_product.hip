@@ -456,7 +456,9 @@ template <Edge EDGE, typename P> __device__ __forceinline__ void slope_take(cons
 // The range of float16.  dp of a float32 gradient may be anything that float32 holds, and float16 ends at 65,504 and at 6e-8: dp is stored times a power of
 // two that brings its largest value to 2^14 .. 2^15, which both products take back from their sums (ACT_SCALED).  Values keep their eleven bits down to
 // 2^-29 of the largest, and an absolute 2^-40 of it below.  This pass finds the largest finite value of every block, k_slope that of all: it reads what
-// k_slope reads once more (262,144 rows of 1,024, without and with an activation: 190 and 290 us).
+// k_slope reads once more (262,144 rows of 1,024, without and with an activation: 190 and 290 us).  At most LARGEST_X blocks lie side by side on the columns,
+// since every block of k_slope goes over all of their values.
+constexpr unsigned LARGEST_X = 2048;
 __device__ __forceinline__ float block_largest(float most, float (&sums)[256])
 {
     sums[threadIdx.x] = most;
@@ -471,10 +473,12 @@ template <typename E, typename R, int ACT, Edge EDGE>
 __global__ __launch_bounds__(256) void k_largest(const SlopeParams<E, R> p)
 {
     __shared__ float sums[256];
-    const int across = 1 << p.across, x = threadIdx.x & (across - 1), y = threadIdx.x >> p.across, c = ((int)blockIdx.x * across + x) * SLOPE_V, count = p.n - c;
+    const int across = 1 << p.across, x = threadIdx.x & (across - 1), y = threadIdx.x >> p.across, pieces = (p.n - 1) / (across * SLOPE_V) + 1;
+    const uint32_t rows = 256u >> p.across, step = gridDim.y * rows;
     float most = 0.0f;
-    if (count > 0) {
-        const uint32_t rows = 256u >> p.across, step = gridDim.y * rows;
+    for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const int c = (piece * across + x) * SLOPE_V, count = p.n - c;
+        if (count <= 0) break;
         for (uint32_t m = blockIdx.y * rows + y; m < p.m; m += step) {
             Pack<R, SLOPE_V> d;
             Pack<E, SLOPE_V> v = {};
@@ -769,7 +773,7 @@ struct Project {
     int64_t weight_row, x_row, dp_row;   // of what lies in the workspace
     bool has_dp, scaled;     // dp lies in the workspace; times a power of two
     int slope_across;
-    unsigned slope_x, slope_y;
+    unsigned slope_x, slope_y, largest_x;
     size_t weight_at, x_at, dp_at, scale_at, sums_at, part_at, total;
 };
 // Where rows cannot go straight to LDS they are copied to where they can, if the product is worth it: reading and writing them takes as long as
@@ -821,7 +825,8 @@ static Project project(const craftax_projection_args* a, bool backward)
         int64_t y = ceil_div(c.rows, 256 >> c.slope_across), most = ceil_div(2048, c.slope_x);
         c.slope_y = (unsigned)(y < most ? y : most);
         c.scaled = c.has_dp && a->dtype == CRAFTAX_F16 && a->out_dtype == CRAFTAX_F32;
-        if (c.scaled) c.scale_at = take((1 + (size_t)c.slope_x * c.slope_y) * sizeof(float));
+        c.largest_x = c.slope_x < LARGEST_X ? c.slope_x : LARGEST_X;
+        if (c.scaled) c.scale_at = take((1 + (size_t)c.largest_x * c.slope_y) * sizeof(float));
         if (a->dbias) c.sums_at = take((size_t)c.slope_y * a->outputs * sizeof(float));
         size_t part = 0;
         if (a->dx.data) {
@@ -936,15 +941,15 @@ int projection_backward(const craftax_projection_args* given, void* stream, cons
             s.dout = static_cast<const R*>(a->dout.data); s.dout_rows = rows_of(a, a->dout);
             s.pre = a->act == CRAFTAX_ACT_NONE ? nullptr : static_cast<const E*>(a->pre.data); s.pre_rows = rows_of(a, a->pre);
             s.dp = own; s.dp_row = c.dp_row;
-            s.factor = factor; s.largest = factor ? factor + 1 : nullptr; s.blocks = (int)(c.slope_x * c.slope_y);
+            s.factor = factor; s.largest = factor ? factor + 1 : nullptr; s.blocks = (int)(c.largest_x * c.slope_y);
             s.part = a->dbias ? reinterpret_cast<float*>(work + c.sums_at) : nullptr;
             s.m = (uint32_t)c.rows; s.n = a->outputs; s.across = c.slope_across;
             auto slope = [&](auto act) {
                 constexpr int ACT = decltype(act)::value;
                 if constexpr (std::is_same_v<E, _Float16> && std::is_same_v<R, float>) {
                     if (factor) {
-                        if (s.n % SLOPE_V == 0) hipLaunchKernelGGL((k_largest<E, R, ACT, VECTORS>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
-                        else hipLaunchKernelGGL((k_largest<E, R, ACT, VALUES>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);
+                        if (s.n % SLOPE_V == 0) hipLaunchKernelGGL((k_largest<E, R, ACT, VECTORS>), dim3(c.largest_x, c.slope_y), dim3(256), 0, st, s);
+                        else hipLaunchKernelGGL((k_largest<E, R, ACT, VALUES>), dim3(c.largest_x, c.slope_y), dim3(256), 0, st, s);
                     }
                 }
                 if (s.n % SLOPE_V == 0) hipLaunchKernelGGL((k_slope<E, R, ACT, VECTORS>), dim3(c.slope_x, c.slope_y), dim3(256), 0, st, s);

@@ -86,6 +86,19 @@ def test_projection_of_float16_keeps_infinite_gradients_in_their_rows(mem, case)
     assert all(bool((v == 0).all()) for v in g)
 
 
+@pytest.mark.parametrize("O", [2200001, 1100000])
+def test_projection_of_float16_finds_the_size_of_its_gradients_in_many_columns(mem, O):
+    """More columns than blocks lie side by side for: the largest value is in the last ones, and scaled as if it were not it would be infinite."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, w = (torch.randint(-2, 3, shape, generator=gen, device="cuda").half() for shape in ((3, 8), (O, 8)))
+    dout = torch.zeros(3, O, device="cuda")
+    dout[:, :5] = 2.0 ** 10
+    dout[:, -3:] = 2.0 ** 20 * torch.randint(1, 4, (3, 3), generator=gen, device="cuda").float()
+    g = mem.projection_backward(dout, x, w, torch.zeros(O, device="cuda"), float_weight=True)
+    assert torch.equal(g.weight.double(), dout.double().t() @ x.double()) and torch.equal(g.bias.double(), dout.double().sum(0))
+    assert torch.equal(g.x, (dout.double() @ w.double()).half())
+
+
 def test_projection_of_float16_finds_the_size_of_its_gradients_at_every_replay(mem):
     """Captured once, replayed with gradients of other sizes in the same tensor, on a side stream beside eager calls: bit for bit as eager."""
     src = Source(5, torch.float16)
