@@ -124,8 +124,9 @@ template <int V> struct Effect {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const bool cut = o.f.v[j] < 0.0f;
-            // a state of 0 stays one, also where the factor of many parts is infinite (rates above 0)
-            b.v[j] = cut || b.v[j] == 0.0f ? o.b.v[j] : __builtin_fmaf(o.f.v[j], b.v[j], o.b.v[j]);
+            // A state of 0 stays one where the factor of many parts is infinite (rates above 0), and an infinite one where it is below all numbers.
+            constexpr int ZERO_OR_INFINITE = 1 << 2 | 1 << 5 | 1 << 6 | 1 << 9;
+            b.v[j] = cut ? o.b.v[j] : __builtin_fmaf(__builtin_amdgcn_classf(b.v[j], ZERO_OR_INFINITE) ? 1.0f : o.f.v[j], b.v[j], o.b.v[j]);
             f.v[j] = cut || f.v[j] < 0.0f ? -1.0f : f.v[j] * o.f.v[j];
         }
     }

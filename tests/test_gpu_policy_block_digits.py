@@ -276,3 +276,27 @@ def test_recurrence_of_nothing_is_nothing_whatever_its_rate(mem, T, n):
     number = want < 1e38
     got = y[..., 1::2].cpu().double()
     assert bool(((got / want - 1).abs()[number] <= 2.0 ** -11).all()) and bool(number.any(0).all())
+
+
+@pytest.mark.parametrize("T,n", [(2000, 1), (2000, 3), (300, 1), (40, 3000)])
+def test_recurrence_of_infinite_states_and_gradients(mem, T, n):
+    """A state that is infinite stays so, with its sign, until an episode begins, and so does a gradient backwards, in one walk as in parts whose factors
+    are below the smallest number; other channels are as without."""
+    src = Source(T + 1, torch.float32)
+    D, begin = 70, T * 3 // 4
+    t = {k: src.normal(T, n, D) for k in ("x", "decay", "intake")}
+    rate = torch.full((D,), -4.0, device="cuda")
+    args, first = [plain(t[k]) for k in ("x", "decay", "intake")] + [rate], torch.zeros(T, n, dtype=torch.uint8, device="cuda")
+    first[begin] = 1
+    state, dstate = plain(src.normal(n, D)), plain(src.normal(n, D))
+    want, want_h, saved = mem.gated_recurrence(*args, state=state, first=first, save=True)
+    less = mem.gated_recurrence_backward(torch.ones_like(want), saved, *args, state=state, first=first, dstate=dstate)
+    state[:, 3], state[:, 69], dstate[:, 5] = float("inf"), -float("inf"), float("inf")
+    got, got_h, saved = mem.gated_recurrence(*args, state=state, first=first, save=True)
+    assert bool((got[:begin, :, 3] == float("inf")).all()) and bool((got[:begin, :, 69] == -float("inf")).all())
+    others = [c for c in range(D) if c not in (3, 69)]
+    assert torch.equal(got[begin:], want[begin:]) and torch.equal(got_h, want_h) and torch.equal(got[..., others], want[..., others])
+    g = mem.gated_recurrence_backward(torch.ones_like(want), saved, *args, state=state, first=first, dstate=dstate)
+    assert bool((g.x[begin:, :, 5] == float("inf")).all()) and torch.equal(g.x[:begin], less.x[:begin])
+    others = [c for c in range(D) if c != 5]
+    assert torch.equal(g.x[..., others], less.x[..., others])
