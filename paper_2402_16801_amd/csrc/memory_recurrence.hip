@@ -8,7 +8,7 @@
 // forward (1.50 GB, 4.7 TB/s), 650 backward (2.58 GB, 4.0 TB/s, 179 registers, which leave room for two wavefronts per SIMD); a token of 65,536 x 512 113 us (5.2 TB/s).
 //
 // Few environments are split into parts along time: a first kernel finds what each part does to the state (a factor and a term), and each block
-// goes through the parts before its own.  That reads the inputs twice: 10,000 steps of one environment of 512 floats take 32 us in 625
+// goes through the parts before its own.  That reads the inputs twice: 10,000 steps of one environment of 512 floats take 33 us in 625
 // parts, one walk alone would take 10,000 steps' latency.
 #include "memory_api.hpp"
 #include "memory_common.hpp"
